@@ -42,7 +42,7 @@ typedef struct fc_pool fc_pool; /* opaque, owned by the library */
 
 enum { FC_OK = 0, FC_EINVAL = -1, FC_ENOMEM = -2, FC_EDEVICE = -3 };
 enum { FC_METHOD_NONE = 0, FC_METHOD_SNAPKV = 1, FC_METHOD_KNORM = 2, FC_METHOD_STREAMING = 3 };
-enum { FC_DTYPE_F16 = 0 };
+enum { FC_DTYPE_F16 = 0, FC_DTYPE_E4M3 = 1 };
 
 #define FC_BLOCK_SIZE 16      /* tokens per pool block (the only supported value) */
 #define FC_MAX_WINDOW 64      /* largest observation window */
@@ -62,7 +62,9 @@ enum { FC_DTYPE_F16 = 0 };
  *           slot j % 16, for every layer and head.
  * kv_bytes  size of that memory; must be >= n_layers*n_blocks*2*n_heads*16*
  *           head_dim*2.
- * block_size must be 16, head_dim 64 or 128, dtype FC_DTYPE_F16.
+ * block_size must be 16, head_dim 64 or 128, dtype FC_DTYPE_F16 or
+ * FC_DTYPE_E4M3 (8-bit rows, see "The 8-bit pool" below: another layout, and
+ * not every call takes such a pool).
  *
  * The free list is a LIFO stack of block ids held in device memory; a fresh
  * pool holds stack[i] = n_blocks-1-i, top = n_blocks, so that the first
@@ -456,6 +458,128 @@ int fc_decode_attention_kept(fc_pool* pool, const int32_t* dev_block_tables,
                              const int32_t* host_budget, const int32_t* dev_kept,
                              const void* dev_q, float* dev_out, int n_req, float scale,
                              void* stream);
+
+/*
+ * The 8-bit pool: what the stage keeps of a cache, in half the bytes (a decode
+ * step reads every cached row, ExecuteDecoding of Algorithm 1, and the pool
+ * holds twice the tokens, "KV-cache Memory Pool" paragraph).
+ *
+ * A row (the head_dim numbers of one token, head and K or V) is held as e4m3
+ * codes (OCP 8-bit floating point: 3 bits of mantissa, largest value 448) times
+ * one power of two 2^e per row.  For a row x of fp16 numbers, e is the smallest
+ * integer with max |x_c| <= 448 * 2^e, at least -15 (and at most 8, which fp16
+ * never exceeds), and the codes are x_c / 2^e rounded to the nearest e4m3
+ * number, ties to even; with e = 8 codes stop at +-240, so that every value a
+ * row stands for is an fp16 number.  The maximum is that of the finite
+ * channels; a channel that is infinite or not a number becomes not a number.  A
+ * value differs from the written one by at most 2^-4 of it, or 2^-10 * 2^e where
+ * it is smaller than 2^-6 * 2^e.
+ *
+ * Memory (kv_base of a pool of FC_DTYPE_E4M3, 1-byte elements):
+ *     kv[layer][block]{ codes[kv: 0=K, 1=V][head][slot 0..15][head_dim],
+ *                       exponents[kv][head][slot] }       (e + 127, unsigned)
+ * that is 32 * n_heads * (head_dim + 1) bytes per layer and block.
+ *
+ * Calls that take such a pool: fc_pool_* (all), fc_set_debug_checks,
+ * fc_append_batch (the new fp16 rows are quantised as they are written),
+ * fc_decode_attention (reads the 8-bit rows), fc_extend_batch, fc_store_chunk,
+ * fc_chunk_attention, fc_prefill_attention and fc_quantise_batch.  The
+ * compression calls, fc_window_lse and fc_decode_attention_kept return
+ * FC_EINVAL: select and compact in an fp16 pool, then quantise what is kept.
+ *
+ * fc_quantise_batch: the cached rows of a batch, from a pool of FC_DTYPE_F16 to
+ * one of FC_DTYPE_E4M3 with the same layers, heads and head_dim.  For every
+ * request r (with host_enable[r] != 0 if it is given) tokens 0..L_r-1 of all
+ * layers and heads are read through dev_src_tables and written through
+ * dev_dst_tables; slots behind them are left as they are.  No block is popped or
+ * released: fc_extend_batch on the 8-bit pool (lengths 0, n_new = L_r) hands out
+ * the blocks before, fc_pool_free releases the old ones afterwards.
+ * Asynchronous on `stream`.
+ * FC_EINVAL: dtypes or geometries that do not match, a length outside
+ * 0..FC_MAX_SEQ_LEN or beyond either table.
+ */
+int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_blocks_per_req,
+                      fc_pool* src, const int32_t* dev_src_tables, int src_max_blocks_per_req,
+                      const int32_t* host_seq_lens, const int32_t* host_enable, int n_req,
+                      void* stream);
+
+/*
+ * A chunk of new tokens per request (Algorithm 1: P.Store(M.Prefill(batch)), and
+ * the next turn of a request whose cache is there already, compressed or not).
+ * A model's forward pass calls fc_extend_batch once, and in every layer
+ * fc_store_chunk and then fc_chunk_attention, with the lengths that
+ * fc_extend_batch left.  A chunk of one token is the decode step.
+ *
+ * host_n_new    host, int32 [n_req]: new tokens of each request, 0 for requests
+ *               that have none.  The rows of all requests' new tokens lie one
+ *               after the other in batch order ("packed"): T = sum of n_new rows.
+ * fc_rows       packed rows: channel c of head h of row t is element
+ *               t * token_stride + h * head_stride + c of fp16 numbers at data;
+ *               data 16-byte aligned, strides multiples of 8, not negative (rows of q, k and v may
+ *               be parts of one projection's rows).
+ *
+ * fc_extend_batch: request r gets the blocks that n_new_r more tokens need,
+ * ceil((L_r + n_new_r)/16) - ceil(L_r/16) of them, popped in batch order, the
+ * first one for the lowest table entry; host_seq_lens[r] becomes L_r + n_new_r
+ * before the call returns.  FC_EINVAL: L_r or n_new_r < 0, L_r + n_new_r >
+ * FC_MAX_SEQ_LEN or more blocks than a table row holds; FC_ENOMEM: more blocks
+ * needed than are free.  Nothing is modified on error.
+ *
+ * fc_store_chunk: writes the new tokens' K and V rows of one layer to token
+ * positions L_r - n_new_r .. L_r - 1 (L_r = host_seq_lens[r], the new tokens
+ * counted in).  In a pool of FC_DTYPE_E4M3 they are quantised as they are written.
+ *   k, v      packed rows, n_heads heads
+ *
+ * fc_chunk_attention: attention of the new tokens of one layer over the cache,
+ * causal: new token i of request r sees tokens 0 .. L_r - n_new_r + i.  Query
+ * head h reads head h / (n_q_heads / n_heads) of K and V.
+ *   out = softmax(scale * K q) . V      (fp16 rows, fp32 sums, fp16 out;
+ *                                        scale <= 0 means 1/sqrt(head_dim))
+ * The soft-max numerators are rounded to fp16 for the product with V.  A key
+ * that a row does not see has no influence on it, whatever its K and V hold.
+ *   q         packed rows, n_q_heads heads
+ *   out       packed rows, n_q_heads heads, written (no two rows share memory)
+ *   dev_lse   NULL, or fp32 [n_req][n_layers][n_q_heads][window] (4-byte
+ *             aligned): the natural log-sum-exp of scale * q.k over the keys it
+ *             sees for each of the last `window` new tokens, entry window - 1 being the
+ *             last one.  The call writes its layer's entries; a request with
+ *             n_new < window writes its last n_new.  This is what
+ *             fc_compress_batch_lse takes.
+ *
+ * fc_prefill_attention: the same for whole prompts whose K and V need not be in
+ * the pool (yet): token i of prompt r sees tokens 0..i of its own prompt.
+ *   q, k, v, out   packed rows of all prompts, host_seq_lens[r] each; K and V
+ *             with n_heads heads.  The pool gives the geometry; its blocks are
+ *             neither read nor written, and its dtype does not matter.
+ *
+ * All four are asynchronous on `stream`; the attentions may split long caches
+ * over workgroups, whose states lie in memory of the pool.  They are not part
+ * of the kernel times.
+ * FC_EINVAL: layer outside 0..n_layers-1, n_new_r outside 0..L_r, L_r >
+ * FC_MAX_SEQ_LEN or beyond the table, n_q_heads not a multiple of n_heads or
+ * more than FC_MAX_GROUP times it, window < 0 (or < 1 with dev_lse), bad alignment or strides, NULL where
+ * a buffer is needed.
+ */
+#define FC_MAX_GROUP 64 /* most query heads that share a head of K and V */
+typedef struct fc_rows {
+  void* data;           /* dev */
+  int64_t token_stride; /* in elements */
+  int64_t head_stride;
+} fc_rows;
+int fc_extend_batch(fc_pool* pool, int32_t* dev_block_tables, int max_blocks_per_req,
+                    int32_t* host_seq_lens, const int32_t* host_n_new, int n_req, void* stream);
+int fc_store_chunk(fc_pool* pool, int layer, const int32_t* dev_block_tables,
+                   int max_blocks_per_req, const int32_t* host_seq_lens,
+                   const int32_t* host_n_new, const fc_rows* k, const fc_rows* v, int n_req,
+                   void* stream);
+int fc_chunk_attention(fc_pool* pool, int layer, const int32_t* dev_block_tables,
+                       int max_blocks_per_req, const int32_t* host_seq_lens,
+                       const int32_t* host_n_new, const fc_rows* q, int n_q_heads,
+                       const fc_rows* out, float* dev_lse, int window, int n_req, float scale,
+                       void* stream);
+int fc_prefill_attention(fc_pool* pool, int layer, const int32_t* host_seq_lens, const fc_rows* q,
+                         const fc_rows* k, const fc_rows* v, int n_q_heads, const fc_rows* out,
+                         float* dev_lse, int window, int n_req, float scale, void* stream);
 
 /*
  * Host-side scheduler of the compress queue (Algorithm 1, ServeRequests:

@@ -11,7 +11,8 @@ LIB_PATH = os.path.join(PKG_DIR, "libfastcache.so")
 
 # (longest compilations first)
 SOURCES = ["fc_fused_wide_128.hip", "fc_fused_narrow_128.hip", "fc_fused_wide_64.hip", "fc_fused_narrow_64.hip",
-           "fc_mlp.hip", "fc_kernels.hip", "fc_decode.hip", "fc_api.hip", "fc_sched.cpp", "fc_plan.cpp"]
+           "fc_attention.hip", "fc_mlp.hip", "fc_kernels.hip", "fc_decode.hip", "fc_chunk.hip", "fc_api.hip", "fc_chunk_api.hip",
+           "fc_sched.cpp", "fc_plan.cpp", "fc_chunk_plan.cpp"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -7,6 +7,7 @@
 #include "../../include/fastcache.h"
 #include "fc_internal.h"
 #include "fc_plan.h"
+#include "fc_pool.h"
 
 #include <math.h>
 #include <stdarg.h>
@@ -20,10 +21,10 @@
 using namespace fc;
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
 
-int fail(int code, const char* fmt, ...) {
+int fc::fail(int code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
@@ -31,34 +32,7 @@ int fail(int code, const char* fmt, ...) {
   return code;
 }
 
-#define FC_HIP(call)                                                            \
-  do {                                                                          \
-    hipError_t e_ = (call);                                                     \
-    if (e_ != hipSuccess)                                                       \
-      return fail(FC_EDEVICE, "%s failed: %s", #call, hipGetErrorString(e_));   \
-  } while (0)
-
-// The calls of a launch sequence change the pool on the device step by step;
-// if one of them fails after the first has been queued, the device state and
-// the host mirrors no longer agree.  The pool is then marked and every later
-// call on it is refused.
-#define FC_HIP_STAGE(pool, call)                                                    \
-  do {                                                                              \
-    hipError_t e_ = (call);                                                         \
-    if (e_ != hipSuccess) {                                                         \
-      (pool)->poisoned = true;                                                      \
-      return fail(FC_EDEVICE, "%s failed: %s; the pool is now unusable", #call,     \
-                  hipGetErrorString(e_));                                           \
-    }                                                                               \
-  } while (0)
-
-#define FC_CHECK_POOL(pool)                                                         \
-  do {                                                                              \
-    if (!(pool)) return fail(FC_EINVAL, "pool is NULL");                            \
-    if ((pool)->poisoned)                                                           \
-      return fail(FC_EDEVICE, "a device error in an earlier call left this pool in an " \
-                              "undefined state; destroy it");                       \
-  } while (0)
+namespace {
 
 const char* const kKernelNames[K_COUNT] = {"plan_alloc", "snapkv_score", "knorm_score",
                                            "select",     "gather",       "reclaim",
@@ -96,8 +70,6 @@ unsigned char* g_scratch_ptr[kMaxDevices] = {};
 
 size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-constexpr int kProfRing = 32;
-
 }  // namespace
 
 static __device__ __align__(256) unsigned char scratch[kNoAllocBytes];
@@ -121,59 +93,9 @@ int fixed_scratch_of_current_device(unsigned char** out) {
 
 }  // namespace
 
-struct fc_pool;
 namespace {
 int release_verdict(fc_pool* p, hipStream_t stream, const char* what);
 }
-
-struct fc_pool {
-  _Float16* kv = nullptr;
-  size_t kv_bytes = 0;
-  int n_blocks = 0, n_layers = 0, n_heads = 0, head_dim = 0;
-  int32_t* stack = nullptr;  // device
-  int top = 0;               // host mirror, exact
-  bool poisoned = false;     // a launch failed in the middle of a stage: device and host disagree
-  unsigned char* fixed_scratch = nullptr;  // this device's copy of the file-scope scratch array
-  // ownership checks (debug mode): one int per block, 0 free, 1 handed out, 2 being released
-  bool debug_checks = false;
-  int32_t* owner = nullptr;
-  int32_t* check_word = nullptr;  // device: what the last release check found
-
-  // scratch, grown on demand
-  float* raw_scores = nullptr;
-  size_t raw_cap = 0;  // floats
-  int32_t* kept = nullptr;
-  size_t kept_cap = 0;  // ints
-  size_t split_refused = ~(size_t)0;  // least score scratch of split heads that could not be had
-  int32_t* ids = nullptr;
-  size_t ids_cap = 0;  // ints (old ids then new ids)
-  char* dev_meta = nullptr;
-  char* host_meta = nullptr;  // pinned
-  size_t meta_cap = 0;
-  hipEvent_t meta_event = nullptr;
-  bool meta_pending = false;
-
-  int n_cu = 0;                   // compute units of the pool's device
-  float* decode_partial = nullptr;  // states of the segments of a split decode attention
-  int32_t* error_flag = nullptr;  // device, one int, zero unless a kernel found something wrong
-  int32_t* arrivals = nullptr;    // device, the int after it: zero between calls (BatchParams)
-  int score_mode = FC_SCORE_AUTO;
-  bool score_pruning = true;       // the fused kernel prunes the second pass of SnapKV units
-  int n_sink = 4;
-  int compact_mode = FC_COMPACT_FRESH;
-  // chunk-MLP compressor weights in operand order (library-owned)
-  int mlp_k = 0, mlp_hidden = 0, mlp_activation = 0;
-  _Float16* mlp_w1p[2] = {nullptr, nullptr};
-  _Float16* mlp_w2p[2] = {nullptr, nullptr};
-  float* mlp_b1[2] = {nullptr, nullptr};
-  float* mlp_b2[2] = {nullptr, nullptr};
-
-  bool profiling = false;
-  // event ring: the last kProfRing profiled calls, [call][kernel][start, stop]
-  hipEvent_t ev[kProfRing][K_COUNT][2] = {};
-  bool timed[kProfRing][K_COUNT] = {};
-  int prof_calls = 0;  // profiled calls since profiling was last switched on
-};
 
 namespace {
 
@@ -234,10 +156,13 @@ int fc_pool_create(fc_pool** out, void* kv_base, size_t kv_bytes, int n_blocks, 
   if (!kv_base || (reinterpret_cast<uintptr_t>(kv_base) & 255))
     return fail(FC_EINVAL, "kv_base must be a 256-byte aligned device pointer");
   if (block_size != FC_BLOCK_SIZE) return fail(FC_EINVAL, "block_size must be 16");
-  if (dtype != FC_DTYPE_F16) return fail(FC_EINVAL, "dtype must be FC_DTYPE_F16");
+  if (dtype != FC_DTYPE_F16 && dtype != FC_DTYPE_E4M3)
+    return fail(FC_EINVAL, "dtype must be FC_DTYPE_F16 or FC_DTYPE_E4M3");
   if (head_dim != 64 && head_dim != 128) return fail(FC_EINVAL, "head_dim must be 64 or 128");
   if (n_blocks < 1 || n_layers < 1 || n_heads < 1) return fail(FC_EINVAL, "bad pool geometry");
-  const size_t need = (size_t)n_layers * n_blocks * 2 * n_heads * FC_BLOCK_SIZE * head_dim * 2;
+  // (an 8-bit row is a code a channel and one exponent)
+  const size_t row_bytes = dtype == FC_DTYPE_E4M3 ? head_dim + 1 : 2 * head_dim;
+  const size_t need = (size_t)n_layers * n_blocks * 2 * n_heads * FC_BLOCK_SIZE * row_bytes;
   if (kv_bytes < need)
     return fail(FC_EINVAL, "kv_bytes %zu is smaller than the pool geometry needs (%zu)", kv_bytes,
                 need);
@@ -253,6 +178,7 @@ int fc_pool_create(fc_pool** out, void* kv_base, size_t kv_bytes, int n_blocks, 
   p->fixed_scratch = fixed;
   p->n_cu = std::max(n_cu, 1);
   p->kv = static_cast<_Float16*>(kv_base);
+  p->dtype = dtype;
   p->kv_bytes = kv_bytes;
   p->n_blocks = n_blocks;
   p->n_layers = n_layers;
@@ -572,6 +498,7 @@ int compress_batch_impl(fc_pool* p, int32_t* dev_block_tables, int max_blocks_pe
                         bool no_alloc) {
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   FC_CHECK_POOL(p);
+  FC_CHECK_F16(p, "fc_compress_batch");
   if (n_req > 0 && !dev_block_tables) return fail(FC_EINVAL, "NULL argument");
 
   // ---- plan with host-known quantities; nothing is touched on error -----------
@@ -801,6 +728,17 @@ int compress_batch_impl(fc_pool* p, int32_t* dev_block_tables, int max_blocks_pe
 
 }  // namespace
 
+int fc::meta_to_device(fc_pool* p, const void* descs, size_t n_bytes, const void** out, hipStream_t stream) {
+  const size_t bytes = round_up(n_bytes, 16);
+  int rc;
+  if ((rc = grow_meta(p, bytes)) != FC_OK) return rc;
+  std::vector<char> image(bytes, 0);
+  memcpy(image.data(), descs, n_bytes);
+  *out = p->dev_meta;
+  if (capturing(stream)) return upload_meta_arguments(image.data(), bytes, p->dev_meta, stream);
+  return upload_meta_pinned(p, image.data(), bytes, p->dev_meta, stream);
+}
+
 extern "C" {
 
 int fc_compress_batch(fc_pool* p, int32_t* dev_block_tables, int max_blocks_per_req,
@@ -855,6 +793,7 @@ int fc_window_lse(fc_pool* p, const int32_t* dev_block_tables, int max_blocks_pe
                   void* stream_) {
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   FC_CHECK_POOL(p);
+  FC_CHECK_F16(p, "fc_window_lse");
   if (n_req < 0) return fail(FC_EINVAL, "n_req < 0");
   if (n_req == 0) return FC_OK;
   if (!dev_block_tables || !host_seq_lens || !dev_q_window || !dev_lse_out)
@@ -912,6 +851,7 @@ int fc_window_lse(fc_pool* p, const int32_t* dev_block_tables, int max_blocks_pe
 int fc_mlp_set_weights(fc_pool* p, const fc_mlp_weights* w, void* stream_) {
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   if (!p || !w) return fail(FC_EINVAL, "NULL argument");
+  FC_CHECK_F16(p, "fc_mlp_set_weights");
   if (w->k < 1 || w->k > 8) return fail(FC_EINVAL, "k must be in 1..8");
   if (w->hidden != 128 && w->hidden != 256) return fail(FC_EINVAL, "hidden must be 128 or 256");
   if (w->activation != FC_ACT_GELU_ERF && w->activation != FC_ACT_GELU_TANH)
@@ -956,6 +896,7 @@ int fc_compress_batch_mlp(fc_pool* p, int32_t* dev_block_tables, int max_blocks_
                           void* stream_) {
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   FC_CHECK_POOL(p);
+  FC_CHECK_F16(p, "fc_compress_batch_mlp");
   if (p->mlp_k == 0) return fail(FC_EINVAL, "fc_mlp_set_weights has not been called");
   if (n_req > 0 && !dev_block_tables) return fail(FC_EINVAL, "NULL argument");
   MlpPlan plan;
@@ -1080,19 +1021,16 @@ int pass_decode_reqs(fc_pool* p, const std::vector<DecodeReq>& reqs, DecodeParam
     std::copy(reqs.begin(), reqs.end(), inline_reqs->req);
     return FC_OK;
   }
-  const size_t bytes = round_up(reqs.size() * sizeof(DecodeReq), 16);
-  int rc;
-  if ((rc = grow_meta(p, bytes)) != FC_OK) return rc;
-  std::vector<char> image(bytes, 0);
-  memcpy(image.data(), reqs.data(), reqs.size() * sizeof(DecodeReq));
-  dp->reqs = reinterpret_cast<const DecodeReq*>(p->dev_meta);
-  if (capturing(stream)) return upload_meta_arguments(image.data(), bytes, p->dev_meta, stream);
-  return upload_meta_pinned(p, image.data(), bytes, p->dev_meta, stream);
+  const void* on_device = nullptr;
+  if (int rc = meta_to_device(p, reqs.data(), reqs.size() * sizeof(DecodeReq), &on_device, stream)) return rc;
+  dp->reqs = static_cast<const DecodeReq*>(on_device);
+  return FC_OK;
 }
 
 DecodeParams decode_params(fc_pool* p) {
   DecodeParams dp = {};
   dp.kv = p->kv;
+  dp.e4m3 = p->dtype == FC_DTYPE_E4M3 ? 1 : 0;
   dp.n_blocks = p->n_blocks;
   dp.n_layers = p->n_layers;
   dp.n_heads = p->n_heads;
@@ -1110,6 +1048,7 @@ int decode_attention_impl(fc_pool* p, const int32_t* dev_block_tables, int max_b
                           float scale, void* stream_) {
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   FC_CHECK_POOL(p);
+  if (dev_kept) FC_CHECK_F16(p, "fc_decode_attention_kept");
   if (n_req < 0) return fail(FC_EINVAL, "n_req < 0");
   if (n_req == 0) return FC_OK;
   if (!dev_block_tables || !host_seq_lens || !dev_q || !dev_out)

@@ -1,0 +1,147 @@
+#include "fc_chunk_plan.h"
+
+#include <stdarg.h>
+#include <stdio.h>
+
+#include <algorithm>
+
+namespace fc {
+
+namespace {
+
+int blocks_for(int tokens) { return (tokens + kPlanBlockSize - 1) / kPlanBlockSize; }
+
+template <typename Plan>
+int fail(Plan* plan, int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(plan->message, sizeof(plan->message), fmt, ap);
+  va_end(ap);
+  plan->code = code;
+  return code;
+}
+
+constexpr int64_t kMaxRows = 0x7fffffff;
+
+}  // namespace
+
+int plan_extend(const PoolView& pool, int n_req, int max_blocks, const int32_t* seq_lens,
+                const int32_t* n_new, ExtendPlan* plan) {
+  *plan = ExtendPlan();
+  if (n_req < 0) return fail(plan, PLAN_EINVAL, "n_req < 0");
+  if (n_req == 0) return PLAN_OK;
+  if (!seq_lens || !n_new) return fail(plan, PLAN_EINVAL, "NULL argument");
+  if (max_blocks < 1) return fail(plan, PLAN_EINVAL, "max_blocks_per_req < 1");
+  int64_t n_pop = 0;
+  for (int r = 0; r < n_req; ++r) {
+    const int L = seq_lens[r], n = n_new[r];
+    if (L < 0 || n < 0 || L > kPlanMaxSeqLen || n > kPlanMaxSeqLen - L)
+      return fail(plan, PLAN_EINVAL, "request %d: %d tokens and %d new ones outside 0..%d", r, L, n, kPlanMaxSeqLen);
+    const int before = blocks_for(L), after = blocks_for(L + n);
+    if (after > max_blocks)
+      return fail(plan, PLAN_EINVAL, "request %d: %d tokens exceed max_blocks_per_req", r, L + n);
+    if (after == before) continue;
+    plan->reqs.push_back({r, before, after - before, (int32_t)std::min(n_pop, kMaxRows)});
+    n_pop += after - before;
+  }
+  if (n_pop > pool.n_free)
+    return fail(plan, PLAN_ENOMEM, "the new tokens need %lld new blocks, %d free", (long long)n_pop, pool.n_free);
+  plan->n_pop = (int)n_pop;
+  return PLAN_OK;
+}
+
+int plan_chunk(int n_req, int max_blocks, const int32_t* seq_lens, const int32_t* n_new, ChunkPlan* plan) {
+  *plan = ChunkPlan();
+  if (n_req < 0) return fail(plan, PLAN_EINVAL, "n_req < 0");
+  if (n_req == 0) return PLAN_OK;
+  if (!seq_lens) return fail(plan, PLAN_EINVAL, "NULL argument");
+  if (max_blocks == 0 || max_blocks < -1) return fail(plan, PLAN_EINVAL, "max_blocks_per_req < 1");
+  for (int r = 0; r < n_req; ++r) {
+    const int L = seq_lens[r], n = n_new ? n_new[r] : L;
+    if (L < 0 || L > kPlanMaxSeqLen)
+      return fail(plan, PLAN_EINVAL, "request %d: length %d outside 0..%d", r, L, kPlanMaxSeqLen);
+    if (n < 0 || n > L) return fail(plan, PLAN_EINVAL, "request %d: %d new tokens of %d", r, n, L);
+    if (max_blocks > 0 && blocks_for(L) > max_blocks)
+      return fail(plan, PLAN_EINVAL, "request %d: %d tokens exceed max_blocks_per_req", r, L);
+    if (n == 0) continue;
+    if (plan->n_rows + n > kMaxRows) return fail(plan, PLAN_EINVAL, "batch too large for one launch");
+    plan->reqs.push_back({r, L, n, (int32_t)plan->n_rows, 0, 0});
+    plan->n_rows += n;
+  }
+  return PLAN_OK;
+}
+
+void plan_store_units(ChunkPlan* plan) {
+  for (ChunkReq& q : plan->reqs) q.unit_start = q.row_off;
+}
+
+int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, int64_t max_states,
+                   ChunkPlan* plan, AttnLaunch launches[ATTN_SHAPES]) {
+  for (int s = 0; s < ATTN_SHAPES; ++s) launches[s] = AttnLaunch();
+  for (const ChunkReq& q : plan->reqs)
+    launches[(int64_t)q.n_new * group <= kFlatRows ? ATTN_FLAT : ATTN_TALL].reqs.push_back(q);
+  int64_t states_left = may_split ? max_states : 0;
+  for (int s = 0; s < ATTN_SHAPES; ++s) {
+    AttnLaunch& l = launches[s];
+    if (l.reqs.empty()) continue;
+    std::stable_sort(l.reqs.begin(), l.reqs.end(),
+                     [](const ChunkReq& a, const ChunkReq& b) { return a.seq_len > b.seq_len; });
+    const int tile = s == ATTN_TALL ? kTallRows : kFlatRows;
+    auto tiles = [&](const ChunkReq& q) { return ((int64_t)q.n_new * group + tile - 1) / tile; };
+    const int longest = blocks_for(l.reqs.front().seq_len);
+    l.seg_blocks = std::max(longest, 1);
+    int64_t total = 0;  // blocks that workgroups walk, all heads
+    for (const ChunkReq& q : l.reqs) {
+      total += tiles(q) * blocks_for(q.seq_len) * pool.n_heads;
+      l.state_rows += q.n_new;
+    }
+    // As the decode attention (plan_decode_segments): segments of an eighth of a CU's share,
+    // at least 16 blocks, if that is at most half of the longest head.
+    const int64_t n_q_heads = (int64_t)group * pool.n_heads;
+    const int64_t room = states_left / (l.state_rows * n_q_heads);  // segments of a row
+    if (room >= 2) {
+      const int64_t eighth = total / (8 * (int64_t)std::max(n_cu, 1));
+      const int64_t seg = std::max<int64_t>({eighth, 16, (longest + room - 1) / room});
+      if (2 * seg <= longest) {
+        l.seg_blocks = (int)seg;
+        l.n_seg = decode_segments(longest, l.seg_blocks);
+        while (l.n_seg > room) l.n_seg = decode_segments(longest, ++l.seg_blocks);
+        states_left -= l.state_rows * n_q_heads * l.n_seg;
+      }
+    }
+    int64_t state_off = 0;
+    for (ChunkReq& q : l.reqs) {
+      q.unit_start = (int32_t)l.n_units;
+      q.state_off = (int32_t)state_off;
+      state_off += q.n_new;
+      l.n_units += tiles(q) * decode_segments(blocks_for(q.seq_len), l.seg_blocks);
+      if (l.n_units * pool.n_heads > kMaxRows || (int64_t)q.n_new * group > kMaxRows)
+        return fail(plan, PLAN_EINVAL, "batch too large for one launch");
+    }
+  }
+  return PLAN_OK;
+}
+
+int plan_quantise(int n_req, int dst_max_blocks, int src_max_blocks, const int32_t* seq_lens,
+                  const int32_t* enable, ChunkPlan* plan) {
+  *plan = ChunkPlan();
+  if (n_req < 0) return fail(plan, PLAN_EINVAL, "n_req < 0");
+  if (n_req == 0) return PLAN_OK;
+  if (!seq_lens) return fail(plan, PLAN_EINVAL, "NULL argument");
+  if (dst_max_blocks < 1 || src_max_blocks < 1) return fail(plan, PLAN_EINVAL, "max_blocks_per_req < 1");
+  for (int r = 0; r < n_req; ++r) {
+    if (enable && !enable[r]) continue;
+    const int L = seq_lens[r];
+    if (L < 0 || L > kPlanMaxSeqLen)
+      return fail(plan, PLAN_EINVAL, "request %d: length %d outside 0..%d", r, L, kPlanMaxSeqLen);
+    if (blocks_for(L) > std::min(dst_max_blocks, src_max_blocks))
+      return fail(plan, PLAN_EINVAL, "request %d: %d tokens exceed max_blocks_per_req", r, L);
+    if (L == 0) continue;
+    plan->reqs.push_back({r, L, 0, 0, (int32_t)plan->n_rows, 0});
+    plan->n_rows += blocks_for(L);
+    if (plan->n_rows > kMaxRows) return fail(plan, PLAN_EINVAL, "batch too large for one launch");
+  }
+  return PLAN_OK;
+}
+
+}  // namespace fc

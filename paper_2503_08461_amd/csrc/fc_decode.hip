@@ -7,7 +7,7 @@
 
 #include <type_traits>
 
-#include "fc_device.h"
+#include "fc_e4m3.h"
 
 namespace fc {
 
@@ -21,7 +21,9 @@ namespace fc {
 // Reqs (here and below): DecodeReqs, the requests in the arguments, or DecodeReqList,
 // on the device.  Kernels of their own: 3.6 KB of arguments that nobody reads cost a
 // launch of small caches several us.
-template <int D, typename Reqs>
+// kE4M3: an 8-bit pool (fc_e4m3.h); the lanes of a row find its largest magnitude among
+// themselves and write codes and the row's exponent.
+template <int D, bool kE4M3, typename Reqs>
 __global__ __launch_bounds__(kThreads) void append_kernel(DecodeParams p, Reqs reqs) {
   const int r = blockIdx.x / p.n_layers;
   const int layer = blockIdx.x - r * p.n_layers;
@@ -43,8 +45,21 @@ __global__ __launch_bounds__(kThreads) void append_kernel(DecodeParams p, Reqs r
   }
   constexpr int PPR = D / 8;  // 16-byte pieces of a row
   const size_t blk_stride = (size_t)2 * p.n_heads * 16 * D;
-  _Float16* dst = p.kv + ((size_t)layer * p.n_blocks + blk) * blk_stride + (size_t)(L & 15) * D;
   const _Float16* src = p.new_kv + ((size_t)rq.table_row * p.n_layers + layer) * 2 * p.n_heads * D;
+  if constexpr (kE4M3) {
+    uint8_t* block = reinterpret_cast<uint8_t*>(p.kv) +
+                     ((size_t)layer * p.n_blocks + blk) * e4m3_block_bytes(p.n_heads, D);
+    for (int i = threadIdx.x; i < 2 * p.n_heads * PPR; i += kThreads) {  // (whole rows)
+      const int rh = i / PPR, piece = i - rh * PPR;
+      const half8 x = load_half8(src + (size_t)rh * D + piece * 8);
+      const int e = e4m3_exponent(row_max_u32<PPR>(finite_max(x)));
+      const size_t at = (size_t)rh * 16 + (L & 15);
+      *reinterpret_cast<uint2v*>(block + at * D + piece * 8) = e4m3_codes(x, e);
+      if (piece == 0) block[blk_stride + at] = (uint8_t)e;
+    }
+    return;
+  }
+  _Float16* dst = p.kv + ((size_t)layer * p.n_blocks + blk) * blk_stride + (size_t)(L & 15) * D;
   for (int i = threadIdx.x; i < 2 * p.n_heads * PPR; i += kThreads) {
     const int rh = i / PPR, piece = i - rh * PPR;  // rh = kv * n_heads + head
     store_half8(dst + (size_t)rh * 16 * D + piece * 8, load_half8(src + (size_t)rh * D + piece * 8));
@@ -66,10 +81,14 @@ hipError_t launch_append(const DecodeParams& p, const DecodeReqs& inline_reqs, h
   const unsigned grid = (unsigned)p.n_req * p.n_layers;
   with_reqs(p, inline_reqs, [&](const auto& reqs) {
     using Reqs = std::decay_t<decltype(reqs)>;
-    if (p.head_dim == 128)
-      append_kernel<128, Reqs><<<grid, kThreads, 0, s>>>(p, reqs);
+    if (p.head_dim == 128 && p.e4m3)
+      append_kernel<128, true, Reqs><<<grid, kThreads, 0, s>>>(p, reqs);
+    else if (p.head_dim == 128)
+      append_kernel<128, false, Reqs><<<grid, kThreads, 0, s>>>(p, reqs);
+    else if (p.e4m3)
+      append_kernel<64, true, Reqs><<<grid, kThreads, 0, s>>>(p, reqs);
     else
-      append_kernel<64, Reqs><<<grid, kThreads, 0, s>>>(p, reqs);
+      append_kernel<64, false, Reqs><<<grid, kThreads, 0, s>>>(p, reqs);
   });
   return hipGetLastError();
 }
@@ -246,6 +265,159 @@ __global__ __launch_bounds__(kThreads) void decode_attention_kernel(DecodeParams
   }
 }
 
+// ---------------------------------------------------------------------------
+// The same over an 8-bit pool: a lane has 16 channels of a row (16 bytes), so D / 16
+// neighbouring lanes a row and 1024 / D rows a load instruction.  Codes become fp32 numbers
+// (exactly); the row's power of two multiplies the key's logit and the value's weight.
+// ---------------------------------------------------------------------------
+
+// sum over the LPR neighbouring lanes of a row (4 or 8), in every one of them
+template <int LPR>
+__device__ __forceinline__ float short_row_sum(float s) {
+  s += from_lane<0xB1>(s);
+  s += from_lane<0x4E>(s);
+  if constexpr (LPR == 8) s += from_lane<0x141>(s);
+  return s;
+}
+
+__device__ __forceinline__ void values_of(uint4v codes, float (&f)[16]) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[w], false);
+    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[w], true);
+    f[4 * w] = lo[0];
+    f[4 * w + 1] = lo[1];
+    f[4 * w + 2] = hi[0];
+    f[4 * w + 3] = hi[1];
+  }
+}
+
+template <int D, bool kCut, typename Reqs>
+__global__ __launch_bounds__(kThreads) void decode_attention_e4m3_kernel(DecodeParams p, Reqs reqs) {
+  constexpr int LPR = D / 16;
+  constexpr int RPI = 64 / LPR;
+  constexpr int IPB = 16 / RPI;
+  constexpr int NG = kWaves * RPI;
+  const int n_lh = p.n_layers * p.n_heads;
+  const int unit = kCut ? blockIdx.x % (p.n_req * n_lh) : blockIdx.x;
+  const int seg = kCut ? blockIdx.x / (p.n_req * n_lh) : 0;
+  const int slot = unit / n_lh;
+  const int lh = unit - slot * n_lh;
+  const DecodeReq rq = reqs.req[slot];
+  const int L = rq.seq_len;
+  const int nb = (L + 15) >> 4;
+  const int n_seg = kCut ? decode_segments(nb, p.seg_blocks) : 1;
+  if (seg >= n_seg) return;  // uniform: this request has fewer segments
+  const int b0 = kCut ? decode_segment_begin(nb, n_seg, seg) : 0;
+  const int b1 = kCut ? decode_segment_begin(nb, n_seg, seg + 1) : nb;
+  const int layer = lh / p.n_heads;
+  const int head = lh - layer * p.n_heads;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int grp = lane / LPR;    // which row of a load instruction
+  const int piece = lane % LPR;  // which 16 channels
+  float* out = p.out + ((size_t)rq.table_row * n_lh + lh) * D;
+
+  const _Float16* qp = p.q + ((size_t)rq.table_row * n_lh + lh) * D + piece * 16;
+  float qf[16];
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const half8 qh = load_half8(qp + 8 * half);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) qf[8 * half + e] = (float)qh[e] * p.scale_log2e;
+  }
+  const int32_t* row = p.block_tables + (size_t)rq.table_row * p.max_blocks;
+  const size_t blk_stride = e4m3_block_bytes(p.n_heads, D);
+  const size_t v_off = (size_t)p.n_heads * 16 * D;
+  const uint8_t* base = reinterpret_cast<const uint8_t*>(p.kv) + (size_t)layer * p.n_blocks * blk_stride;
+  const size_t code_at = ((size_t)head * 16 + grp) * D + piece * 16;
+  const size_t exp_at = 2 * v_off + (size_t)head * 16 + grp;
+
+  float m = -INFINITY, z = 0.f, acc[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  struct Rows {
+    uint4v k[IPB], v[IPB];
+    uint32_t ke[IPB], ve[IPB];
+  };
+  auto fetch = [&](int b, Rows& x) {
+    const uint8_t* block = base + (size_t)clamp_block(row[b], p.n_blocks) * blk_stride;
+#pragma unroll
+    for (int i = 0; i < IPB; ++i) {
+      x.k[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4v*>(block + code_at + (size_t)i * RPI * D));
+      x.v[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4v*>(block + code_at + v_off + (size_t)i * RPI * D));
+      x.ke[i] = block[exp_at + i * RPI];
+      x.ve[i] = block[exp_at + (size_t)p.n_heads * 16 + i * RPI];
+    }
+  };
+  auto attend = [&](int b, const Rows& x) {
+#pragma unroll
+    for (int i = 0; i < IPB; ++i) {
+      float f[16];
+      values_of(x.k[i], f);
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s += qf[e] * f[e];
+      s = short_row_sum<LPR>(s) * e4m3_scale(x.ke[i]);
+      const int tok = b * 16 + i * RPI + grp;
+      if (tok < L) {  // the whole lane group takes the same branch
+        const float mn = fmaxf(m, s);
+        const float a = __builtin_amdgcn_exp2f(m - mn);  // 0 for the first token (m = -inf)
+        const float w = __builtin_amdgcn_exp2f(s - mn);
+        z = z * a + w;
+        const float wv = w * e4m3_scale(x.ve[i]);
+        values_of(x.v[i], f);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] = acc[e] * a + wv * f[e];
+        m = mn;
+      }
+    }
+  };
+  if constexpr (kCut) {
+    stream_tiles<Rows>(
+        own_tiles(b1 - b0, wave, kWaves), [&](int i, Rows& x) { fetch(b0 + wave + kWaves * i, x); },
+        [&](int i, const Rows& x) { attend(b0 + wave + kWaves * i, x); });
+  } else {
+    for (int b = wave; b < nb; b += kWaves) {
+      Rows x;
+      fetch(b, x);
+      attend(b, x);
+    }
+  }
+
+  // merge the NG states, as above
+  __shared__ float sm_m[NG], sm_z[NG];
+  __shared__ float sm_acc[NG][D];
+  const int g = wave * RPI + grp;
+  if (piece == 0) {
+    sm_m[g] = m;
+    sm_z[g] = z;
+  }
+#pragma unroll
+  for (int e = 0; e < 16; ++e) sm_acc[g][piece * 16 + e] = acc[e];
+  __syncthreads();
+  float mm = -INFINITY, zz = 0.f, o = 0.f;
+  if (threadIdx.x < D) {
+    for (int i = 0; i < NG; ++i) mm = fmaxf(mm, sm_m[i]);
+    for (int i = 0; i < NG; ++i) {
+      // (a sum of zero: no token; not a number stays not a number)
+      const float f = sm_z[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(sm_m[i] - mm);
+      zz += sm_z[i] * f;
+      o += sm_acc[i][threadIdx.x] * f;
+    }
+  }
+  if (n_seg == 1) {  // uniform
+    if (threadIdx.x < D) out[threadIdx.x] = L > 0 ? o / zz : 0.f;
+    return;
+  }
+  float* mine = p.partial + (((size_t)slot * n_lh + lh) * p.n_seg + seg) * DecodeParams::state_words(D);
+  if (threadIdx.x < D) mine[threadIdx.x] = o;
+  if (threadIdx.x == 0) {
+    mine[D] = mm;
+    mine[D + 1] = zz;
+  }
+}
+
 // segments of at least 16 blocks, of a head of at most 32768 tokens
 static constexpr int kMaxHeadSegments = kPlanMaxSeqLen / kPlanBlockSize / 16;
 
@@ -293,10 +465,34 @@ static void launch_decode_one(const DecodeParams& p, const DecodeReqs& inline_re
   });
 }
 
+template <int D>
+static void launch_decode_e4m3(const DecodeParams& p, const DecodeReqs& inline_reqs, hipStream_t s) {
+  const unsigned heads = (unsigned)p.n_req * p.n_layers * p.n_heads;
+  with_reqs(p, inline_reqs, [&](const auto& reqs) {
+    using Reqs = std::decay_t<decltype(reqs)>;
+    if (p.n_seg == 1) {
+      decode_attention_e4m3_kernel<D, false, Reqs><<<heads, kThreads, 0, s>>>(p, reqs);
+      return;
+    }
+    decode_attention_e4m3_kernel<D, true, Reqs><<<heads * p.n_seg, kThreads, 0, s>>>(p, reqs);
+    decode_merge_kernel<D, false, Reqs><<<heads, D, 0, s>>>(p, reqs);
+  });
+}
+
 hipError_t launch_decode_attention(const DecodeParams& p, const DecodeReqs& inline_reqs, hipStream_t s) {
   if (p.n_req == 0) return hipSuccess;
   if (p.n_seg < 1 || p.n_seg > kMaxHeadSegments || p.seg_blocks < 1) return hipErrorInvalidValue;
   const bool indexed = p.kept != nullptr;
+  if (p.e4m3) {  // (whole caches only)
+    if (indexed) return hipErrorInvalidValue;
+    if (p.head_dim == 128)
+      launch_decode_e4m3<128>(p, inline_reqs, s);
+    else if (p.head_dim == 64)
+      launch_decode_e4m3<64>(p, inline_reqs, s);
+    else
+      return hipErrorInvalidValue;
+    return hipGetLastError();
+  }
   if (p.head_dim == 128 && !indexed)
     launch_decode_one<128, false>(p, inline_reqs, s);
   else if (p.head_dim == 128)

@@ -37,6 +37,7 @@ static constexpr size_t kMaxArgumentBytes = 4096;  // what the arguments of a ke
 
 struct DecodeParams {
   _Float16* kv;
+  int32_t e4m3;  // 1: the pool's rows are 8-bit (fc_e4m3.h), kv counts bytes
   int32_t n_blocks, n_layers, n_heads, head_dim;
   const int32_t* stack;  // free stack (append: new blocks are stack[top_before - 1 - pop_index])
   int32_t top_before;
@@ -60,6 +61,87 @@ struct DecodeParams {
   static constexpr int state_words(int head_dim) { return head_dim + 32; }
 };
 static_assert(sizeof(DecodeParams) + sizeof(DecodeReqs) <= kMaxArgumentBytes, "decode kernels");
+
+// Requests of the calls on chunks of new tokens, as arguments or on the device (DecodeReqs).
+struct ExtendReqs {
+  static constexpr int kInline = 3584 / sizeof(ExtendReq);  // 224
+  ExtendReq req[kInline];
+};
+struct ExtendReqList {
+  const ExtendReq* req;
+};
+struct ChunkReqs {
+  static constexpr int kInline = 3584 / sizeof(ChunkReq);  // 149
+  ChunkReq req[kInline];
+};
+struct ChunkReqList {
+  const ChunkReq* req;
+};
+static_assert(sizeof(ExtendReq) == 16 && sizeof(ChunkReq) == 24, "tests count on the sizes of descriptors");
+
+struct ExtendParams {
+  const int32_t* stack;
+  int32_t top_before, n_blocks;
+  int32_t* block_tables;
+  int32_t max_blocks;
+  const ExtendReq* reqs;  // NULL: in the ExtendReqs argument
+  int32_t n_req;
+  int32_t* owner;  // ownership checks (debug mode), else NULL
+  int32_t* error_flag;
+};
+
+struct RowsView {  // packed rows (fc_rows)
+  _Float16* data;
+  int64_t token_stride, head_stride;
+};
+
+struct StoreParams {
+  void* kv;  // the layer's blocks
+  int32_t e4m3;
+  int32_t n_blocks, n_heads, head_dim;
+  const int32_t* block_tables;
+  int32_t max_blocks;
+  const ChunkReq* reqs;  // NULL: in the ChunkReqs argument
+  int32_t n_req;
+  int32_t n_rows;
+  RowsView k, v;
+};
+
+struct QuantiseParams {
+  const _Float16* src;
+  uint8_t* dst;
+  int32_t src_blocks, dst_blocks, n_layers, n_heads, head_dim;
+  const int32_t *src_tables, *dst_tables;
+  int32_t src_max_blocks, dst_max_blocks;
+  const ChunkReq* reqs;  // NULL: in the ChunkReqs argument
+  int32_t n_req;
+  int32_t n_units;  // blocks of all requests
+};
+
+enum { ATTN_ROWS = 0, ATTN_F16 = 1, ATTN_E4M3 = 2 };  // where K and V are: packed rows, a pool
+struct AttnParams {
+  const void* kv;  // the layer's blocks
+  int32_t source;  // ATTN_*
+  int32_t n_blocks, n_heads, group, head_dim;
+  const int32_t* block_tables;
+  int32_t max_blocks;
+  const ChunkReq* reqs;  // NULL: in the ChunkReqs argument
+  int32_t n_req;
+  int32_t n_units;       // row tiles x segments of all requests
+  int32_t seg_blocks, n_seg;
+  int32_t state_rows;    // rows (tokens) of the requests of this launch
+  RowsView q, k, v, out;
+  float* lse;            // nullable: this layer's [head][window] of request 0
+  int64_t lse_stride;    // between requests
+  int32_t window;
+  float scale_log2e;
+  float* states;         // [row][head][n_seg][DecodeParams::state_words]
+};
+static_assert(sizeof(AttnParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
+                  sizeof(StoreParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
+                  sizeof(QuantiseParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
+                  sizeof(ExtendParams) + sizeof(ExtendReqs) <= kMaxArgumentBytes,
+              "kernels of chunks");
 
 // Everything a kernel of the stage needs.  Passed by value.
 struct BatchParams {
@@ -187,6 +269,12 @@ hipError_t kernels_one_time_setup();
 // decode-side pool traffic (fc_decode.hip)
 hipError_t launch_append(const DecodeParams& p, const DecodeReqs& inline_reqs, hipStream_t s);
 hipError_t launch_decode_attention(const DecodeParams& p, const DecodeReqs& inline_reqs, hipStream_t s);
+// chunks of new tokens: blocks, rows into the pool, fp16 pool to 8-bit pool (fc_chunk.hip)
+hipError_t launch_extend(const ExtendParams& p, const ExtendReqs& inline_reqs, hipStream_t s);
+hipError_t launch_store_chunk(const StoreParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
+hipError_t launch_quantise(const QuantiseParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
+// ... and their attention (fc_attention.hip); flat: few rows a request (ATTN_FLAT)
+hipError_t launch_attention(const AttnParams& p, bool flat, const ChunkReqs& inline_reqs, hipStream_t s);
 // chunk-MLP compressor (fc_mlp.hip)
 hipError_t mlp_one_time_setup();
 size_t mlp_w1p_elems(int head_dim, int hidden, int k);

@@ -48,4 +48,23 @@ struct DecodeReq {
   int64_t kept_off;   // attention over a kept list: start of [layer][head][budget] in `kept`
 };
 
+// One request of fc_extend_batch that gets blocks.
+struct ExtendReq {
+  int32_t table_row;
+  int32_t first;      // table entry of its first new block
+  int32_t n_pop;      // new blocks
+  int32_t pop_index;  // which pop of this call gives it the first one
+};
+
+// One request with new rows: of fc_store_chunk, of a chunk's or a prompt's attention, or (no
+// rows, units of blocks) of fc_quantise_batch.
+struct ChunkReq {
+  int32_t table_row;   // row of dev_block_tables, of dev_lse
+  int32_t seq_len;     // keys, the new tokens counted in
+  int32_t n_new;       // new tokens
+  int32_t row_off;     // its first packed row
+  int32_t unit_start;  // first work unit of this request in the launch
+  int32_t state_off;   // attention that is split: its first row among the rows that have states
+};
+
 }  // namespace fc

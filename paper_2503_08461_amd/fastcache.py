@@ -13,7 +13,7 @@ import numpy as np
 
 FC_OK, FC_EINVAL, FC_ENOMEM, FC_EDEVICE = 0, -1, -2, -3
 FC_METHOD_NONE, FC_METHOD_SNAPKV, FC_METHOD_KNORM, FC_METHOD_STREAMING = 0, 1, 2, 3
-FC_DTYPE_F16 = 0
+FC_DTYPE_F16, FC_DTYPE_E4M3 = 0, 1
 FC_BLOCK_SIZE = 16
 FC_N_KERNELS = 11
 FC_SCORE_AUTO, FC_SCORE_TWO_PASS = 0, 1
@@ -29,6 +29,7 @@ EXPORTS = [
     "fc_compress_batch", "fc_compress_batch_noalloc", "fc_compress_batch_var", "fc_compress_batch_lse", "fc_window_lse",
     "fc_append_batch", "fc_decode_attention",
     "fc_decode_attention_kept",
+    "fc_extend_batch", "fc_store_chunk", "fc_chunk_attention", "fc_prefill_attention", "fc_quantise_batch",
     "fc_mlp_set_weights", "fc_compress_batch_mlp", "fc_set_compaction_mode", "fc_set_streaming_sinks", "fc_set_score_mode", "fc_set_score_pruning", "fc_set_debug_checks", "fc_set_profiling", "fc_get_kernel_times",
     "fc_kernel_name", "fc_last_error",
     "fc_sched_create", "fc_sched_destroy", "fc_sched_submit", "fc_sched_pending",
@@ -44,6 +45,12 @@ class MlpWeights(ctypes.Structure):
     _fields_ = [("k", ctypes.c_int), ("hidden", ctypes.c_int), ("activation", ctypes.c_int),
                 ("w1", ctypes.c_void_p * 2), ("b1", ctypes.c_void_p * 2),
                 ("w2", ctypes.c_void_p * 2), ("b2", ctypes.c_void_p * 2)]
+
+
+class Rows(ctypes.Structure):
+    """struct fc_rows"""
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
 
 
 class FastCacheError(RuntimeError):
@@ -99,6 +106,14 @@ def load_library():
     lib.fc_decode_attention.argtypes = [vp, vp, i, i32p, vp, vp, i, ctypes.c_float, vp]
     lib.fc_decode_attention_kept.argtypes = [vp, vp, i, i32p, i32p, vp, vp, vp, i, ctypes.c_float,
                                              vp]
+    rows = ctypes.POINTER(Rows)
+    lib.fc_extend_batch.argtypes = [vp, vp, i, i32p, i32p, i, vp]
+    lib.fc_store_chunk.argtypes = [vp, i, vp, i, i32p, i32p, rows, rows, i, vp]
+    lib.fc_chunk_attention.argtypes = [vp, i, vp, i, i32p, i32p, rows, i, rows, vp, i, i,
+                                       ctypes.c_float, vp]
+    lib.fc_prefill_attention.argtypes = [vp, i, i32p, rows, rows, rows, i, rows, vp, i, i,
+                                         ctypes.c_float, vp]
+    lib.fc_quantise_batch.argtypes = [vp, vp, i, vp, vp, i, i32p, i32p, i, vp]
     lib.fc_mlp_set_weights.argtypes = [vp, ctypes.POINTER(MlpWeights), vp]
     lib.fc_compress_batch_mlp.argtypes = [vp, vp, i, i32p, i32p, i32p, i32p, i, vp]
     lib.fc_set_score_mode.argtypes = [vp, i]
@@ -147,6 +162,18 @@ def _dev_ptr(t, dtype=None):
     return t.data_ptr()
 
 
+def _rows(t, name, n_rows, n_heads, head_dim):
+    """fc_rows of a [row][head][channel] fp16 tensor; rows and heads may be strided."""
+    import torch
+    if not t.is_cuda or t.dtype != torch.float16 or tuple(t.shape) != (n_rows, n_heads, head_dim):
+        raise ValueError("%s must be a fp16 device tensor of shape %s" % (name, (n_rows, n_heads, head_dim)))
+    if t.stride(2) != 1:
+        raise ValueError("%s must have its channels next to each other" % name)
+    # (an axis of one element may have any stride)
+    return Rows(t.data_ptr(), t.stride(0) if n_rows > 1 else n_heads * head_dim,
+                t.stride(1) if n_heads > 1 else head_dim)
+
+
 def _stream_ptr(stream):
     if stream is not None:
         return stream.cuda_stream
@@ -187,14 +214,18 @@ class PoolHandle:
             n_blocks, n_layers, n_heads, head_dim
 
 
-def fc_pool_create(kv, n_blocks, n_layers, n_heads, head_dim, block_size=FC_BLOCK_SIZE):
-    """kv: torch fp16 device tensor holding kv[layer][block][2][head][16][head_dim]."""
+def fc_pool_create(kv, n_blocks, n_layers, n_heads, head_dim, block_size=FC_BLOCK_SIZE,
+                   dtype=FC_DTYPE_F16):
+    """kv: torch fp16 device tensor holding kv[layer][block][2][head][16][head_dim]; with
+    dtype FC_DTYPE_E4M3 a uint8 one, per layer and block the codes [2][head][16][head_dim]
+    and then the exponents [2][head][16]."""
     import torch
     lib = load_library()
     out = ctypes.c_void_p()
-    _check(lib.fc_pool_create(ctypes.byref(out), _dev_ptr(kv, torch.float16),
+    want = torch.uint8 if dtype == FC_DTYPE_E4M3 else torch.float16
+    _check(lib.fc_pool_create(ctypes.byref(out), _dev_ptr(kv, want),
                               kv.numel() * kv.element_size(), n_blocks, block_size,
-                              n_layers, n_heads, head_dim, FC_DTYPE_F16))
+                              n_layers, n_heads, head_dim, int(dtype)))
     return PoolHandle(out, kv, n_blocks, n_layers, n_heads, head_dim)
 
 
@@ -446,6 +477,111 @@ def fc_decode_attention_kept(pool, block_tables, seq_lens, budget, kept, q, out=
         _dev_ptr(q, torch.float16), _dev_ptr(out, torch.float32), n_req, float(scale),
         _stream_ptr(stream)))
     return out
+
+
+def _new_rows(block_tables, seq_lens, n_new):
+    """(requests, packed rows) of a call on new tokens."""
+    n_req = int(seq_lens.shape[0])
+    if block_tables.dim() != 2 or block_tables.shape[0] != n_req:
+        raise ValueError("block_tables must be [n_req][max_blocks]")
+    if n_new.shape[0] != n_req:
+        raise ValueError("n_new must have n_req entries")
+    return n_req, int(n_new.sum(dtype=np.int64))
+
+
+def fc_extend_batch(pool, block_tables, seq_lens, n_new, stream=None):
+    """Blocks for n_new (int32 numpy [n_req]) more tokens of every request; block_tables
+    (int32 device tensor) and seq_lens (int32 numpy) are updated."""
+    import torch
+    lib = load_library()
+    n_req, _ = _new_rows(block_tables, seq_lens, n_new)
+    _check(lib.fc_extend_batch(pool.ptr, _dev_ptr(block_tables, torch.int32), int(block_tables.shape[1]),
+                               _host_i32(seq_lens), _host_i32(n_new), n_req, _stream_ptr(stream)))
+
+
+def fc_store_chunk(pool, layer, block_tables, seq_lens, n_new, k, v, stream=None):
+    """K and V of the new tokens of one layer into the pool.  k, v: fp16 device tensors
+    [sum n_new][n_heads][head_dim], packed in batch order, rows and heads may be strided;
+    seq_lens: with the new tokens counted in."""
+    import torch
+    lib = load_library()
+    n_req, n_rows = _new_rows(block_tables, seq_lens, n_new)
+    _check(lib.fc_store_chunk(
+        pool.ptr, int(layer), _dev_ptr(block_tables, torch.int32), int(block_tables.shape[1]),
+        _host_i32(seq_lens), _host_i32(n_new),
+        ctypes.byref(_rows(k, "k", n_rows, pool.n_heads, pool.head_dim)),
+        ctypes.byref(_rows(v, "v", n_rows, pool.n_heads, pool.head_dim)), n_req, _stream_ptr(stream)))
+
+
+def _lse_ptr(pool, lse_out, n_req, n_q_heads, window):
+    import torch
+    if lse_out is not None and tuple(lse_out.shape) != (n_req, pool.n_layers, n_q_heads, window):
+        raise ValueError("lse_out must be [n_req][n_layers][n_q_heads][window]")
+    return _dev_ptr(lse_out, torch.float32)
+
+
+def fc_chunk_attention(pool, layer, block_tables, seq_lens, n_new, q, out=None, lse_out=None,
+                       window=0, scale=0.0, stream=None):
+    """Causal attention of the new tokens of one layer over the cache.  q: fp16 device tensor
+    [sum n_new][n_q_heads][head_dim], strided like fc_store_chunk's k; returns out, fp16 of the
+    same shape (created if None).  lse_out: fp32 [n_req][n_layers][n_q_heads][window], the
+    log-sum-exps of each request's last `window` new tokens, or None."""
+    import torch
+    lib = load_library()
+    n_req, n_rows = _new_rows(block_tables, seq_lens, n_new)
+    n_q = int(q.shape[1])
+    if out is None:
+        out = torch.empty((n_rows, n_q, pool.head_dim), dtype=torch.float16, device=q.device)
+    _check(lib.fc_chunk_attention(
+        pool.ptr, int(layer), _dev_ptr(block_tables, torch.int32), int(block_tables.shape[1]),
+        _host_i32(seq_lens), _host_i32(n_new),
+        ctypes.byref(_rows(q, "q", n_rows, n_q, pool.head_dim)), n_q,
+        ctypes.byref(_rows(out, "out", n_rows, n_q, pool.head_dim)),
+        _lse_ptr(pool, lse_out, n_req, n_q, window), int(window), n_req, float(scale),
+        _stream_ptr(stream)))
+    return out
+
+
+def fc_prefill_attention(pool, layer, q, k, v, seq_lens, out=None, lse_out=None, window=0, scale=0.0,
+                         stream=None):
+    """Causal attention of whole prompts, packed one after the other (seq_lens: int32 numpy
+    [n_req]).  q: fp16 device tensor [sum seq_lens][n_q_heads][head_dim], k and v with the
+    pool's n_heads; rows and heads may be strided.  Returns out, fp16 of q's shape (created if
+    None); lse_out as for fc_chunk_attention."""
+    import torch
+    lib = load_library()
+    n_req, n_rows = int(seq_lens.shape[0]), int(seq_lens.sum(dtype=np.int64))
+    n_q = int(q.shape[1])
+    if out is None:
+        out = torch.empty((n_rows, n_q, pool.head_dim), dtype=torch.float16, device=q.device)
+    _check(lib.fc_prefill_attention(
+        pool.ptr, int(layer), _host_i32(seq_lens),
+        ctypes.byref(_rows(q, "q", n_rows, n_q, pool.head_dim)),
+        ctypes.byref(_rows(k, "k", n_rows, pool.n_heads, pool.head_dim)),
+        ctypes.byref(_rows(v, "v", n_rows, pool.n_heads, pool.head_dim)), n_q,
+        ctypes.byref(_rows(out, "out", n_rows, n_q, pool.head_dim)),
+        _lse_ptr(pool, lse_out, n_req, n_q, window), int(window), n_req, float(scale),
+        _stream_ptr(stream)))
+    return out
+
+
+def fc_quantise_batch(pool, block_tables, src_pool, src_block_tables, seq_lens, enable=None, stream=None):
+    """Copies the cached rows of a batch from an fp16 pool (src_pool, through src_block_tables)
+    into an 8-bit one (pool, through block_tables, whose blocks the caller has from
+    fc_extend_batch); seq_lens, enable: int32 numpy arrays [n_req]."""
+    import torch
+    lib = load_library()
+    n_req = int(seq_lens.shape[0])
+    for t in (block_tables, src_block_tables):
+        if t.dim() != 2 or t.shape[0] != n_req:
+            raise ValueError("block tables must be [n_req][max_blocks]")
+    if enable is not None and enable.shape[0] != n_req:
+        raise ValueError("enable must have n_req entries")
+    _check(lib.fc_quantise_batch(
+        pool.ptr, _dev_ptr(block_tables, torch.int32), int(block_tables.shape[1]),
+        src_pool.ptr, _dev_ptr(src_block_tables, torch.int32), int(src_block_tables.shape[1]),
+        _host_i32(seq_lens), _host_i32(enable) if enable is not None else None, n_req,
+        _stream_ptr(stream)))
 
 
 def fc_mlp_set_weights(pool, k, w1, b1, w2, b2, activation=FC_ACT_GELU_ERF, stream=None):
