@@ -17,10 +17,8 @@
 // products in fp32, p rounded to fp16 for the matrix cores (a relative 2^-11 each, where the
 // result itself is rounded to as much).
 //
-// Shapes of a workgroup: four wavefronts of 32 rows each over the same keys (kRowWaves 4:
-// prompts and long chunks, bound by the matrix cores), or four wavefronts over the same 32
-// rows, each with a quarter of every tile's keys (kRowWaves 1: single tokens and short
-// chunks, bound by memory), whose states are joined through LDS.
+// Two kernels: many rows (prompts, long chunks; bound by the matrix cores) and few rows (single
+// tokens, short chunks; bound by memory).
 
 #include <type_traits>
 
@@ -36,22 +34,8 @@ typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef __fp16 fp16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) fp16x4* LdsQuad;
 
-constexpr int kWaveRows = 32;
+constexpr float kSlack = 8.f;
 constexpr float kLn2 = 0.69314718055994530942f;
-
-template <int D, int WM, int WK, int SRC>
-struct AttnShape {
-  static constexpr int kThreads = 64 * WM * WK;
-  static constexpr int kRows = kWaveRows * WM;
-  static constexpr int kSub = WK == 1 ? 2 : 1;    // 32-key subtiles of a wavefront's share of a tile
-  static constexpr int kKeys = 32 * kSub * WK;    // keys of a tile
-  static constexpr int kElems = SRC == ATTN_E4M3 ? 16 : 8;  // channels of 16 bytes
-  static constexpr int kLanesPerRow = D / kElems;
-  static constexpr int kRowsPerPiece = kThreads / kLanesPerRow;
-  static constexpr int kPieces = kKeys / kRowsPerPiece;  // 16-byte pieces a thread brings in, of K and of V
-  static constexpr int kLdsBytes = 2 * kKeys * D * 2;
-  static_assert(kPieces * kRowsPerPiece == kKeys, "whole tiles");
-};
 
 // Where 16-byte chunk c of key row r lies in a tile: rows of D / 8 chunks, permuted within
 // the row so that the lanes of one read hit all banks.  K is read as 32 rows at one chunk,
@@ -103,131 +87,74 @@ __device__ __forceinline__ half8 finite_only(half8 x) {
   return x;
 }
 
-template <int D, int WM, int WK, int SRC, bool kSplit, typename Reqs>
-__global__ __launch_bounds__(64 * WM * WK) void attention_kernel(AttnParams p, Reqs reqs) {
-  using Shape = AttnShape<D, WM, WK, SRC>;
-  constexpr int kKeys = Shape::kKeys, kSub = Shape::kSub, kPieces = Shape::kPieces;
-  constexpr int DT = D / 32;  // 32-channel tiles of the result
-  constexpr int KK = D / 16;  // slabs of the first product
-  extern __shared__ __align__(16) half8 sm[];
-  half8* sm_k = sm;
-  half8* sm_v = sm + kKeys * D / 8;
+// Loads from memory straight to LDS: lane l's 16 bytes go to to[l].
+typedef __amdgpu_buffer_rsrc_t BufferPtr;
+__device__ __forceinline__ BufferPtr buffer_of(const void* base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ void load_to_lds(BufferPtr from, int lane_offset, int offset, half8* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, lane_offset, offset,
+                                           0, 0);
+}
+// V's operand: lane l gets, of the four rows that the sixteen lanes around it point to (four
+// lanes a row, 8 bytes each), channel l % 16.  (restrict: without it the compiler waits for
+// every load to LDS that is on its way; the waits that are needed are written out.)
+__device__ __forceinline__ fp16x4 read_columns(const _Float16* __restrict at) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4f16((LdsQuad)at);
+}
+// Waits until at most N of the wavefront's vector memory accesses are on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "six bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
+}
+// A barrier that leaves vector memory accesses on their way.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
-  const int unit = blockIdx.x / p.n_heads;
-  const int head = blockIdx.x - unit * p.n_heads;
-  const ChunkReq rq = reqs.req[request_of(reqs, p.n_req, unit)];
-  const int n_rows = rq.n_new * p.group;
-  const int n_tiles = (n_rows + Shape::kRows - 1) / Shape::kRows;
-  const int nb = (rq.seq_len + 15) >> 4;
-  const int n_seg = kSplit ? decode_segments(nb, p.seg_blocks) : 1;
-  const int at = unit - rq.unit_start;
-  const int seg = kSplit ? at % n_seg : 0;
-  const int tile = n_tiles - 1 - (kSplit ? at / n_seg : at);  // (the last rows see most keys: first)
-
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = WM == 1 ? 0 : wave % WM, wk = WK == 1 ? 0 : wave / WM;
-  const int half = lane >> 5;
-  const int first_key = rq.seq_len - rq.n_new;  // what token 0 sees last
-  const int row0 = tile * Shape::kRows + wm * kWaveRows;
-  const int row = row0 + (lane & 31);
-  const bool real = row < n_rows;
-  const int token = min(row, n_rows - 1) / p.group;
-  const int q_head = head * p.group + min(row, n_rows - 1) - token * p.group;
-  const int last_key = first_key + token;  // what this lane's row sees
-  // of the workgroup, of the wavefront
-  const int tile_last = first_key + (min((tile + 1) * Shape::kRows, n_rows) - 1) / p.group;
-  const int wave_first = first_key + min(row0, n_rows - 1) / p.group;
-  const int wave_last = first_key + min(row0 + kWaveRows - 1, n_rows - 1) / p.group;
-  int key_begin = 0, key_end = tile_last + 1;
-  if (kSplit) {
-    key_begin = 16 * decode_segment_begin(nb, n_seg, seg);
-    key_end = min(key_end, 16 * decode_segment_begin(nb, n_seg, seg + 1));
-  }
-  const int lane_last = min(last_key, key_end - 1);  // (a segment may end inside a tile)
-  const int n_key_tiles = key_end > key_begin ? (key_end - key_begin + kKeys - 1) / kKeys : 0;
-
-  // ---- queries: the B operand (lane: row, eight channels of a slab by half) --------------
-  half8 q[KK];
-  {
-    const _Float16* from = p.q.data + (int64_t)(rq.row_off + token) * p.q.token_stride +
-                           (int64_t)q_head * p.q.head_stride + half * 8;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) q[kk] = load_half8(from + kk * 16);
-  }
-
-  // ---- bringing in keys: a thread has one 16-byte piece of every kRowsPerPiece-th row ----
-  const int in_row = threadIdx.x / Shape::kLanesPerRow;
-  const int in_piece = threadIdx.x % Shape::kLanesPerRow;
-  const int32_t* table = p.block_tables + (SRC == ATTN_ROWS ? 0 : (size_t)rq.table_row * p.max_blocks);
-  const size_t v_off = (size_t)p.n_heads * 16 * D;
-  uint4v kr[kPieces], vr[kPieces];
-  uint32_t ke[SRC == ATTN_E4M3 ? kPieces : 1], ve[SRC == ATTN_E4M3 ? kPieces : 1];
-  auto request = [&](int base) {
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int r = base + i * Shape::kRowsPerPiece + in_row;
-      if constexpr (SRC == ATTN_ROWS) {
-        const int64_t t = rq.row_off + min(r, rq.seq_len - 1);
-        kr[i] = *reinterpret_cast<const uint4v*>(p.k.data + t * p.k.token_stride + head * p.k.head_stride + in_piece * 8);
-        vr[i] = *reinterpret_cast<const uint4v*>(p.v.data + t * p.v.token_stride + head * p.v.head_stride + in_piece * 8);
-      } else {
-        // (behind the last block: its rows again, which no row of this call sees there)
-        const int blk = clamp_block(table[min(r >> 4, nb - 1)], p.n_blocks);
-        const size_t at_row = (size_t)head * 16 + (r & 15);
-        if constexpr (SRC == ATTN_F16) {
-          const _Float16* from = static_cast<const _Float16*>(p.kv) + (size_t)blk * 2 * v_off + at_row * D + in_piece * 8;
-          kr[i] = *reinterpret_cast<const uint4v*>(from);
-          vr[i] = *reinterpret_cast<const uint4v*>(from + v_off);
-        } else {
-          const uint8_t* block = static_cast<const uint8_t*>(p.kv) + (size_t)blk * e4m3_block_bytes(p.n_heads, D);
-          const uint8_t* from = block + at_row * D + in_piece * 16;
-          kr[i] = *reinterpret_cast<const uint4v*>(from);
-          vr[i] = *reinterpret_cast<const uint4v*>(from + v_off);
-          ke[i] = block[2 * v_off + at_row];
-          ve[i] = block[2 * v_off + (size_t)p.n_heads * 16 + at_row];
-        }
-      }
-    }
-  };
-  auto put = [&] {
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int r = i * Shape::kRowsPerPiece + in_row;
-      if constexpr (SRC == ATTN_E4M3) {
-        const float ks = e4m3_scale(ke[i]), vs = e4m3_scale(ve[i]);
-        sm_k[k_chunk<D>(r, 2 * in_piece)] = e4m3_values(kr[i][0], kr[i][1], ks);
-        sm_k[k_chunk<D>(r, 2 * in_piece + 1)] = e4m3_values(kr[i][2], kr[i][3], ks);
-        sm_v[v_chunk<D>(r, 2 * in_piece)] = e4m3_values(vr[i][0], vr[i][1], vs);
-        sm_v[v_chunk<D>(r, 2 * in_piece + 1)] = e4m3_values(vr[i][2], vr[i][3], vs);
-      } else {
-        sm_k[k_chunk<D>(r, in_piece)] = __builtin_bit_cast(half8, kr[i]);
-        sm_v[v_chunk<D>(r, in_piece)] = __builtin_bit_cast(half8, vr[i]);
-      }
-    }
-  };
-
+// The 32 rows of a wavefront: operands, result and soft-max state of each lane's row.
+template <int D>
+struct Rows32 {
+  static constexpr int DT = D / 32;  // 32-channel tiles of the result
+  static constexpr int KK = D / 16;  // slabs of the first product
+  half8 q[KK];                       // B operand (eight channels of a slab by half)
   floatx16 o[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-  float m = -INFINITY, z = 0.f;  // z: this lane's keys
+  float m, z;  // running maximum (log2 units), and sum of this lane's keys
 
-  // ---- one tile: this wavefront's keys start at key0 -------------------------------------
-  auto attend = [&](int key0, auto masked_) {
-    constexpr bool kMasked = decltype(masked_)::value;
-    const int sub0 = wk * kSub * 32;
+  __device__ __forceinline__ void start(const _Float16* from) {  // the lane's row
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) q[kk] = load_half8(from + kk * 16 + half * 8);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+    m = -INFINITY;
+    z = 0.f;
+  }
+
+  // kSub * 32 keys that lie in LDS from row `at` of sm_k and sm_v; key0: the first one's
+  // number.  kMasked: the lane's row sees keys up to last_key only.
+  template <int kSub, bool kMasked>
+  __device__ __forceinline__ void attend(const half8* sm_k, const half8* sm_v, int at, int key0, int last_key,
+                                         float scale_log2e) {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
     floatx16 s[kSub];
 #pragma unroll
-    for (int u = 0; u < kSub; ++u) {
+    for (int u = 0; u < kSub; ++u)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk)
-        s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(sm_k[k_chunk<D>(sub0 + u * 32 + (lane & 31), 2 * kk + half)], q[kk],
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int u = 0; u < kSub; ++u)
+        s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(sm_k[k_chunk<D>(at + u * 32 + (lane & 31), 2 * kk + half)], q[kk],
                                                       s[u], 0, 0, 0);
-    }
     float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kSub; ++u)
@@ -235,12 +162,14 @@ __global__ __launch_bounds__(64 * WM * WK) void attention_kernel(AttnParams p, R
       for (int r = 0; r < 16; ++r) {
         if constexpr (kMasked) {
           const int key = key0 + u * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-          if (key > lane_last) s[u][r] = -INFINITY;
+          if (key > last_key) s[u][r] = -INFINITY;
         }
         top = fmaxf(top, s[u][r]);
       }
-    const float mn = fmaxf(m, other_half_max(top) * p.scale_log2e);
-    if (__any(mn > m)) {
+    // m follows the maximum when it falls more than kSlack behind: the numerators stay below
+    // 2^kSlack, which fp16 and the sums hold as exactly as those below 1.
+    const float mn = fmaxf(m, other_half_max(top) * scale_log2e);
+    if (__any(mn > m + kSlack)) {
       // (nothing seen so far: nothing to rescale, but what was not a number, or infinite, stays)
       const float a = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       z *= a;
@@ -257,19 +186,19 @@ __global__ __launch_bounds__(64 * WM * WK) void attention_kernel(AttnParams p, R
     if constexpr (kMasked) {
       uint32_t found = 0;
 #pragma unroll
-      for (int i = 0; i < kSub * 32 * D / 8 / 64; ++i) found |= nonfinite(sm_v[sub0 * (D / 8) + i * 64 + lane]);
+      for (int i = 0; i < kSub * 32 * D / 8 / 64; ++i) found |= nonfinite(sm_v[at * (D / 8) + i * 64 + lane]);
       dirty = __any(found != 0);
       if (dirty) {
 #pragma unroll 1
         for (int key = 0; key < kSub * 32; ++key) {
-          const bool seen = key0 + key <= lane_last;
+          const bool seen = key0 + key <= last_key;
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const int c = dt * 32 + j * 8 + half * 4;
               const half4 x = *reinterpret_cast<const half4*>(
-                  reinterpret_cast<const _Float16*>(sm_v + v_chunk<D>(sub0 + key, c / 8)) + half * 4);
+                  reinterpret_cast<const _Float16*>(sm_v + v_chunk<D>(at + key, c / 8)) + half * 4);
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 if (seen && abs_bits(x[e]) >= 0x7c00u) o[dt][4 * j + e] += (float)x[e];
@@ -282,21 +211,20 @@ __global__ __launch_bounds__(64 * WM * WK) void attention_kernel(AttnParams p, R
       half8 pb[2];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(s[u][r], p.scale_log2e, -base));
+        const float w = __builtin_amdgcn_exp2f(fmaf(s[u][r], scale_log2e, -base));
         z += w;
         pb[r >> 3][r & 7] = (_Float16)w;
       }
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
         // keys 16 kk + 4 half + 0..3 and 8 more: rows (lane % 16) / 4 of the transposing reads
-        const int r = sub0 + u * 32 + kk * 16 + half * 4 + ((lane & 15) >> 2);
+        const int r = at + u * 32 + kk * 16 + half * 4 + ((lane & 15) >> 2);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
           const int c = dt * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
           const _Float16* a0 = reinterpret_cast<const _Float16*>(sm_v + v_chunk<D>(r, c)) + (lane & 1) * 4;
           const _Float16* a1 = reinterpret_cast<const _Float16*>(sm_v + v_chunk<D>(r + 8, c)) + (lane & 1) * 4;
-          const fp16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4f16((LdsQuad)a0);
-          const fp16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4f16((LdsQuad)a1);
+          const fp16x4 lo = read_columns(a0), hi = read_columns(a1);
           half8 v = {(_Float16)lo[0], (_Float16)lo[1], (_Float16)lo[2], (_Float16)lo[3],
                      (_Float16)hi[0], (_Float16)hi[1], (_Float16)hi[2], (_Float16)hi[3]};
           if constexpr (kMasked) {
@@ -306,122 +234,387 @@ __global__ __launch_bounds__(64 * WM * WK) void attention_kernel(AttnParams p, R
         }
       }
     }
-  };
-
-  if (n_key_tiles > 0) request(key_begin);
-  for (int t = 0; t < n_key_tiles; ++t) {
-    const int base = key_begin + t * kKeys;
-    __syncthreads();  // the tile before has been read
-    put();
-    __syncthreads();
-    if (t + 1 < n_key_tiles) request(base + kKeys);
-    const int key0 = base + wk * kSub * 32;
-    if (key0 > min(wave_last, key_end - 1)) continue;  // uniform over the wavefront: none of its rows sees these
-    // a segment that ends inside the tile hides the keys behind it, as does the causal mask
-    if (key0 + kSub * 32 - 1 <= min(wave_first, key_end - 1))
-      attend(key0, std::false_type());
-    else
-      attend(key0, std::true_type());
   }
-  z = other_half_sum(z);
+};
 
-  // ---- joining the wavefronts that shared the rows ----------------------------------------
-  // (from here on: o normalised, m the log2 of the sum of the row's numerators, -inf: no key)
-  _Float16* out = p.out.data + (int64_t)(rq.row_off + token) * p.out.token_stride + (int64_t)q_head * p.out.head_stride;
-  constexpr int kWords = DecodeParams::state_words(D);
-  float* state = nullptr;
-  if (kSplit && n_seg > 1)
-    state = p.states + (((int64_t)(rq.state_off + token) * p.n_heads * p.group + q_head) * p.n_seg + seg) * kWords;
-  auto write_lse = [&](float log2_sum) {
-    if (!p.lse) return;
-    const int i = p.window - rq.n_new + token;
-    if (i >= 0) p.lse[(int64_t)rq.table_row * p.lse_stride + (int64_t)q_head * p.window + i] = log2_sum * kLn2;
-  };
-  if constexpr (WK == 1) {
-    const float inv = z == 0.f ? 0.f : 1.f / z;
-    const float log2_sum = z == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(z);
-    if (!real) return;
-    if (kSplit && n_seg > 1) {
+// Where a workgroup is in its request (tile: row tile of kRows) and which keys it walks.
+struct Place {
+  ChunkReq rq;
+  int n_rows, tile, nb, n_seg, seg, key_begin, key_end;
+};
+template <int kRows, bool kSplit, typename Reqs>
+__device__ __forceinline__ Place place_of(const AttnParams& p, const Reqs& reqs, int unit) {
+  Place w;
+  w.rq = reqs.req[request_of(reqs, p.n_req, unit)];
+  w.n_rows = w.rq.n_new * p.group;
+  w.nb = (w.rq.seq_len + 15) >> 4;
+  w.n_seg = kSplit ? decode_segments(w.nb, p.seg_blocks) : 1;
+  const int at = unit - w.rq.unit_start;
+  w.seg = kSplit ? at % w.n_seg : 0;
+  // (the last rows see most keys: first)
+  w.tile = (w.n_rows + kRows - 1) / kRows - 1 - (kSplit ? at / w.n_seg : at);
+  w.key_begin = 0;
+  w.key_end = w.rq.seq_len - w.rq.n_new + (min((w.tile + 1) * kRows, w.n_rows) - 1) / p.group + 1;
+  if (kSplit) {
+    w.key_begin = 16 * decode_segment_begin(w.nb, w.n_seg, w.seg);
+    w.key_end = min(w.key_end, 16 * decode_segment_begin(w.nb, w.n_seg, w.seg + 1));
+  }
+  return w;
+}
+
+// A lane's row: its token and query head (rows behind the last one: the last one's).
+struct LaneRow {
+  int token, q_head;
+  bool real;
+};
+__device__ __forceinline__ LaneRow lane_row(const AttnParams& p, int row, int n_rows, int head) {
+  LaneRow r;
+  r.real = row < n_rows;
+  row = min(row, n_rows - 1);
+  r.token = row / p.group;
+  r.q_head = head * p.group + row - r.token * p.group;
+  return r;
+}
+__device__ __forceinline__ _Float16* row_of(const RowsView& v, const ChunkReq& rq, int token, int head) {
+  return v.data + (int64_t)(rq.row_off + token) * v.token_stride + (int64_t)head * v.head_stride;
+}
+template <int D>
+__device__ __forceinline__ float* state_of(const AttnParams& p, const ChunkReq& rq, int token, int q_head, int seg) {
+  return p.states + (((int64_t)(rq.state_off + token) * p.n_heads * p.group + q_head) * p.n_seg + seg) *
+                        DecodeParams::state_words(D);
+}
+__device__ __forceinline__ void write_lse(const AttnParams& p, const ChunkReq& rq, int token, int q_head, float log2_sum) {
+  const int i = p.window - rq.n_new + token;
+  if (p.lse && i >= 0) p.lse[(int64_t)rq.table_row * p.lse_stride + (int64_t)q_head * p.window + i] = log2_sum * kLn2;
+}
+
+// Sixteen keys (a pool block) on their way to LDS by one wavefront, K and V in one call each.
+// The rows lie in LDS from slot 0 of `to`, which is a multiple of 16 rows into a tile; the
+// permutation of the chunks is in the addresses that the lanes read from.
+template <int D>
+struct BlockLoader {
+  static constexpr int kInstr = 16 * D / 8 / 64;  // wavefront loads of K, and of V
+  int k_at[kInstr], v_at[kInstr];                 // byte offset of the lane's chunk, by load
+  __device__ __forceinline__ BlockLoader(int k_row_bytes, int v_row_bytes) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          floatx4 x;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = o[dt][4 * j + e] * inv;
-          *reinterpret_cast<floatx4*>(state + dt * 32 + j * 8 + half * 4) = x;
-        }
-      if (half == 0) state[D] = log2_sum;
-      return;
+    for (int i = 0; i < kInstr; ++i) {
+      const int r = (i * 64 + lane) / (D / 8), c = lane % (D / 8);
+      k_at[i] = r * k_row_bytes + (k_chunk<D>(r, c) - r * (D / 8)) * 16;
+      v_at[i] = r * v_row_bytes + (v_chunk<D>(r, c) - r * (D / 8)) * 16;
     }
+  }
+  __device__ __forceinline__ void k(BufferPtr from, half8* to) const {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+    for (int i = 0; i < kInstr; ++i) load_to_lds(from, k_at[i], 0, to + i * 64);
+  }
+  __device__ __forceinline__ void v(BufferPtr from, half8* to) const {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        half4 x;
+    for (int i = 0; i < kInstr; ++i) load_to_lds(from, v_at[i], 0, to + i * 64);
+  }
+};
+
+// Sixteen keys of an 8-bit pool through registers: codes, exponents; fp16 numbers into LDS.
+template <int D>
+struct Block8 {
+  static constexpr int kLanes = D / 16, kInstr = 16 * kLanes / 64;  // lanes of a row; loads of K, and of V
+  uint4v kc[kInstr], vc[kInstr];
+  uint32_t ke[kInstr], ve[kInstr];
+  __device__ __forceinline__ void request(const uint8_t* block, int n_heads, int head) {
+    const int lane = threadIdx.x & 63;
+    const size_t v_off = (size_t)n_heads * 16 * D;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = (_Float16)(o[dt][4 * j + e] * inv);
-        *reinterpret_cast<half4*>(out + dt * 32 + j * 8 + half * 4) = x;
+    for (int i = 0; i < kInstr; ++i) {
+      const size_t row = (size_t)head * 16 + (i * 64 + lane) / kLanes;
+      const uint8_t* from = block + row * D + (lane % kLanes) * 16;
+      kc[i] = *reinterpret_cast<const uint4v*>(from);
+      vc[i] = *reinterpret_cast<const uint4v*>(from + v_off);
+      ke[i] = block[2 * v_off + row];
+      ve[i] = block[2 * v_off + (size_t)n_heads * 16 + row];
+    }
+  }
+  __device__ __forceinline__ void put(half8* sm_k, half8* sm_v, int at) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < kInstr; ++i) {
+      const int r = at + (i * 64 + lane) / kLanes, c = (lane % kLanes) * 2;
+      const float ks = e4m3_scale(ke[i]), vs = e4m3_scale(ve[i]);
+      sm_k[k_chunk<D>(r, c)] = e4m3_values(kc[i][0], kc[i][1], ks);
+      sm_k[k_chunk<D>(r, c + 1)] = e4m3_values(kc[i][2], kc[i][3], ks);
+      sm_v[v_chunk<D>(r, c)] = e4m3_values(vc[i][0], vc[i][1], vs);
+      sm_v[v_chunk<D>(r, c + 1)] = e4m3_values(vc[i][2], vc[i][3], vs);
+    }
+  }
+};
+
+// Block b of the request's cache (behind the last one: the last one, whose rows nobody sees there).
+__device__ __forceinline__ int block_id(const AttnParams& p, const int32_t* table, int b, int nb) {
+  return clamp_block(load_uniform(table + min(b, nb - 1)), p.n_blocks);
+}
+template <int D>
+__device__ __forceinline__ BufferPtr f16_block(const AttnParams& p, int blk, int head, int which) {
+  const size_t half_block = (size_t)p.n_heads * 16 * D;
+  return buffer_of(static_cast<const _Float16*>(p.kv) + (size_t)blk * 2 * half_block + which * half_block + (size_t)head * 16 * D,
+                   16 * D * 2);
+}
+// Packed rows from address `from` on, rows_left of them the request's (what is read behind
+// them is zeros).
+template <int D>
+__device__ __forceinline__ BufferPtr rows_at(const _Float16* from, int stride, int rows_left) {
+  return buffer_of(from, rows_left > 0 ? (min(rows_left, 16) - 1) * stride * 2 + D * 2 : 0);
+}
+
+// ---------------------------------------------------------------------------
+// Many rows: four wavefronts of 32 rows over the same keys, 64 at a time.  Two tiles in LDS:
+// while one is worked on, each wavefront brings in 16 keys of the next.
+// ---------------------------------------------------------------------------
+template <int D, int SRC, bool kSplit, typename Reqs>
+__global__ __launch_bounds__(256, 2) void attention_tall_kernel(AttnParams p, Reqs reqs) {
+  constexpr int kKeys = 64, kTile = kKeys * D / 8;  // half8s of K, and of V
+  extern __shared__ __align__(16) half8 sm[];       // [2][K, V][kTile]
+  const int unit = blockIdx.x / p.n_heads;
+  const int head = blockIdx.x - unit * p.n_heads;
+  const Place w = place_of<kTallRows, kSplit>(p, reqs, unit);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int first_key = w.rq.seq_len - w.rq.n_new;  // what token 0 sees last
+  const int row0 = w.tile * kTallRows + wave * 32;
+  const LaneRow me = lane_row(p, row0 + (lane & 31), w.n_rows, head);
+  const int last_key = min(first_key + me.token, w.key_end - 1);  // (a segment may end inside a tile)
+  const int wave_last = min(first_key + min(row0 + 31, w.n_rows - 1) / p.group, w.key_end - 1);
+  const int n_tiles = w.key_end > w.key_begin ? (w.key_end - w.key_begin + kKeys - 1) / kKeys : 0;
+  // tiles that every row of the workgroup sees whole
+  const int n_full = max(min(first_key + w.tile * kTallRows / p.group, w.key_end - 1) + 1 - w.key_begin, 0) / kKeys;
+
+  Rows32<D> rows;
+  rows.start(row_of(p.q, w.rq, me.token, me.q_head));
+
+  const int32_t* table = SRC == ATTN_ROWS ? nullptr : p.block_tables + (size_t)w.rq.table_row * p.max_blocks;
+  const int k_stride = SRC == ATTN_ROWS ? (int)p.k.token_stride : D, v_stride = SRC == ATTN_ROWS ? (int)p.v.token_stride : D;
+  const BlockLoader<D> loader(2 * k_stride, 2 * v_stride);
+  half8* to_mine = sm + wave * 16 * D / 8;
+  // the next 16 keys that this wavefront brings in
+  int block = (w.key_begin >> 4) + wave, next_id = 0;
+  int rows_left = w.rq.seq_len - 16 * block;
+  const _Float16 *k_from = nullptr, *v_from = nullptr;
+  if constexpr (SRC == ATTN_ROWS) {
+    k_from = row_of(p.k, w.rq, 16 * block, head);
+    v_from = row_of(p.v, w.rq, 16 * block, head);
+  } else if (n_tiles > 0) {
+    next_id = block_id(p, table, block, w.nb);
+  }
+  Block8<D> b8;
+  auto request = [&](int t) {
+    half8* to = to_mine + (t & 1) * 2 * kTile;
+    if constexpr (SRC == ATTN_ROWS) {
+      loader.k(rows_at<D>(k_from, k_stride, rows_left), to);
+      loader.v(rows_at<D>(v_from, v_stride, rows_left), to + kTile);
+      k_from += (int64_t)kKeys * k_stride;
+      v_from += (int64_t)kKeys * v_stride;
+      rows_left -= kKeys;
+    } else {
+      if constexpr (SRC == ATTN_F16) {
+        loader.k(f16_block<D>(p, next_id, head, 0), to);
+        loader.v(f16_block<D>(p, next_id, head, 1), to + kTile);
+      } else {
+        b8.request(static_cast<const uint8_t*>(p.kv) + (size_t)next_id * e4m3_block_bytes(p.n_heads, D), p.n_heads, head);
       }
-    if (half == 0) write_lse(log2_sum);
-  } else {
-    static_assert(WM == 1, "wavefronts with rows of their own or with shared rows");
-    float* sm_f = reinterpret_cast<float*>(sm);
-    __syncthreads();
-    if (half == 0) {
-      sm_f[(wk * 32 + lane) * 2] = m;
-      sm_f[(wk * 32 + lane) * 2 + 1] = z;
+      block += kKeys / 16;
+      next_id = block_id(p, table, block, w.nb);
     }
-    __syncthreads();
-    float mm = -INFINITY, zz = 0.f;
-#pragma unroll
-    for (int w = 0; w < WK; ++w) mm = fmaxf(mm, sm_f[(w * 32 + (lane & 31)) * 2]);
-#pragma unroll
-    for (int w = 0; w < WK; ++w) {
-      const float zw = sm_f[(w * 32 + (lane & 31)) * 2 + 1];
-      zz += zw == 0.f ? 0.f : zw * __builtin_amdgcn_exp2f(sm_f[(w * 32 + (lane & 31)) * 2] - mm);
+  };
+  auto put8 = [&](int t) {
+    half8* to = sm + (t & 1) * 2 * kTile;
+    b8.put(to, to + kTile, wave * 16);
+  };
+  auto step = [&](int t, auto masked_) {
+    constexpr bool kMasked = decltype(masked_)::value;
+    if constexpr (SRC != ATTN_E4M3) wait_loads<0>();
+    lds_barrier();  // tile t is there, the one before has been read
+    if (t + 1 < n_tiles) request(t + 1);
+    const half8* sm_k = sm + (t & 1) * 2 * kTile;
+    const int key0 = w.key_begin + t * kKeys;
+    if (!kMasked || key0 <= wave_last)  // uniform over the wavefront: else none of its rows sees these
+      rows.template attend<2, kMasked>(sm_k, sm_k + kTile, 0, key0, last_key, p.scale_log2e);
+    if constexpr (SRC == ATTN_E4M3) {
+      if (t + 1 < n_tiles) put8(t + 1);
     }
-    const float log2_sum = zz == 0.f ? -INFINITY : mm + __builtin_amdgcn_logf(zz);
-    const float f = z == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - mm) / zz;
-    __syncthreads();
-    // [wavefront][row][channel], quads permuted within the row against bank conflicts
-    constexpr int kQuads = D / 4;
-    floatx4* sm_o = reinterpret_cast<floatx4*>(sm);
+  };
+  if (n_tiles > 0) {
+    request(0);
+    if constexpr (SRC == ATTN_E4M3) put8(0);
+  }
+  int t = 0;
+  for (; t < n_full; ++t) step(t, std::false_type());
+  for (; t < n_tiles; ++t) step(t, std::true_type());
+
+  const float z = other_half_sum(rows.z);
+  const float inv = z == 0.f ? 0.f : 1.f / z;
+  const float log2_sum = z == 0.f ? -INFINITY : rows.m + __builtin_amdgcn_logf(z);
+  if (!me.real) return;
+  if (kSplit && w.n_seg > 1) {  // a segment's state: the normalised result and the log2 of the sum
+    float* state = state_of<D>(p, w.rq, me.token, me.q_head, w.seg);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+    for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         floatx4 x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = o[dt][4 * j + e] * f;
-        const int c = dt * 8 + j * 2 + half, r = lane & 31;
-        sm_o[(wk * 32 + r) * kQuads + (c ^ (r & (kQuads - 1)))] = x;
+        for (int e = 0; e < 4; ++e) x[e] = rows.o[dt][4 * j + e] * inv;
+        *reinterpret_cast<floatx4*>(state + dt * 32 + j * 8 + half * 4) = x;
       }
-    if (wave == 0 && half == 0 && real) {
-      if (kSplit && n_seg > 1)
-        state[D] = log2_sum;
-      else
-        write_lse(log2_sum);
+    if (half == 0) state[D] = log2_sum;
+    return;
+  }
+  _Float16* out = row_of(p.out, w.rq, me.token, me.q_head);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      half4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (_Float16)(rows.o[dt][4 * j + e] * inv);
+      *reinterpret_cast<half4*>(out + dt * 32 + j * 8 + half * 4) = x;
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 32 * kQuads; i += Shape::kThreads) {
-      const int r = i / kQuads, c = i % kQuads;
-      if (tile * Shape::kRows + r >= n_rows) break;
-      floatx4 x = sm_o[r * kQuads + (c ^ (r & (kQuads - 1)))];
+  if (half == 0) write_lse(p, w.rq, me.token, me.q_head, log2_sum);
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: four wavefronts over the same 32 rows; each takes every fourth 32 keys, which it
+// brings in by itself (no barrier in the loop), and the four states are joined at the end.
+// ---------------------------------------------------------------------------
+template <int D, int SRC, bool kSplit, typename Reqs>
+__global__ __launch_bounds__(256) void attention_flat_kernel(AttnParams p, Reqs reqs) {
+  constexpr int kKeys = 32, kTile = kKeys * D / 8;
+  constexpr int kBuffers = SRC == ATTN_E4M3 ? 1 : 2;
+  extern __shared__ __align__(16) half8 sm[];  // [wavefront][buffer][K, V][kTile]
+  const int unit = blockIdx.x / p.n_heads;
+  const int head = blockIdx.x - unit * p.n_heads;
+  const Place w = place_of<kFlatRows, kSplit>(p, reqs, unit);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int first_key = w.rq.seq_len - w.rq.n_new;
+  const int row0 = w.tile * kFlatRows;
+  const LaneRow me = lane_row(p, row0 + (lane & 31), w.n_rows, head);
+  const int last_key = min(first_key + me.token, w.key_end - 1);
+  const int first_seen = min(first_key + row0 / p.group, w.key_end - 1);  // all rows see keys up to this one
+  const int n_tiles = w.key_end > w.key_begin ? (w.key_end - w.key_begin + kKeys - 1) / kKeys : 0;
+  const int mine = own_tiles(n_tiles, wave, 4);
+
+  const int32_t* table = SRC == ATTN_ROWS ? nullptr : p.block_tables + (size_t)w.rq.table_row * p.max_blocks;
+  const BlockLoader<D> loader(SRC == ATTN_ROWS ? (int)p.k.token_stride * 2 : D * 2,
+                              SRC == ATTN_ROWS ? (int)p.v.token_stride * 2 : D * 2);
+  half8* sm_mine = sm + wave * kBuffers * 2 * kTile;
+  Block8<D> b8[2];
+  int ids[2] = {0, 0};
+  auto block_of = [&](int i, int j) { return (w.key_begin >> 4) + 2 * (wave + 4 * i) + j; };
+  auto look_up = [&](int i) {
+    if constexpr (SRC != ATTN_ROWS) {
+      ids[0] = block_id(p, table, block_of(i, 0), w.nb);
+      ids[1] = block_id(p, table, block_of(i, 1), w.nb);
+    }
+  };
+  auto request = [&](int i) {
 #pragma unroll
-      for (int w = 1; w < WK; ++w) x += sm_o[(w * 32 + r) * kQuads + (c ^ (r & (kQuads - 1)))];
-      const int tok = (tile * Shape::kRows + r) / p.group;
-      const int h = head * p.group + (tile * Shape::kRows + r) - tok * p.group;
-      if (kSplit && n_seg > 1) {
-        float* to = p.states + (((int64_t)(rq.state_off + tok) * p.n_heads * p.group + h) * p.n_seg + seg) * kWords;
-        *reinterpret_cast<floatx4*>(to + c * 4) = x;
+    for (int j = 0; j < 2; ++j) {
+      half8* to = sm_mine + (i % kBuffers) * 2 * kTile + j * 16 * D / 8;
+      if constexpr (SRC == ATTN_ROWS) {
+        const int first = 16 * block_of(i, j);
+        loader.k(rows_at<D>(row_of(p.k, w.rq, first, head), (int)p.k.token_stride, w.rq.seq_len - first), to);
+        loader.v(rows_at<D>(row_of(p.v, w.rq, first, head), (int)p.v.token_stride, w.rq.seq_len - first), to + kTile);
+      } else if constexpr (SRC == ATTN_F16) {
+        loader.k(f16_block<D>(p, ids[j], head, 0), to);
+        loader.v(f16_block<D>(p, ids[j], head, 1), to + kTile);
       } else {
-        half4 y;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = (_Float16)x[e];
-        *reinterpret_cast<half4*>(p.out.data + (int64_t)(rq.row_off + tok) * p.out.token_stride +
-                                  (int64_t)h * p.out.head_stride + c * 4) = y;
+        b8[j].request(static_cast<const uint8_t*>(p.kv) + (size_t)ids[j] * e4m3_block_bytes(p.n_heads, D), p.n_heads, head);
       }
+    }
+    look_up(i + 1);
+  };
+
+  Rows32<D> rows;
+  rows.start(row_of(p.q, w.rq, me.token, me.q_head));
+  if (mine > 0) {
+    look_up(0);
+    request(0);
+  }
+  auto step = [&](int i, auto masked_) {
+    const half8* sm_k = sm_mine + (i % kBuffers) * 2 * kTile;
+    if constexpr (SRC == ATTN_E4M3) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) b8[j].put(sm_mine, sm_mine + kTile, 16 * j);
+      wave_lds_barrier();
+      if (i + 1 < mine) request(i + 1);
+    } else {
+      if (i + 1 < mine) {
+        request(i + 1);
+        wait_loads<4 * BlockLoader<D>::kInstr>();
+      } else {
+        wait_loads<0>();
+      }
+    }
+    rows.template attend<1, decltype(masked_)::value>(sm_k, sm_k + kTile, 0, w.key_begin + (wave + 4 * i) * kKeys, last_key,
+                                                      p.scale_log2e);
+    wave_lds_barrier();
+  };
+  // tiles that every row sees whole come first
+  const int full = min(mine, own_tiles(max(first_seen + 1 - w.key_begin, 0) / kKeys, wave, 4));
+  int i = 0;
+  for (; i < full; ++i) step(i, std::false_type());
+  for (; i < mine; ++i) step(i, std::true_type());
+  const float z = other_half_sum(rows.z), m = rows.m;
+
+  // ---- joining the four states -----------------------------------------------------------
+  __shared__ float sm_m[4][32], sm_z[4][32];
+  if (half == 0) {
+    sm_m[wave][lane] = m;
+    sm_z[wave][lane] = z;
+  }
+  __syncthreads();  // (and every wavefront is done with its keys)
+  float mm = -INFINITY, zz = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) mm = fmaxf(mm, sm_m[i][lane & 31]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float zi = sm_z[i][lane & 31];
+    zz += zi == 0.f ? 0.f : zi * __builtin_amdgcn_exp2f(sm_m[i][lane & 31] - mm);
+  }
+  const float log2_sum = zz == 0.f ? -INFINITY : mm + __builtin_amdgcn_logf(zz);
+  const float f = z == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - mm) / zz;
+  // [wavefront][row][channel], quads permuted within the row against bank conflicts
+  constexpr int kQuads = D / 4;
+  floatx4* sm_o = reinterpret_cast<floatx4*>(sm);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      floatx4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = rows.o[dt][4 * j + e] * f;
+      const int c = dt * 8 + j * 2 + half, r = lane & 31;
+      sm_o[(wave * 32 + r) * kQuads + (c ^ (r & (kQuads - 1)))] = x;
+    }
+  if (wave == 0 && half == 0 && me.real) {
+    if (kSplit && w.n_seg > 1)
+      state_of<D>(p, w.rq, me.token, me.q_head, w.seg)[D] = log2_sum;
+    else
+      write_lse(p, w.rq, me.token, me.q_head, log2_sum);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * kQuads; i += 256) {
+    const int r = i / kQuads, c = i % kQuads;
+    const LaneRow it = lane_row(p, row0 + r, w.n_rows, head);
+    if (!it.real) break;
+    floatx4 x = sm_o[r * kQuads + (c ^ (r & (kQuads - 1)))];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) x += sm_o[(k * 32 + r) * kQuads + (c ^ (r & (kQuads - 1)))];
+    if (kSplit && w.n_seg > 1) {
+      *reinterpret_cast<floatx4*>(state_of<D>(p, w.rq, it.token, it.q_head, w.seg) + c * 4) = x;
+    } else {
+      half4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = (_Float16)x[e];
+      *reinterpret_cast<half4*>(row_of(p.out, w.rq, it.token, it.q_head) + c * 4) = y;
     }
   }
 }
@@ -464,31 +657,59 @@ __global__ __launch_bounds__(D) void attention_merge_kernel(AttnParams p, Reqs r
         zz == 0.f ? -INFINITY : (mm + __builtin_amdgcn_logf(zz)) * kLn2;
 }
 
-template <int D, int WM, int WK, int SRC, typename Reqs>
-void launch_one(const AttnParams& p, const Reqs& reqs, hipStream_t s) {
-  using Shape = AttnShape<D, WM, WK, SRC>;
+constexpr int tall_lds(int head_dim) { return 2 * 2 * 64 * head_dim * 2; }
+// (the joined states need as much as one buffer)
+constexpr int flat_lds(int head_dim, int source) { return 4 * (source == ATTN_E4M3 ? 1 : 2) * 2 * 32 * head_dim * 2; }
+
+template <int D, int SRC, bool kSplit, typename Reqs>
+void launch_kernel(const AttnParams& p, bool flat, const Reqs& reqs, hipStream_t s) {
   const unsigned grid = (unsigned)p.n_units * p.n_heads;
+  if (flat)
+    attention_flat_kernel<D, SRC, kSplit, Reqs><<<grid, 256, flat_lds(D, SRC), s>>>(p, reqs);
+  else
+    attention_tall_kernel<D, SRC, kSplit, Reqs><<<grid, 256, tall_lds(D), s>>>(p, reqs);
+}
+
+template <int D, int SRC, typename Reqs>
+void launch_source(const AttnParams& p, bool flat, const Reqs& reqs, hipStream_t s) {
   if constexpr (SRC != ATTN_ROWS) {
     if (p.n_seg > 1) {
-      attention_kernel<D, WM, WK, SRC, true, Reqs><<<grid, Shape::kThreads, Shape::kLdsBytes, s>>>(p, reqs);
+      launch_kernel<D, SRC, true>(p, flat, reqs, s);
       attention_merge_kernel<D, Reqs><<<(unsigned)p.state_rows * p.n_heads * p.group, D, 0, s>>>(p, reqs);
       return;
     }
   }
-  attention_kernel<D, WM, WK, SRC, false, Reqs><<<grid, Shape::kThreads, Shape::kLdsBytes, s>>>(p, reqs);
+  launch_kernel<D, SRC, false>(p, flat, reqs, s);
 }
 
 template <int D, typename Reqs>
 void launch_shape(const AttnParams& p, bool flat, const Reqs& reqs, hipStream_t s) {
   if (p.source == ATTN_ROWS)
-    flat ? launch_one<D, 1, 4, ATTN_ROWS>(p, reqs, s) : launch_one<D, 4, 1, ATTN_ROWS>(p, reqs, s);
+    launch_source<D, ATTN_ROWS>(p, flat, reqs, s);
   else if (p.source == ATTN_F16)
-    flat ? launch_one<D, 1, 4, ATTN_F16>(p, reqs, s) : launch_one<D, 4, 1, ATTN_F16>(p, reqs, s);
+    launch_source<D, ATTN_F16>(p, flat, reqs, s);
   else
-    flat ? launch_one<D, 1, 4, ATTN_E4M3>(p, reqs, s) : launch_one<D, 4, 1, ATTN_E4M3>(p, reqs, s);
+    launch_source<D, ATTN_E4M3>(p, flat, reqs, s);
+}
+
+template <typename Reqs>
+hipError_t allow_lds_with() {  // more than 64 KB
+  hipError_t e = hipSuccess;
+  auto allow = [&](const void* kernel, int bytes) {
+    if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  };
+  allow(reinterpret_cast<const void*>(&attention_flat_kernel<128, ATTN_ROWS, false, Reqs>), flat_lds(128, ATTN_ROWS));
+  allow(reinterpret_cast<const void*>(&attention_flat_kernel<128, ATTN_F16, false, Reqs>), flat_lds(128, ATTN_F16));
+  allow(reinterpret_cast<const void*>(&attention_flat_kernel<128, ATTN_F16, true, Reqs>), flat_lds(128, ATTN_F16));
+  return e;
 }
 
 }  // namespace
+
+hipError_t attention_one_time_setup() {
+  const hipError_t e = allow_lds_with<ChunkReqs>();
+  return e == hipSuccess ? allow_lds_with<ChunkReqList>() : e;
+}
 
 hipError_t launch_attention(const AttnParams& p, bool flat, const ChunkReqs& inline_reqs, hipStream_t s) {
   if (p.n_units == 0) return hipSuccess;

@@ -47,8 +47,8 @@ int check_rows(const fc_rows* rows, const char* name, int64_t n_rows, int n_head
   if (reinterpret_cast<uintptr_t>(rows->data) & 15) return fail(FC_EINVAL, "%s must be 16-byte aligned", name);
   const int64_t t = rows->token_stride, h = rows->head_stride;
   if ((t | h) & 7 || t < 0 || h < 0) return fail(FC_EINVAL, "strides of %s must be multiples of 8, 0 or more", name);
-  // (no product of strides and numbers of rows and heads passes 63 bits)
-  if (t > (int64_t)1 << 30 || h > (int64_t)1 << 46) return fail(FC_EINVAL, "strides of %s are too large", name);
+  // (16 rows span less than 2^31 bytes, no product with rows or heads passes 63 bits)
+  if (t > (int64_t)1 << 24 || h > (int64_t)1 << 46) return fail(FC_EINVAL, "strides of %s are too large", name);
   if (written && !(h >= head_dim && t >= (n_heads - 1) * h + head_dim) && !(t >= head_dim && h >= (n_rows - 1) * t + head_dim))
     return fail(FC_EINVAL, "rows of %s overlap", name);
   return FC_OK;

@@ -274,6 +274,7 @@ hipError_t launch_extend(const ExtendParams& p, const ExtendReqs& inline_reqs, h
 hipError_t launch_store_chunk(const StoreParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
 hipError_t launch_quantise(const QuantiseParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
 // ... and their attention (fc_attention.hip); flat: few rows a request (ATTN_FLAT)
+hipError_t attention_one_time_setup();
 hipError_t launch_attention(const AttnParams& p, bool flat, const ChunkReqs& inline_reqs, hipStream_t s);
 // chunk-MLP compressor (fc_mlp.hip)
 hipError_t mlp_one_time_setup();

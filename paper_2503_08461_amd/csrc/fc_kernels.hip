@@ -371,6 +371,7 @@ hipError_t kernels_one_time_setup() {
                                      hipFuncAttributeMaxDynamicSharedMemorySize, (stage_words(32768) + need_words(32768)) * 4);
   if (e == hipSuccess) e = fused_wide_setup_64();
   if (e == hipSuccess) e = fused_wide_setup_128();
+  if (e == hipSuccess) e = attention_one_time_setup();
   return e;
 }
 
