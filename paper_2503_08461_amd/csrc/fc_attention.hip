@@ -20,6 +20,7 @@
 // Two kernels: many rows (prompts, long chunks; bound by the matrix cores) and few rows (single
 // tokens, short chunks; bound by memory).
 
+#include <algorithm>
 #include <type_traits>
 
 #include "fc_chunk_plan.h"
@@ -33,6 +34,8 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef __fp16 fp16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) fp16x4* LdsQuad;
+typedef int int2v __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) int2v* LdsPair;
 
 constexpr float kSlack = 8.f;
 constexpr float kLn2 = 0.69314718055994530942f;
@@ -60,8 +63,8 @@ __device__ __forceinline__ float other_half_sum(float v) {
 }
 
 template <typename Reqs>
-__device__ __forceinline__ int request_of(const Reqs& reqs, int n_req, int u) {
-  int lo = 0, hi = n_req - 1;
+__device__ __forceinline__ int request_of(const Reqs& reqs, int begin, int end, int u) {
+  int lo = begin, hi = end - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (reqs.req[mid].unit_start <= u)
@@ -117,6 +120,46 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// 32-key subtiles of fp16 rows in LDS, from row `at` of tiles k and v.
+template <int D>
+struct F16Keys {
+  static constexpr bool kPairedSlabs = false;
+  const half8 *k, *v;
+  int at;
+  // A operands: of a slab of K (lane: key, eight channels by half), ...
+  __device__ __forceinline__ half8 k_slab(int u, int kk) const {
+    const int lane = threadIdx.x & 63;
+    return k[k_chunk<D>(at + u * 32 + (lane & 31), 2 * kk + (lane >> 5))];
+  }
+  // ... and of V^T: keys 16 kk + 4 half + 0..3 and 8 more, rows (lane % 16) / 4 of the transposing reads
+  __device__ __forceinline__ half8 v_slab(int u, int kk, int dt) const {
+    const int lane = threadIdx.x & 63;
+    const int r = at + u * 32 + kk * 16 + (lane >> 5) * 4 + ((lane & 15) >> 2);
+    const int c = dt * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+    const fp16x4 lo = read_columns(reinterpret_cast<const _Float16*>(v + v_chunk<D>(r, c)) + (lane & 1) * 4);
+    const fp16x4 hi = read_columns(reinterpret_cast<const _Float16*>(v + v_chunk<D>(r + 8, c)) + (lane & 1) * 4);
+    return half8{(_Float16)lo[0], (_Float16)lo[1], (_Float16)lo[2], (_Float16)lo[3],
+                 (_Float16)hi[0], (_Float16)hi[1], (_Float16)hi[2], (_Float16)hi[3]};
+  }
+  // whether V holds anything but finite numbers
+  template <int kSub>
+  __device__ __forceinline__ bool dirty() const {
+    uint32_t found = 0;
+#pragma unroll
+    for (int i = 0; i < kSub * 32 * D / 8 / 64; ++i) found |= nonfinite(v[at * (D / 8) + i * 64 + (threadIdx.x & 63)]);
+    return __any(found != 0);
+  }
+  // four channels of one key, those that are no finite numbers (0 for the others)
+  __device__ __forceinline__ floatx4 not_finite(int key, int channel) const {
+    const half4 x = *reinterpret_cast<const half4*>(
+        reinterpret_cast<const _Float16*>(v + v_chunk<D>(at + key, channel / 8)) + channel % 8);
+    floatx4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = abs_bits(x[e]) >= 0x7c00u ? (float)x[e] : 0.f;
+    return y;
+  }
+};
+
 // The 32 rows of a wavefront: operands, result and soft-max state of each lane's row.
 template <int D>
 struct Rows32 {
@@ -126,10 +169,12 @@ struct Rows32 {
   floatx16 o[DT];
   float m, z;  // running maximum (log2 units), and sum of this lane's keys
 
+  template <bool kPairedSlabs>
   __device__ __forceinline__ void start(const _Float16* from) {  // the lane's row
     const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) q[kk] = load_half8(from + kk * 16 + half * 8);
+    for (int kk = 0; kk < KK; ++kk)
+      q[kk] = load_half8(from + (kPairedSlabs ? 16 * (2 * (kk / 2) + half) + 8 * (kk % 2) : kk * 16 + half * 8));
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -138,12 +183,12 @@ struct Rows32 {
     z = 0.f;
   }
 
-  // kSub * 32 keys that lie in LDS from row `at` of sm_k and sm_v; key0: the first one's
-  // number.  kMasked: the lane's row sees keys up to last_key only.
-  template <int kSub, bool kMasked>
-  __device__ __forceinline__ void attend(const half8* sm_k, const half8* sm_v, int at, int key0, int last_key,
-                                         float scale_log2e) {
-    const int lane = threadIdx.x & 63, half = lane >> 5;
+  // kSub * 32 keys, key0: the first one's number.  kMasked: the lane's row sees keys up to
+  // last_key only.  after_k: K has been read; before_v: V is needed.
+  template <int kSub, bool kMasked, typename Keys, typename AfterK, typename BeforeV>
+  __device__ __forceinline__ void attend(const Keys& keys, int key0, int last_key, float scale_log2e, AfterK after_k,
+                                         BeforeV before_v) {
+    const int half = (threadIdx.x & 63) >> 5;
     floatx16 s[kSub];
 #pragma unroll
     for (int u = 0; u < kSub; ++u)
@@ -153,8 +198,8 @@ struct Rows32 {
     for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
       for (int u = 0; u < kSub; ++u)
-        s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(sm_k[k_chunk<D>(at + u * 32 + (lane & 31), 2 * kk + half)], q[kk],
-                                                      s[u], 0, 0, 0);
+        s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(keys.k_slab(u, kk), q[kk], s[u], 0, 0, 0);
+    after_k();
     float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kSub; ++u)
@@ -180,14 +225,12 @@ struct Rows32 {
       m = mn;
     }
     const float base = m == -INFINITY ? 0.f : m;
+    before_v();
     // Where some row does not see some key, 0 * inf and 0 * NaN must not reach it: channels of V
     // that are no finite numbers are added where their key is seen, and are zeros in the product.
     bool dirty = false;
     if constexpr (kMasked) {
-      uint32_t found = 0;
-#pragma unroll
-      for (int i = 0; i < kSub * 32 * D / 8 / 64; ++i) found |= nonfinite(sm_v[at * (D / 8) + i * 64 + lane]);
-      dirty = __any(found != 0);
+      dirty = keys.template dirty<kSub>();
       if (dirty) {
 #pragma unroll 1
         for (int key = 0; key < kSub * 32; ++key) {
@@ -196,12 +239,9 @@ struct Rows32 {
           for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const int c = dt * 32 + j * 8 + half * 4;
-              const half4 x = *reinterpret_cast<const half4*>(
-                  reinterpret_cast<const _Float16*>(sm_v + v_chunk<D>(at + key, c / 8)) + half * 4);
+              const floatx4 x = keys.not_finite(key, dt * 32 + j * 8 + half * 4);
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (seen && abs_bits(x[e]) >= 0x7c00u) o[dt][4 * j + e] += (float)x[e];
+              for (int e = 0; e < 4; ++e) o[dt][4 * j + e] += seen ? x[e] : 0.f;
             }
         }
       }
@@ -216,23 +256,15 @@ struct Rows32 {
         pb[r >> 3][r & 7] = (_Float16)w;
       }
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        // keys 16 kk + 4 half + 0..3 and 8 more: rows (lane % 16) / 4 of the transposing reads
-        const int r = at + u * 32 + kk * 16 + half * 4 + ((lane & 15) >> 2);
+      for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
-          const int c = dt * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-          const _Float16* a0 = reinterpret_cast<const _Float16*>(sm_v + v_chunk<D>(r, c)) + (lane & 1) * 4;
-          const _Float16* a1 = reinterpret_cast<const _Float16*>(sm_v + v_chunk<D>(r + 8, c)) + (lane & 1) * 4;
-          const fp16x4 lo = read_columns(a0), hi = read_columns(a1);
-          half8 v = {(_Float16)lo[0], (_Float16)lo[1], (_Float16)lo[2], (_Float16)lo[3],
-                     (_Float16)hi[0], (_Float16)hi[1], (_Float16)hi[2], (_Float16)hi[3]};
+          half8 v = keys.v_slab(u, kk, dt);
           if constexpr (kMasked) {
             if (dirty) v = finite_only(v);
           }
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pb[kk], o[dt], 0, 0, 0);
         }
-      }
     }
   }
 };
@@ -243,12 +275,12 @@ struct Place {
   int n_rows, tile, nb, n_seg, seg, key_begin, key_end;
 };
 template <int kRows, bool kSplit, typename Reqs>
-__device__ __forceinline__ Place place_of(const AttnParams& p, const Reqs& reqs, int unit) {
+__device__ __forceinline__ Place place_of(const AttnParams& p, const Reqs& reqs, const AttnLaunchView& l, int unit) {
   Place w;
-  w.rq = reqs.req[request_of(reqs, p.n_req, unit)];
+  w.rq = reqs.req[request_of(reqs, l.first_req, l.first_req + l.n_req, unit)];
   w.n_rows = w.rq.n_new * p.group;
   w.nb = (w.rq.seq_len + 15) >> 4;
-  w.n_seg = kSplit ? decode_segments(w.nb, p.seg_blocks) : 1;
+  w.n_seg = kSplit ? decode_segments(w.nb, l.seg_blocks) : 1;
   const int at = unit - w.rq.unit_start;
   w.seg = kSplit ? at % w.n_seg : 0;
   // (the last rows see most keys: first)
@@ -279,8 +311,9 @@ __device__ __forceinline__ _Float16* row_of(const RowsView& v, const ChunkReq& r
   return v.data + (int64_t)(rq.row_off + token) * v.token_stride + (int64_t)head * v.head_stride;
 }
 template <int D>
-__device__ __forceinline__ float* state_of(const AttnParams& p, const ChunkReq& rq, int token, int q_head, int seg) {
-  return p.states + (((int64_t)(rq.state_off + token) * p.n_heads * p.group + q_head) * p.n_seg + seg) *
+__device__ __forceinline__ float* state_of(const AttnParams& p, const AttnLaunchView& l, const ChunkReq& rq, int token,
+                                           int q_head, int seg) {
+  return l.states + (((int64_t)(rq.state_off + token) * p.n_heads * p.group + q_head) * l.n_seg + seg) *
                         DecodeParams::state_words(D);
 }
 __device__ __forceinline__ void write_lse(const AttnParams& p, const ChunkReq& rq, int token, int q_head, float log2_sum) {
@@ -347,6 +380,115 @@ struct Block8 {
   }
 };
 
+// The same as codes for a wavefront that works on them alone: they go straight to LDS and
+// become fp16 numbers as they are read.  Rows of D bytes, 16-byte chunks permuted for K's
+// reads (32 rows at one chunk) and V's transposing ones (eight rows, of two blocks of
+// channels).
+template <int D>
+__device__ __forceinline__ int k8_chunk(int r, int c) {
+  return r * (D / 16) + (D == 128 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3));
+}
+template <int D>
+__device__ __forceinline__ int v8_chunk(int r, int c) {
+  const int swap = D == 128 ? (((r >> 1) & 1) << 1) | (((r >> 3) & 1) << 2) : ((r >> 3) & 1) << 1;
+  return r * (D / 16) + (c ^ swap);
+}
+template <int D>
+struct Loader8 {
+  static constexpr int kInstr = D / 64;  // wavefront loads of 16 rows of K, and of V
+  int k_at[kInstr], v_at[kInstr];
+  __device__ __forceinline__ Loader8() {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < kInstr; ++i) {
+      const int r = (i * 64 + lane) / (D / 16), c = lane % (D / 16);
+      k_at[i] = k8_chunk<D>(r, c) * 16;
+      v_at[i] = v8_chunk<D>(r, c) * 16;
+    }
+  }
+  __device__ __forceinline__ void k(BufferPtr from, half8* to) const {
+#pragma unroll
+    for (int i = 0; i < kInstr; ++i) load_to_lds(from, k_at[i], 0, to + i * 64);
+  }
+  __device__ __forceinline__ void v(BufferPtr from, half8* to) const {
+#pragma unroll
+    for (int i = 0; i < kInstr; ++i) load_to_lds(from, v_at[i], 0, to + i * 64);
+  }
+};
+// (lane l: of the eight rows that the sixteen lanes around it point to, two lanes a row, byte l % 16)
+__device__ __forceinline__ int2v read_byte_columns(const uint8_t* __restrict at) {
+  return __builtin_amdgcn_ds_read_tr8_b64_v2i32((LdsPair)at);
+}
+template <int D>
+struct E4m3Keys {
+  static constexpr bool kPairedSlabs = true;  // a 16-byte read of K is its lane's part of two slabs
+  const uint8_t *k, *v;
+  float k_scale;         // of the lane's key
+  half2v v_scale[2][4];  // of the lane's eight keys of a slab of V
+  __device__ __forceinline__ half8 k_slab(int, int kk) const {
+    const int lane = threadIdx.x & 63;
+    const uint4v c = *reinterpret_cast<const uint4v*>(k + k8_chunk<D>(lane & 31, 2 * (kk / 2) + (lane >> 5)) * 16);
+    return e4m3_values(c[2 * (kk % 2)], c[2 * (kk % 2) + 1], k_scale);
+  }
+  // exponents of the two blocks; keys behind `last` are seen by no row (and their slots may
+  // hold anything): times zero
+  template <bool kMasked>
+  __device__ __forceinline__ void set_v(const uint4v (&exponents)[2], int last) {
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const uint32_t e = half ? exponents[kk][2 * w + 1] : exponents[kk][2 * w];
+        float f[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          f[j] = e4m3_scale((e >> (8 * j)) & 255u);
+          if (kMasked && 16 * kk + 8 * w + 4 * half + j > last) f[j] = 0.f;
+        }
+        v_scale[kk][2 * w] = half2v{(_Float16)f[0], (_Float16)f[1]};
+        v_scale[kk][2 * w + 1] = half2v{(_Float16)f[2], (_Float16)f[3]};
+      }
+  }
+  __device__ __forceinline__ half8 v_slab(int, int kk, int dt) const {
+    const int lane = threadIdx.x & 63;
+    // row (lane % 16) / 2 of the read: keys 4 half + 0..3, then 8 more
+    const int i = (lane & 15) >> 1;
+    const int r = kk * 16 + (lane >> 5) * 4 + (i & 3) + (i & 4) * 2;
+    const int c = dt * 2 + ((lane >> 4) & 1);
+    const int2v x = read_byte_columns(v + v8_chunk<D>(r, c) * 16 + (lane & 1) * 8);
+    half8 y;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const half2v a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x[w], 1.f, false) * v_scale[kk][2 * w];
+      const half2v b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x[w], 1.f, true) * v_scale[kk][2 * w + 1];
+      y[4 * w] = a[0];
+      y[4 * w + 1] = a[1];
+      y[4 * w + 2] = b[0];
+      y[4 * w + 3] = b[1];
+    }
+    return y;
+  }
+  template <int kSub>
+  __device__ __forceinline__ bool dirty() const {
+    uint32_t found = 0;
+#pragma unroll
+    for (int i = 0; i < 32 * D / 16 / 64; ++i) {
+      const uint4v x = reinterpret_cast<const uint4v*>(v)[i * 64 + (threadIdx.x & 63)];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) found |= (x[w] & 0x7f7f7f7fu) + 0x01010101u;
+    }
+    return __any((found & 0x80808080u) != 0);
+  }
+  __device__ __forceinline__ floatx4 not_finite(int key, int channel) const {
+    const uint32_t x = *reinterpret_cast<const uint32_t*>(v + v8_chunk<D>(key, channel / 16) * 16 + channel % 16);
+    floatx4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = ((x >> (8 * e)) & 0x7fu) == 0x7fu ? __builtin_nanf("") : 0.f;
+    return y;
+  }
+};
+
 // Block b of the request's cache (behind the last one: the last one, whose rows nobody sees there).
 __device__ __forceinline__ int block_id(const AttnParams& p, const int32_t* table, int b, int nb) {
   return clamp_block(load_uniform(table + min(b, nb - 1)), p.n_blocks);
@@ -369,12 +511,10 @@ __device__ __forceinline__ BufferPtr rows_at(const _Float16* from, int stride, i
 // while one is worked on, each wavefront brings in 16 keys of the next.
 // ---------------------------------------------------------------------------
 template <int D, int SRC, bool kSplit, typename Reqs>
-__global__ __launch_bounds__(256, 2) void attention_tall_kernel(AttnParams p, Reqs reqs) {
-  constexpr int kKeys = 64, kTile = kKeys * D / 8;  // half8s of K, and of V
-  extern __shared__ __align__(16) half8 sm[];       // [2][K, V][kTile]
-  const int unit = blockIdx.x / p.n_heads;
-  const int head = blockIdx.x - unit * p.n_heads;
-  const Place w = place_of<kTallRows, kSplit>(p, reqs, unit);
+__device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& reqs, half8* sm, int unit, int head) {
+  constexpr int kKeys = 64, kTile = kKeys * D / 8;  // half8s of K, and of V; sm: [2][K, V][kTile]
+  const AttnLaunchView& l = p.launch[ATTN_TALL];
+  const Place w = place_of<kTallRows, kSplit>(p, reqs, l, unit);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int first_key = w.rq.seq_len - w.rq.n_new;  // what token 0 sees last
@@ -387,7 +527,7 @@ __global__ __launch_bounds__(256, 2) void attention_tall_kernel(AttnParams p, Re
   const int n_full = max(min(first_key + w.tile * kTallRows / p.group, w.key_end - 1) + 1 - w.key_begin, 0) / kKeys;
 
   Rows32<D> rows;
-  rows.start(row_of(p.q, w.rq, me.token, me.q_head));
+  rows.template start<false>(row_of(p.q, w.rq, me.token, me.q_head));
 
   const int32_t* table = SRC == ATTN_ROWS ? nullptr : p.block_tables + (size_t)w.rq.table_row * p.max_blocks;
   const int k_stride = SRC == ATTN_ROWS ? (int)p.k.token_stride : D, v_stride = SRC == ATTN_ROWS ? (int)p.v.token_stride : D;
@@ -435,7 +575,7 @@ __global__ __launch_bounds__(256, 2) void attention_tall_kernel(AttnParams p, Re
     const half8* sm_k = sm + (t & 1) * 2 * kTile;
     const int key0 = w.key_begin + t * kKeys;
     if (!kMasked || key0 <= wave_last)  // uniform over the wavefront: else none of its rows sees these
-      rows.template attend<2, kMasked>(sm_k, sm_k + kTile, 0, key0, last_key, p.scale_log2e);
+      rows.template attend<2, kMasked>(F16Keys<D>{sm_k, sm_k + kTile, 0}, key0, last_key, p.scale_log2e, [] {}, [] {});
     if constexpr (SRC == ATTN_E4M3) {
       if (t + 1 < n_tiles) put8(t + 1);
     }
@@ -453,7 +593,7 @@ __global__ __launch_bounds__(256, 2) void attention_tall_kernel(AttnParams p, Re
   const float log2_sum = z == 0.f ? -INFINITY : rows.m + __builtin_amdgcn_logf(z);
   if (!me.real) return;
   if (kSplit && w.n_seg > 1) {  // a segment's state: the normalised result and the log2 of the sum
-    float* state = state_of<D>(p, w.rq, me.token, me.q_head, w.seg);
+    float* state = state_of<D>(p, l, w.rq, me.token, me.q_head, w.seg);
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -482,15 +622,23 @@ __global__ __launch_bounds__(256, 2) void attention_tall_kernel(AttnParams p, Re
 // ---------------------------------------------------------------------------
 // Few rows: four wavefronts over the same 32 rows; each takes every fourth 32 keys, which it
 // brings in by itself (no barrier in the loop), and the four states are joined at the end.
+// A wavefront has room for one tile: K of the next one is on its way as soon as K has been
+// read, V as soon as V has, so that a tile's K or V always is.
 // ---------------------------------------------------------------------------
+
+// Bytes of one row of K or V in the LDS of such a wavefront.
+template <int D, int SRC>
+constexpr int kFlatRowBytes = SRC == ATTN_E4M3 ? D : 2 * D;
+
+// LDS reads before this point have been answered: what they read may be overwritten by loads.
+__device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 template <int D, int SRC, bool kSplit, typename Reqs>
-__global__ __launch_bounds__(256) void attention_flat_kernel(AttnParams p, Reqs reqs) {
-  constexpr int kKeys = 32, kTile = kKeys * D / 8;
-  constexpr int kBuffers = SRC == ATTN_E4M3 ? 1 : 2;
-  extern __shared__ __align__(16) half8 sm[];  // [wavefront][buffer][K, V][kTile]
-  const int unit = blockIdx.x / p.n_heads;
-  const int head = blockIdx.x - unit * p.n_heads;
-  const Place w = place_of<kFlatRows, kSplit>(p, reqs, unit);
+__device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& reqs, half8* sm, int unit, int head) {
+  constexpr int kKeys = 32;
+  constexpr int kTile = kKeys * kFlatRowBytes<D, SRC> / 16;  // sm: [wavefront][K, V][kTile]
+  const AttnLaunchView& l = p.launch[ATTN_FLAT];
+  const Place w = place_of<kFlatRows, kSplit>(p, reqs, l, unit);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int first_key = w.rq.seq_len - w.rq.n_new;
@@ -500,12 +648,15 @@ __global__ __launch_bounds__(256) void attention_flat_kernel(AttnParams p, Reqs 
   const int first_seen = min(first_key + row0 / p.group, w.key_end - 1);  // all rows see keys up to this one
   const int n_tiles = w.key_end > w.key_begin ? (w.key_end - w.key_begin + kKeys - 1) / kKeys : 0;
   const int mine = own_tiles(n_tiles, wave, 4);
+  // tiles that every row sees whole come first
+  const int full = min(mine, own_tiles(max(first_seen + 1 - w.key_begin, 0) / kKeys, wave, 4));
+
+  Rows32<D> rows;
+  rows.template start<SRC == ATTN_E4M3>(row_of(p.q, w.rq, me.token, me.q_head));
 
   const int32_t* table = SRC == ATTN_ROWS ? nullptr : p.block_tables + (size_t)w.rq.table_row * p.max_blocks;
-  const BlockLoader<D> loader(SRC == ATTN_ROWS ? (int)p.k.token_stride * 2 : D * 2,
-                              SRC == ATTN_ROWS ? (int)p.v.token_stride * 2 : D * 2);
-  half8* sm_mine = sm + wave * kBuffers * 2 * kTile;
-  Block8<D> b8[2];
+  half8* sm_k = sm + wave * 2 * kTile;
+  half8* sm_v = sm_k + kTile;
   int ids[2] = {0, 0};
   auto block_of = [&](int i, int j) { return (w.key_begin >> 4) + 2 * (wave + 4 * i) + j; };
   auto look_up = [&](int i) {
@@ -514,54 +665,124 @@ __global__ __launch_bounds__(256) void attention_flat_kernel(AttnParams p, Reqs 
       ids[1] = block_id(p, table, block_of(i, 1), w.nb);
     }
   };
-  auto request = [&](int i) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      half8* to = sm_mine + (i % kBuffers) * 2 * kTile + j * 16 * D / 8;
-      if constexpr (SRC == ATTN_ROWS) {
-        const int first = 16 * block_of(i, j);
-        loader.k(rows_at<D>(row_of(p.k, w.rq, first, head), (int)p.k.token_stride, w.rq.seq_len - first), to);
-        loader.v(rows_at<D>(row_of(p.v, w.rq, first, head), (int)p.v.token_stride, w.rq.seq_len - first), to + kTile);
-      } else if constexpr (SRC == ATTN_F16) {
-        loader.k(f16_block<D>(p, ids[j], head, 0), to);
-        loader.v(f16_block<D>(p, ids[j], head, 1), to + kTile);
-      } else {
-        b8[j].request(static_cast<const uint8_t*>(p.kv) + (size_t)ids[j] * e4m3_block_bytes(p.n_heads, D), p.n_heads, head);
-      }
-    }
-    look_up(i + 1);
-  };
+  auto key_of = [&](int i) { return w.key_begin + (wave + 4 * i) * kKeys; };
 
-  Rows32<D> rows;
-  rows.start(row_of(p.q, w.rq, me.token, me.q_head));
-  if (mine > 0) {
-    look_up(0);
-    request(0);
-  }
-  auto step = [&](int i, auto masked_) {
-    const half8* sm_k = sm_mine + (i % kBuffers) * 2 * kTile;
-    if constexpr (SRC == ATTN_E4M3) {
+  if constexpr (SRC == ATTN_E4M3) {
+    const Loader8<D> loader;
+    E4m3Keys<D> keys{reinterpret_cast<const uint8_t*>(sm_k), reinterpret_cast<const uint8_t*>(sm_v)};
+    uint4v ve[2];
+    uint32_t ke = 0;
+    auto block_at = [&](int j) {
+      return static_cast<const uint8_t*>(p.kv) + (size_t)ids[j] * e4m3_block_bytes(p.n_heads, D);
+    };
+    const size_t v_off = (size_t)p.n_heads * 16 * D;
+    const int e_at = head * 16;  // of the block's exponents
+    auto request_k = [&] {
+      const uint8_t* mine_at = (lane & 16 ? block_at(1) : block_at(0)) + 2 * v_off + e_at + (lane & 15);
+      ke = *mine_at;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) b8[j].put(sm_mine, sm_mine + kTile, 16 * j);
-      wave_lds_barrier();
-      if (i + 1 < mine) request(i + 1);
-    } else {
-      if (i + 1 < mine) {
-        request(i + 1);
-        wait_loads<4 * BlockLoader<D>::kInstr>();
-      } else {
-        wait_loads<0>();
-      }
+      for (int j = 0; j < 2; ++j) loader.k(buffer_of(block_at(j) + (size_t)head * 16 * D, 16 * D), sm_k + j * D);
+    };
+    auto request_v = [&] {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        ve[j] = *reinterpret_cast<const uint4v*>(block_at(j) + 2 * v_off + (size_t)p.n_heads * 16 + e_at);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) loader.v(buffer_of(block_at(j) + v_off + (size_t)head * 16 * D, 16 * D), sm_v + j * D);
+    };
+    constexpr int kLoads = 2 * Loader8<D>::kInstr;
+    if (mine > 0) {
+      look_up(0);
+      request_k();
+      lds_reads_done();  // (K's loads stay ahead of V's, as the waits count on)
+      request_v();
     }
-    rows.template attend<1, decltype(masked_)::value>(sm_k, sm_k + kTile, 0, w.key_begin + (wave + 4 * i) * kKeys, last_key,
-                                                      p.scale_log2e);
-    wave_lds_barrier();
-  };
-  // tiles that every row sees whole come first
-  const int full = min(mine, own_tiles(max(first_seen + 1 - w.key_begin, 0) / kKeys, wave, 4));
-  int i = 0;
-  for (; i < full; ++i) step(i, std::false_type());
-  for (; i < mine; ++i) step(i, std::true_type());
+    auto step = [&](int i, auto masked_) {
+      constexpr bool kMasked = decltype(masked_)::value;
+      const bool more = i + 1 < mine;
+      const int key0 = key_of(i);
+      wait_loads<kLoads + 2>();  // (V and its exponents may be on their way)
+      keys.k_scale = e4m3_scale(ke);
+      rows.template attend<1, kMasked>(
+          keys, key0, last_key, p.scale_log2e,
+          [&] {
+            keys.template set_v<kMasked>(ve, w.key_end - 1 - key0);
+            look_up(i + 1);
+            if (more) {
+              lds_reads_done();
+              request_k();
+            }
+          },
+          [&] {
+            if (more)
+              wait_loads<kLoads + 1>();
+            else
+              wait_loads<0>();
+          });
+      if (more) {
+        lds_reads_done();
+        request_v();
+      }
+    };
+    int i = 0;
+    for (; i < full; ++i) step(i, std::false_type());
+    for (; i < mine; ++i) step(i, std::true_type());
+  } else {
+    const BlockLoader<D> loader(SRC == ATTN_ROWS ? (int)p.k.token_stride * 2 : D * 2,
+                                SRC == ATTN_ROWS ? (int)p.v.token_stride * 2 : D * 2);
+    const F16Keys<D> keys{sm_k, sm_v, 0};
+    auto request_k = [&](int i) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int first = 16 * block_of(i, j);
+        loader.k(SRC == ATTN_ROWS ? rows_at<D>(row_of(p.k, w.rq, first, head), (int)p.k.token_stride, w.rq.seq_len - first)
+                                  : f16_block<D>(p, ids[j], head, 0),
+                 sm_k + j * 2 * D);
+      }
+    };
+    auto request_v = [&](int i) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int first = 16 * block_of(i, j);
+        loader.v(SRC == ATTN_ROWS ? rows_at<D>(row_of(p.v, w.rq, first, head), (int)p.v.token_stride, w.rq.seq_len - first)
+                                  : f16_block<D>(p, ids[j], head, 1),
+                 sm_v + j * 2 * D);
+      }
+    };
+    constexpr int kLoads = 2 * BlockLoader<D>::kInstr;
+    if (mine > 0) {
+      look_up(0);
+      request_k(0);
+      lds_reads_done();  // (K's loads stay ahead of V's, as the waits count on)
+      request_v(0);
+    }
+    auto step = [&](int i, auto masked_) {
+      const bool more = i + 1 < mine;
+      wait_loads<kLoads>();  // (V may be on its way)
+      rows.template attend<1, decltype(masked_)::value>(
+          keys, key_of(i), last_key, p.scale_log2e,
+          [&] {
+            look_up(i + 1);
+            if (more) {
+              lds_reads_done();
+              request_k(i + 1);
+            }
+          },
+          [&] {
+            if (more)
+              wait_loads<kLoads>();
+            else
+              wait_loads<0>();
+          });
+      if (more) {
+        lds_reads_done();
+        request_v(i + 1);
+      }
+    };
+    int i = 0;
+    for (; i < full; ++i) step(i, std::false_type());
+    for (; i < mine; ++i) step(i, std::true_type());
+  }
   const float z = other_half_sum(rows.z), m = rows.m;
 
   // ---- joining the four states -----------------------------------------------------------
@@ -596,7 +817,7 @@ __global__ __launch_bounds__(256) void attention_flat_kernel(AttnParams p, Reqs 
     }
   if (wave == 0 && half == 0 && me.real) {
     if (kSplit && w.n_seg > 1)
-      state_of<D>(p, w.rq, me.token, me.q_head, w.seg)[D] = log2_sum;
+      state_of<D>(p, l, w.rq, me.token, me.q_head, w.seg)[D] = log2_sum;
     else
       write_lse(p, w.rq, me.token, me.q_head, log2_sum);
   }
@@ -609,7 +830,7 @@ __global__ __launch_bounds__(256) void attention_flat_kernel(AttnParams p, Reqs 
 #pragma unroll
     for (int k = 1; k < 4; ++k) x += sm_o[(k * 32 + r) * kQuads + (c ^ (r & (kQuads - 1)))];
     if (kSplit && w.n_seg > 1) {
-      *reinterpret_cast<floatx4*>(state_of<D>(p, w.rq, it.token, it.q_head, w.seg) + c * 4) = x;
+      *reinterpret_cast<floatx4*>(state_of<D>(p, l, w.rq, it.token, it.q_head, w.seg) + c * 4) = x;
     } else {
       half4 y;
 #pragma unroll
@@ -619,14 +840,26 @@ __global__ __launch_bounds__(256) void attention_flat_kernel(AttnParams p, Reqs 
   }
 }
 
+// The units with many rows come first: they are the heavy ones.
+template <int D, int SRC, bool kSplit, typename Reqs>
+__global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, Reqs reqs) {
+  extern __shared__ __align__(16) half8 sm[];
+  const int unit = blockIdx.x / p.n_heads;
+  const int head = blockIdx.x - unit * p.n_heads;
+  if (unit < p.launch[ATTN_TALL].n_units)
+    attend_tall<D, SRC, kSplit>(p, reqs, sm, unit, head);
+  else
+    attend_flat<D, SRC, kSplit>(p, reqs, sm, unit - p.launch[ATTN_TALL].n_units, head);
+}
+
 // Rows whose keys were split: the result from the segments' states.  Workgroup = (token of
 // the launch, query head), one thread per channel.
 template <int D, typename Reqs>
-__global__ __launch_bounds__(D) void attention_merge_kernel(AttnParams p, Reqs reqs) {
+__global__ __launch_bounds__(D) void attention_merge_kernel(AttnParams p, AttnLaunchView l, Reqs reqs) {
   const int n_q = p.n_heads * p.group;
   const int t = blockIdx.x / n_q;
   const int h = blockIdx.x - t * n_q;
-  int lo = 0, hi = p.n_req - 1;
+  int lo = l.first_req, hi = l.first_req + l.n_req - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (reqs.req[mid].state_off <= t)
@@ -635,10 +868,10 @@ __global__ __launch_bounds__(D) void attention_merge_kernel(AttnParams p, Reqs r
       hi = mid - 1;
   }
   const ChunkReq rq = reqs.req[lo];
-  const int n_seg = decode_segments((rq.seq_len + 15) >> 4, p.seg_blocks);
+  const int n_seg = decode_segments((rq.seq_len + 15) >> 4, l.seg_blocks);
   if (n_seg <= 1) return;  // written by the kernel above
   constexpr int kWords = DecodeParams::state_words(D);
-  const float* states = p.states + (int64_t)blockIdx.x * p.n_seg * kWords;
+  const float* states = l.states + (int64_t)blockIdx.x * l.n_seg * kWords;
   float mm = -INFINITY, zz = 0.f, o = 0.f;
   for (int i = 0; i < n_seg; ++i) mm = fmaxf(mm, states[(size_t)i * kWords + D]);
 #pragma unroll 4
@@ -657,50 +890,50 @@ __global__ __launch_bounds__(D) void attention_merge_kernel(AttnParams p, Reqs r
         zz == 0.f ? -INFINITY : (mm + __builtin_amdgcn_logf(zz)) * kLn2;
 }
 
-constexpr int tall_lds(int head_dim) { return 2 * 2 * 64 * head_dim * 2; }
-// (the joined states need as much as one buffer)
-constexpr int flat_lds(int head_dim, int source) { return 4 * (source == ATTN_E4M3 ? 1 : 2) * 2 * 32 * head_dim * 2; }
+// two tiles of many rows; four states of few (which need more than their keys)
+constexpr int lds_bytes(int head_dim) { return std::max(2 * 2 * 64 * head_dim * 2, 4 * 32 * head_dim * 4); }
 
 template <int D, int SRC, bool kSplit, typename Reqs>
-void launch_kernel(const AttnParams& p, bool flat, const Reqs& reqs, hipStream_t s) {
-  const unsigned grid = (unsigned)p.n_units * p.n_heads;
-  if (flat)
-    attention_flat_kernel<D, SRC, kSplit, Reqs><<<grid, 256, flat_lds(D, SRC), s>>>(p, reqs);
-  else
-    attention_tall_kernel<D, SRC, kSplit, Reqs><<<grid, 256, tall_lds(D), s>>>(p, reqs);
+void launch_kernel(const AttnParams& p, const Reqs& reqs, hipStream_t s) {
+  const unsigned grid = (unsigned)(p.launch[0].n_units + p.launch[1].n_units) * p.n_heads;
+  attention_kernel<D, SRC, kSplit, Reqs><<<grid, 256, lds_bytes(D), s>>>(p, reqs);
 }
 
 template <int D, int SRC, typename Reqs>
-void launch_source(const AttnParams& p, bool flat, const Reqs& reqs, hipStream_t s) {
+void launch_source(const AttnParams& p, const Reqs& reqs, hipStream_t s) {
   if constexpr (SRC != ATTN_ROWS) {
-    if (p.n_seg > 1) {
-      launch_kernel<D, SRC, true>(p, flat, reqs, s);
-      attention_merge_kernel<D, Reqs><<<(unsigned)p.state_rows * p.n_heads * p.group, D, 0, s>>>(p, reqs);
+    if (p.launch[0].n_seg > 1 || p.launch[1].n_seg > 1) {
+      launch_kernel<D, SRC, true>(p, reqs, s);
+      for (const AttnLaunchView& l : p.launch)
+        if (l.n_seg > 1)
+          attention_merge_kernel<D, Reqs><<<(unsigned)l.state_rows * p.n_heads * p.group, D, 0, s>>>(p, l, reqs);
       return;
     }
   }
-  launch_kernel<D, SRC, false>(p, flat, reqs, s);
+  launch_kernel<D, SRC, false>(p, reqs, s);
 }
 
 template <int D, typename Reqs>
-void launch_shape(const AttnParams& p, bool flat, const Reqs& reqs, hipStream_t s) {
+void launch_shape(const AttnParams& p, const Reqs& reqs, hipStream_t s) {
   if (p.source == ATTN_ROWS)
-    launch_source<D, ATTN_ROWS>(p, flat, reqs, s);
+    launch_source<D, ATTN_ROWS>(p, reqs, s);
   else if (p.source == ATTN_F16)
-    launch_source<D, ATTN_F16>(p, flat, reqs, s);
+    launch_source<D, ATTN_F16>(p, reqs, s);
   else
-    launch_source<D, ATTN_E4M3>(p, flat, reqs, s);
+    launch_source<D, ATTN_E4M3>(p, reqs, s);
 }
 
 template <typename Reqs>
-hipError_t allow_lds_with() {  // more than 64 KB
+hipError_t allow_lds_with() {  // (with the static words more than 64 KB)
   hipError_t e = hipSuccess;
-  auto allow = [&](const void* kernel, int bytes) {
-    if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  auto allow = [&](const void* kernel) {
+    if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(128));
   };
-  allow(reinterpret_cast<const void*>(&attention_flat_kernel<128, ATTN_ROWS, false, Reqs>), flat_lds(128, ATTN_ROWS));
-  allow(reinterpret_cast<const void*>(&attention_flat_kernel<128, ATTN_F16, false, Reqs>), flat_lds(128, ATTN_F16));
-  allow(reinterpret_cast<const void*>(&attention_flat_kernel<128, ATTN_F16, true, Reqs>), flat_lds(128, ATTN_F16));
+  allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_ROWS, false, Reqs>));
+  allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_F16, false, Reqs>));
+  allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_F16, true, Reqs>));
+  allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_E4M3, false, Reqs>));
+  allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_E4M3, true, Reqs>));
   return e;
 }
 
@@ -711,15 +944,16 @@ hipError_t attention_one_time_setup() {
   return e == hipSuccess ? allow_lds_with<ChunkReqList>() : e;
 }
 
-hipError_t launch_attention(const AttnParams& p, bool flat, const ChunkReqs& inline_reqs, hipStream_t s) {
-  if (p.n_units == 0) return hipSuccess;
-  if ((p.head_dim != 64 && p.head_dim != 128) || p.n_seg < 1 || p.seg_blocks < 1 || (p.source == ATTN_ROWS && p.n_seg > 1))
-    return hipErrorInvalidValue;
+hipError_t launch_attention(const AttnParams& p, const ChunkReqs& inline_reqs, hipStream_t s) {
+  if (p.head_dim != 64 && p.head_dim != 128) return hipErrorInvalidValue;
+  for (const AttnLaunchView& l : p.launch)
+    if (l.n_seg < 1 || l.seg_blocks < 1 || (p.source == ATTN_ROWS && l.n_seg > 1)) return hipErrorInvalidValue;
+  if (p.launch[0].n_units + p.launch[1].n_units == 0) return hipSuccess;
   auto with = [&](const auto& reqs) {
     if (p.head_dim == 128)
-      launch_shape<128>(p, flat, reqs, s);
+      launch_shape<128>(p, reqs, s);
     else
-      launch_shape<64>(p, flat, reqs, s);
+      launch_shape<64>(p, reqs, s);
   };
   if (p.reqs)
     with(ChunkReqList{p.reqs});

@@ -15,7 +15,7 @@ using namespace fc;
 
 namespace {
 
-static_assert(kPlanMaxGroup == FC_MAX_GROUP, "limits");
+static_assert(kPlanMaxGroup == FC_MAX_GROUP && kAttnKinds == ATTN_KINDS, "limits");
 
 // (a vector that cannot grow must not throw into C)
 template <typename F>
@@ -92,7 +92,7 @@ int attention(fc_pool* p, int layer, const int32_t* dev_block_tables, int max_bl
   if (!paged && ((rc = check_rows(k, "k", plan.n_rows, p->n_heads, p->head_dim, false)) ||
                  (rc = check_rows(v, "v", plan.n_rows, p->n_heads, p->head_dim, false))))
     return rc;
-  AttnLaunch launches[ATTN_SHAPES];
+  AttnLaunch launches[ATTN_KINDS];
   if (plan_attention(geometry(p), p->n_cu, n_q_heads / p->n_heads, paged, p->decode_partial ? kMaxDecodeSegments : 0, &plan,
                      launches) != PLAN_OK)
     return fail(plan.code, "%s", plan.message);
@@ -118,34 +118,28 @@ int attention(fc_pool* p, int layer, const int32_t* dev_block_tables, int max_bl
     ap.lse_stride = (int64_t)p->n_layers * n_q_heads * window;
   }
   ap.scale_log2e = ((scale > 0.f) ? scale : 1.0f / sqrtf((float)p->head_dim)) * 1.44269504088896340736f;
-  // the requests of both launches: as arguments where each launch's fit, else together to the device
-  ChunkReqs inline_reqs[ATTN_SHAPES];
-  const ChunkReq* on_device = nullptr;
-  if (launches[0].reqs.size() > ChunkReqs::kInline || launches[1].reqs.size() > ChunkReqs::kInline) {
-    std::vector<ChunkReq> all(launches[0].reqs);
-    all.insert(all.end(), launches[1].reqs.begin(), launches[1].reqs.end());
-    const void* at = nullptr;
-    if ((rc = meta_to_device(p, all.data(), all.size() * sizeof(ChunkReq), &at, stream))) return rc;
-    on_device = static_cast<const ChunkReq*>(at);
-  }
-  int64_t states_before = 0;
-  for (int s = 0; s < ATTN_SHAPES; ++s) {
+  std::vector<ChunkReq> reqs(launches[ATTN_TALL].reqs);
+  reqs.insert(reqs.end(), launches[ATTN_FLAT].reqs.begin(), launches[ATTN_FLAT].reqs.end());
+  ChunkReqs inline_reqs;
+  if ((rc = pass_reqs(p, reqs, &inline_reqs, &ap.reqs, stream))) return rc;
+  int first_req = 0;
+  int64_t states = 0;
+  for (int s = 0; s < ATTN_KINDS; ++s) {
     const AttnLaunch& l = launches[s];
-    if (l.reqs.empty()) continue;
-    if (!on_device) std::copy(l.reqs.begin(), l.reqs.end(), inline_reqs[s].req);
-    AttnParams a = ap;
-    a.reqs = on_device ? on_device + (s ? launches[0].reqs.size() : 0) : nullptr;
+    AttnLaunchView& a = ap.launch[s];
+    a.first_req = first_req;
     a.n_req = (int)l.reqs.size();
     a.n_units = (int)l.n_units;
-    a.seg_blocks = l.seg_blocks;
+    a.seg_blocks = std::max(l.seg_blocks, 1);
     a.n_seg = l.n_seg;
+    first_req += a.n_req;
     if (l.n_seg > 1) {
       a.state_rows = (int)l.state_rows;
-      a.states = p->decode_partial + states_before * DecodeParams::state_words(p->head_dim);
-      states_before += l.state_rows * n_q_heads * l.n_seg;
+      a.states = p->decode_partial + states * DecodeParams::state_words(p->head_dim);
+      states += l.state_rows * n_q_heads * l.n_seg;
     }
-    FC_HIP(launch_attention(a, s == ATTN_FLAT, inline_reqs[s], stream));
   }
+  FC_HIP(launch_attention(ap, inline_reqs, stream));
   return FC_OK;
 }
 

@@ -76,17 +76,17 @@ void plan_store_units(ChunkPlan* plan) {
 }
 
 int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, int64_t max_states,
-                   ChunkPlan* plan, AttnLaunch launches[ATTN_SHAPES]) {
-  for (int s = 0; s < ATTN_SHAPES; ++s) launches[s] = AttnLaunch();
+                   ChunkPlan* plan, AttnLaunch launches[kAttnKinds]) {
+  for (int s = 0; s < kAttnKinds; ++s) launches[s] = AttnLaunch();
   for (const ChunkReq& q : plan->reqs)
-    launches[(int64_t)q.n_new * group <= kFlatRows ? ATTN_FLAT : ATTN_TALL].reqs.push_back(q);
+    launches[(int64_t)q.n_new * group <= kFlatRows ? 1 : 0].reqs.push_back(q);
   int64_t states_left = may_split ? max_states : 0;
-  for (int s = 0; s < ATTN_SHAPES; ++s) {
+  for (int s = 0; s < kAttnKinds; ++s) {
     AttnLaunch& l = launches[s];
     if (l.reqs.empty()) continue;
     std::stable_sort(l.reqs.begin(), l.reqs.end(),
                      [](const ChunkReq& a, const ChunkReq& b) { return a.seq_len > b.seq_len; });
-    const int tile = s == ATTN_TALL ? kTallRows : kFlatRows;
+    const int tile = s == 0 ? kTallRows : kFlatRows;
     auto tiles = [&](const ChunkReq& q) { return ((int64_t)q.n_new * group + tile - 1) / tile; };
     const int longest = blocks_for(l.reqs.front().seq_len);
     l.seg_blocks = std::max(longest, 1);
@@ -115,7 +115,7 @@ int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, in
       q.state_off = (int32_t)state_off;
       state_off += q.n_new;
       l.n_units += tiles(q) * decode_segments(blocks_for(q.seq_len), l.seg_blocks);
-      if (l.n_units * pool.n_heads > kMaxRows || (int64_t)q.n_new * group > kMaxRows)
+      if ((launches[0].n_units + launches[1].n_units) * pool.n_heads > kMaxRows)
         return fail(plan, PLAN_EINVAL, "batch too large for one launch");
     }
   }

@@ -30,10 +30,10 @@ int plan_chunk(int n_req, int max_blocks, const int32_t* seq_lens, const int32_t
 // fc_store_chunk: a unit is a packed row.
 void plan_store_units(ChunkPlan* plan);
 
-// The launches of an attention: requests with many rows to a head of K and V take workgroups
-// whose wavefronts have rows of their own, requests with few rows wavefronts that share the
-// keys (fc_attention.hip).
-enum { ATTN_TALL = 0, ATTN_FLAT = 1, ATTN_SHAPES = 2 };
+// The requests of an attention by kind: those with many rows to a head of K and V take
+// workgroups whose wavefronts have rows of their own, those with few rows wavefronts that
+// share the keys (fc_attention.hip).  AttnLaunch[0] has many rows, [1] few.
+static constexpr int kAttnKinds = 2;
 static constexpr int kTallRows = 128;  // rows (new tokens x query heads of a group) of a workgroup
 static constexpr int kFlatRows = 32;
 struct AttnLaunch {
@@ -45,7 +45,7 @@ struct AttnLaunch {
 // group: query heads per head of K and V; max_states: states that fit the pool's memory, 0 for
 // none.  FC_EINVAL (plan->code) where the launch would be too large.
 int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, int64_t max_states,
-                   ChunkPlan* plan, AttnLaunch launches[ATTN_SHAPES]);
+                   ChunkPlan* plan, AttnLaunch launches[kAttnKinds]);
 
 // fc_quantise_batch: a unit is a block of a request.
 int plan_quantise(int n_req, int dst_max_blocks, int src_max_blocks, const int32_t* seq_lens,

@@ -118,7 +118,16 @@ struct QuantiseParams {
   int32_t n_units;  // blocks of all requests
 };
 
+enum { ATTN_TALL = 0, ATTN_FLAT = 1, ATTN_KINDS = 2 };  // many rows a request, few (fc_chunk_plan.h)
 enum { ATTN_ROWS = 0, ATTN_F16 = 1, ATTN_E4M3 = 2 };  // where K and V are: packed rows, a pool
+// The requests of one kind (ATTN_TALL, ATTN_FLAT) among those of a launch.
+struct AttnLaunchView {
+  int32_t first_req, n_req;
+  int32_t n_units;            // row tiles x segments
+  int32_t seg_blocks, n_seg;  // blocks per segment of a head, segments of the longest one
+  int32_t state_rows;         // rows (tokens) that have states
+  float* states;              // [row][head][n_seg][DecodeParams::state_words]
+};
 struct AttnParams {
   const void* kv;  // the layer's blocks
   int32_t source;  // ATTN_*
@@ -126,18 +135,14 @@ struct AttnParams {
   const int32_t* block_tables;
   int32_t max_blocks;
   const ChunkReq* reqs;  // NULL: in the ChunkReqs argument
-  int32_t n_req;
-  int32_t n_units;       // row tiles x segments of all requests
-  int32_t seg_blocks, n_seg;
-  int32_t state_rows;    // rows (tokens) of the requests of this launch
+  AttnLaunchView launch[ATTN_KINDS];
   RowsView q, k, v, out;
   float* lse;            // nullable: this layer's [head][window] of request 0
   int64_t lse_stride;    // between requests
   int32_t window;
   float scale_log2e;
-  float* states;         // [row][head][n_seg][DecodeParams::state_words]
 };
-static_assert(sizeof(AttnParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
+static_assert(sizeof(AttnParams) + sizeof(AttnLaunchView) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
                   sizeof(StoreParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
                   sizeof(QuantiseParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
                   sizeof(ExtendParams) + sizeof(ExtendReqs) <= kMaxArgumentBytes,
@@ -273,9 +278,9 @@ hipError_t launch_decode_attention(const DecodeParams& p, const DecodeReqs& inli
 hipError_t launch_extend(const ExtendParams& p, const ExtendReqs& inline_reqs, hipStream_t s);
 hipError_t launch_store_chunk(const StoreParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
 hipError_t launch_quantise(const QuantiseParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
-// ... and their attention (fc_attention.hip); flat: few rows a request (ATTN_FLAT)
+// ... and their attention (fc_attention.hip)
 hipError_t attention_one_time_setup();
-hipError_t launch_attention(const AttnParams& p, bool flat, const ChunkReqs& inline_reqs, hipStream_t s);
+hipError_t launch_attention(const AttnParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
 // chunk-MLP compressor (fc_mlp.hip)
 hipError_t mlp_one_time_setup();
 size_t mlp_w1p_elems(int head_dim, int hidden, int k);

@@ -153,6 +153,41 @@ def test_what_a_row_does_not_see_has_no_influence(bad, dim):
         c.close()
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("fill", [0x00, 0x7e, 0xff])
+def test_what_lies_behind_the_last_token_of_an_8_bit_block(fill, dim):
+    """Codes and exponents of slots that hold no token: zeros, the largest numbers, not a number."""
+    import torch
+    from paper_2503_08461_amd import fastcache as fc
+    lens, news = [5, 40, 200, 81], [5, 1, 70, 17]
+    c = Chunk(lens, news, 2, 2, dim, dtype="e4m3")
+    try:
+        h = c.heads
+        for r, n in enumerate(lens):
+            if n % 16:
+                block = c.kv_dev[1, int(c.table[r, n // 16])]
+                block[:32 * h * dim].view(2, h, 16, dim)[:, :, n % 16:] = fill
+                block[32 * h * dim:].view(2, h, 16)[:, :, n % 16:] = fill
+        # a token that only the last rows see is not a number
+        c.v_dev[5 + 1 + 60, 1, 7] = float("nan")
+        fc.fc_store_chunk(c.pool, 1, c.table_dev, c.lens, c.news, c.k_dev, c.v_dev)
+        out = fc.fc_chunk_attention(c.pool, 1, c.table_dev, c.lens, c.news, c.q_dev).cpu().numpy()
+        assert np.isnan(out[5 + 1 + 60:76, 2:, 7]).all()
+        out[5 + 1 + 60:76, 2:] = 0
+        assert np.isfinite(out).all()
+        rows = c.pool_rows(1)
+        at = 0
+        for r, n in enumerate(news):
+            k, v = c.cached(rows, r)
+            for j in range(4):
+                seen = 60 if r == 2 and j >= 2 else n     # rows before the one that is not a number
+                check(c.q[at:at + seen, j], k[j // 2][:lens[r] - n + seen], v[j // 2][:lens[r] - n + seen], lens[r] - n,
+                      out[at:at + seen, j])
+            at += n
+    finally:
+        c.close()
+
+
 def test_extend_pops_in_batch_order():
     import torch
     from paper_2503_08461_amd import fastcache as fc
