@@ -5,6 +5,7 @@
 // no host wait happens inside fc_compress_batch once scratch is sized.
 
 #include "../../include/fastcache.h"
+#include "fc_chunk_plan.h"
 #include "fc_internal.h"
 #include "fc_plan.h"
 #include "fc_pool.h"
@@ -190,11 +191,12 @@ int fc_pool_create(fc_pool** out, void* kv_base, size_t kv_bytes, int n_blocks, 
   if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void**>(&p->error_flag), 2 * sizeof(int32_t));
   if (e == hipSuccess) e = launch_zero_ints(p->error_flag, 2, nullptr);
   p->arrivals = p->error_flag ? p->error_flag + 1 : nullptr;
-  // (a fixed size, here and not on demand: no decode step waits for an allocation;
-  // without it no head is cut into segments)
+  // (a fixed size, here and not on demand: no decode step waits for an allocation, and a
+  // captured one finds it where it was; without it no head is cut into segments)
   if (e == hipSuccess &&
       hipMalloc(reinterpret_cast<void**>(&p->decode_partial),
-                (size_t)kMaxDecodeSegments * DecodeParams::state_words(head_dim) * sizeof(float)) != hipSuccess) {
+                (size_t)std::max(kMaxDecodeSegments, kMaxAttnStates) * DecodeParams::state_words(head_dim) * sizeof(float)) !=
+          hipSuccess) {
     p->decode_partial = nullptr;
     (void)hipGetLastError();  // (a later launch must not report it)
   }

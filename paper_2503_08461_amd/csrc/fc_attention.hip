@@ -62,19 +62,6 @@ __device__ __forceinline__ float other_half_sum(float v) {
   return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
-template <typename Reqs>
-__device__ __forceinline__ int request_of(const Reqs& reqs, int begin, int end, int u) {
-  int lo = begin, hi = end - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (reqs.req[mid].unit_start <= u)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
-  return lo;
-}
-
 // Nonzero where one of the eight numbers is infinite or not a number (exponent bits all set).
 __device__ __forceinline__ uint32_t nonfinite(half8 x) {
   const uint4v w = __builtin_bit_cast(uint4v, x);
@@ -95,9 +82,14 @@ typedef __amdgpu_buffer_rsrc_t BufferPtr;
 __device__ __forceinline__ BufferPtr buffer_of(const void* base, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
 }
-__device__ __forceinline__ void load_to_lds(BufferPtr from, int lane_offset, int offset, half8* to) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, lane_offset, offset,
-                                           0, 0);
+// kOnce: the line is the first to leave the caches (no workgroup but this one reads it).
+template <bool kOnce>
+__device__ __forceinline__ void load_to_lds(BufferPtr from, int lane_offset, half8* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, lane_offset, 0, 0,
+                                           kOnce ? 2 : 0);
+}
+__device__ __forceinline__ void load_word_to_lds(BufferPtr from, int lane_offset, void* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 4, lane_offset, 0, 0, 0);
 }
 // V's operand: lane l gets, of the four rows that the sixteen lanes around it point to (four
 // lanes a row, 8 bytes each), channel l % 16.  (restrict: without it the compiler waits for
@@ -277,7 +269,7 @@ struct Place {
 template <int kRows, bool kSplit, typename Reqs>
 __device__ __forceinline__ Place place_of(const AttnParams& p, const Reqs& reqs, const AttnLaunchView& l, int unit) {
   Place w;
-  w.rq = reqs.req[request_of(reqs, l.first_req, l.first_req + l.n_req, unit)];
+  w.rq = reqs.req[request_of(l.first_req, l.n_req, unit, [&](int i) { return reqs.req[i].unit_start; })];
   w.n_rows = w.rq.n_new * p.group;
   w.nb = (w.rq.seq_len + 15) >> 4;
   w.n_seg = kSplit ? decode_segments(w.nb, l.seg_blocks) : 1;
@@ -324,7 +316,7 @@ __device__ __forceinline__ void write_lse(const AttnParams& p, const ChunkReq& r
 // Sixteen keys (a pool block) on their way to LDS by one wavefront, K and V in one call each.
 // The rows lie in LDS from slot 0 of `to`, which is a multiple of 16 rows into a tile; the
 // permutation of the chunks is in the addresses that the lanes read from.
-template <int D>
+template <int D, bool kOnce>
 struct BlockLoader {
   static constexpr int kInstr = 16 * D / 8 / 64;  // wavefront loads of K, and of V
   int k_at[kInstr], v_at[kInstr];                 // byte offset of the lane's chunk, by load
@@ -339,11 +331,11 @@ struct BlockLoader {
   }
   __device__ __forceinline__ void k(BufferPtr from, half8* to) const {
 #pragma unroll
-    for (int i = 0; i < kInstr; ++i) load_to_lds(from, k_at[i], 0, to + i * 64);
+    for (int i = 0; i < kInstr; ++i) load_to_lds<kOnce>(from, k_at[i], to + i * 64);
   }
   __device__ __forceinline__ void v(BufferPtr from, half8* to) const {
 #pragma unroll
-    for (int i = 0; i < kInstr; ++i) load_to_lds(from, v_at[i], 0, to + i * 64);
+    for (int i = 0; i < kInstr; ++i) load_to_lds<kOnce>(from, v_at[i], to + i * 64);
   }
 };
 
@@ -408,17 +400,18 @@ struct Loader8 {
   }
   __device__ __forceinline__ void k(BufferPtr from, half8* to) const {
 #pragma unroll
-    for (int i = 0; i < kInstr; ++i) load_to_lds(from, k_at[i], 0, to + i * 64);
+    for (int i = 0; i < kInstr; ++i) load_to_lds<true>(from, k_at[i], to + i * 64);
   }
   __device__ __forceinline__ void v(BufferPtr from, half8* to) const {
 #pragma unroll
-    for (int i = 0; i < kInstr; ++i) load_to_lds(from, v_at[i], 0, to + i * 64);
+    for (int i = 0; i < kInstr; ++i) load_to_lds<true>(from, v_at[i], to + i * 64);
   }
 };
 // (lane l: of the eight rows that the sixteen lanes around it point to, two lanes a row, byte l % 16)
 __device__ __forceinline__ int2v read_byte_columns(const uint8_t* __restrict at) {
   return __builtin_amdgcn_ds_read_tr8_b64_v2i32((LdsPair)at);
 }
+constexpr int kExponentBytes = 256;  // of a block, in LDS (what one load of a word a lane fills)
 template <int D>
 struct E4m3Keys {
   static constexpr bool kPairedSlabs = true;  // a 16-byte read of K is its lane's part of two slabs
@@ -430,16 +423,20 @@ struct E4m3Keys {
     const uint4v c = *reinterpret_cast<const uint4v*>(k + k8_chunk<D>(lane & 31, 2 * (kk / 2) + (lane >> 5)) * 16);
     return e4m3_values(c[2 * (kk % 2)], c[2 * (kk % 2) + 1], k_scale);
   }
-  // exponents of the two blocks; keys behind `last` are seen by no row (and their slots may
-  // hold anything): times zero
+  // From the exponents in LDS, 16 of K and 16 of V for each of the two blocks.  Keys behind
+  // `last` are seen by no row (and their slots may hold anything): times zero.
+  __device__ __forceinline__ void set_k(const uint8_t* exponents) {
+    const int lane = threadIdx.x & 63;
+    k_scale = e4m3_scale(exponents[((lane & 31) >> 4) * kExponentBytes + (lane & 15)]);
+  }
   template <bool kMasked>
-  __device__ __forceinline__ void set_v(const uint4v (&exponents)[2], int last) {
+  __device__ __forceinline__ void set_v(const uint8_t* exponents, int last) {
     const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
-        const uint32_t e = half ? exponents[kk][2 * w + 1] : exponents[kk][2 * w];
+        const uint32_t e = *reinterpret_cast<const uint32_t*>(exponents + kk * kExponentBytes + 16 + 8 * w + 4 * half);
         float f[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -494,10 +491,10 @@ __device__ __forceinline__ int block_id(const AttnParams& p, const int32_t* tabl
   return clamp_block(load_uniform(table + min(b, nb - 1)), p.n_blocks);
 }
 template <int D>
-__device__ __forceinline__ BufferPtr f16_block(const AttnParams& p, int blk, int head, int which) {
+__device__ __forceinline__ BufferPtr f16_block(const AttnParams& p, int blk, int head, int which, bool wanted = true) {
   const size_t half_block = (size_t)p.n_heads * 16 * D;
   return buffer_of(static_cast<const _Float16*>(p.kv) + (size_t)blk * 2 * half_block + which * half_block + (size_t)head * 16 * D,
-                   16 * D * 2);
+                   wanted ? 16 * D * 2 : 0);
 }
 // Packed rows from address `from` on, rows_left of them the request's (what is read behind
 // them is zeros).
@@ -531,7 +528,7 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
 
   const int32_t* table = SRC == ATTN_ROWS ? nullptr : p.block_tables + (size_t)w.rq.table_row * p.max_blocks;
   const int k_stride = SRC == ATTN_ROWS ? (int)p.k.token_stride : D, v_stride = SRC == ATTN_ROWS ? (int)p.v.token_stride : D;
-  const BlockLoader<D> loader(2 * k_stride, 2 * v_stride);
+  const BlockLoader<D, false> loader(2 * k_stride, 2 * v_stride);
   half8* to_mine = sm + wave * 16 * D / 8;
   // the next 16 keys that this wavefront brings in
   int block = (w.key_begin >> 4) + wave, next_id = 0;
@@ -636,7 +633,10 @@ __device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmc
 template <int D, int SRC, bool kSplit, typename Reqs>
 __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& reqs, half8* sm, int unit, int head) {
   constexpr int kKeys = 32;
-  constexpr int kTile = kKeys * kFlatRowBytes<D, SRC> / 16;  // sm: [wavefront][K, V][kTile]
+  // (codes: two tiles a wavefront fit where one of fp16 rows does; one keeps 6 KB on the way
+  // on average, and 2048 wavefronts of them draw 4.2 TB/s)
+  constexpr int kStages = SRC == ATTN_E4M3 ? 2 : 1;
+  constexpr int kTile = kKeys * kFlatRowBytes<D, SRC> / 16;  // sm: [wavefront][stage][K, V][kTile], exponents
   const AttnLaunchView& l = p.launch[ATTN_FLAT];
   const Place w = place_of<kFlatRows, kSplit>(p, reqs, l, unit);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -655,8 +655,7 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
   rows.template start<SRC == ATTN_E4M3>(row_of(p.q, w.rq, me.token, me.q_head));
 
   const int32_t* table = SRC == ATTN_ROWS ? nullptr : p.block_tables + (size_t)w.rq.table_row * p.max_blocks;
-  half8* sm_k = sm + wave * 2 * kTile;
-  half8* sm_v = sm_k + kTile;
+  half8* sm_k = sm + wave * 2 * kStages * kTile;
   int ids[2] = {0, 0};
   auto block_of = [&](int i, int j) { return (w.key_begin >> 4) + 2 * (wave + 4 * i) + j; };
   auto look_up = [&](int i) {
@@ -667,76 +666,74 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
   };
   auto key_of = [&](int i) { return w.key_begin + (wave + 4 * i) * kKeys; };
 
+  // (tiles behind the last one are requested as nothing: every wait counts the same loads)
   if constexpr (SRC == ATTN_E4M3) {
     const Loader8<D> loader;
-    E4m3Keys<D> keys{reinterpret_cast<const uint8_t*>(sm_k), reinterpret_cast<const uint8_t*>(sm_v)};
-    uint4v ve[2];
-    uint32_t ke = 0;
+    uint8_t* sm_e = reinterpret_cast<uint8_t*>(sm + 4 * 2 * kStages * kTile) + wave * kStages * 2 * kExponentBytes;
+    const size_t codes = (size_t)2 * p.n_heads * 16 * D;
+    // words 0..3 of the exponents: K's, 4..7: V's
+    const int e_at = lane < 4 ? head * 16 + lane * 4 : lane < 8 ? (p.n_heads + head) * 16 + (lane - 4) * 4 : 1 << 30;
     auto block_at = [&](int j) {
       return static_cast<const uint8_t*>(p.kv) + (size_t)ids[j] * e4m3_block_bytes(p.n_heads, D);
     };
-    const size_t v_off = (size_t)p.n_heads * 16 * D;
-    const int e_at = head * 16;  // of the block's exponents
-    auto request_k = [&] {
-      const uint8_t* mine_at = (lane & 16 ? block_at(1) : block_at(0)) + 2 * v_off + e_at + (lane & 15);
-      ke = *mine_at;
+    auto request_k = [&](int i) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) loader.k(buffer_of(block_at(j) + (size_t)head * 16 * D, 16 * D), sm_k + j * D);
+      for (int j = 0; j < 2; ++j) {
+        load_word_to_lds(buffer_of(block_at(j) + codes, i < mine ? 2 * p.n_heads * 16 : 0), e_at,
+                         sm_e + ((i % kStages) * 2 + j) * kExponentBytes);
+        loader.k(buffer_of(block_at(j) + (size_t)head * 16 * D, i < mine ? 16 * D : 0), sm_k + (i % kStages) * 2 * kTile + j * D);
+      }
     };
-    auto request_v = [&] {
+    auto request_v = [&](int i) {
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        ve[j] = *reinterpret_cast<const uint4v*>(block_at(j) + 2 * v_off + (size_t)p.n_heads * 16 + e_at);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) loader.v(buffer_of(block_at(j) + v_off + (size_t)head * 16 * D, 16 * D), sm_v + j * D);
+        loader.v(buffer_of(block_at(j) + codes / 2 + (size_t)head * 16 * D, i < mine ? 16 * D : 0),
+                 sm_k + (i % kStages) * 2 * kTile + kTile + j * D);
     };
-    constexpr int kLoads = 2 * Loader8<D>::kInstr;
+    constexpr int kV = 2 * Loader8<D>::kInstr, kK = kV + 2;  // loads of a tile
     if (mine > 0) {
-      look_up(0);
-      request_k();
-      lds_reads_done();  // (K's loads stay ahead of V's, as the waits count on)
-      request_v();
+#pragma unroll
+      for (int i = 0; i < kStages; ++i) {
+        look_up(i);
+        request_k(i);
+        lds_reads_done();  // (K's loads stay ahead of V's, as the waits count on)
+        request_v(i);
+        lds_reads_done();
+      }
     }
     auto step = [&](int i, auto masked_) {
       constexpr bool kMasked = decltype(masked_)::value;
-      const bool more = i + 1 < mine;
+      const uint8_t* here = reinterpret_cast<const uint8_t*>(sm_k + (i % kStages) * 2 * kTile);
+      const uint8_t* exponents = sm_e + (i % kStages) * 2 * kExponentBytes;
+      E4m3Keys<D> keys{here, here + kTile * 16};
       const int key0 = key_of(i);
-      wait_loads<kLoads + 2>();  // (V and its exponents may be on their way)
-      keys.k_scale = e4m3_scale(ke);
+      look_up(i + kStages);
+      wait_loads<(kStages - 1) * (kK + kV) + kV>();
+      keys.set_k(exponents);
+      keys.template set_v<kMasked>(exponents, w.key_end - 1 - key0);
       rows.template attend<1, kMasked>(
           keys, key0, last_key, p.scale_log2e,
           [&] {
-            keys.template set_v<kMasked>(ve, w.key_end - 1 - key0);
-            look_up(i + 1);
-            if (more) {
-              lds_reads_done();
-              request_k();
-            }
+            lds_reads_done();
+            request_k(i + kStages);
           },
-          [&] {
-            if (more)
-              wait_loads<kLoads + 1>();
-            else
-              wait_loads<0>();
-          });
-      if (more) {
-        lds_reads_done();
-        request_v();
-      }
+          [] { wait_loads<(kStages - 1) * (kK + kV) + kK>(); });
+      lds_reads_done();
+      request_v(i + kStages);
     };
     int i = 0;
     for (; i < full; ++i) step(i, std::false_type());
     for (; i < mine; ++i) step(i, std::true_type());
   } else {
-    const BlockLoader<D> loader(SRC == ATTN_ROWS ? (int)p.k.token_stride * 2 : D * 2,
-                                SRC == ATTN_ROWS ? (int)p.v.token_stride * 2 : D * 2);
-    const F16Keys<D> keys{sm_k, sm_v, 0};
+    const BlockLoader<D, SRC == ATTN_F16> loader(SRC == ATTN_ROWS ? (int)p.k.token_stride * 2 : D * 2,
+                                                 SRC == ATTN_ROWS ? (int)p.v.token_stride * 2 : D * 2);
+    const F16Keys<D> keys{sm_k, sm_k + kTile, 0};
     auto request_k = [&](int i) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int first = 16 * block_of(i, j);
         loader.k(SRC == ATTN_ROWS ? rows_at<D>(row_of(p.k, w.rq, first, head), (int)p.k.token_stride, w.rq.seq_len - first)
-                                  : f16_block<D>(p, ids[j], head, 0),
+                                  : f16_block<D>(p, ids[j], head, 0, i < mine),
                  sm_k + j * 2 * D);
       }
     };
@@ -745,11 +742,11 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
       for (int j = 0; j < 2; ++j) {
         const int first = 16 * block_of(i, j);
         loader.v(SRC == ATTN_ROWS ? rows_at<D>(row_of(p.v, w.rq, first, head), (int)p.v.token_stride, w.rq.seq_len - first)
-                                  : f16_block<D>(p, ids[j], head, 1),
-                 sm_v + j * 2 * D);
+                                  : f16_block<D>(p, ids[j], head, 1, i < mine),
+                 sm_k + kTile + j * 2 * D);
       }
     };
-    constexpr int kLoads = 2 * BlockLoader<D>::kInstr;
+    constexpr int kLoads = 2 * BlockLoader<D, false>::kInstr;
     if (mine > 0) {
       look_up(0);
       request_k(0);
@@ -757,32 +754,23 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
       request_v(0);
     }
     auto step = [&](int i, auto masked_) {
-      const bool more = i + 1 < mine;
+      look_up(i + 1);
       wait_loads<kLoads>();  // (V may be on its way)
       rows.template attend<1, decltype(masked_)::value>(
           keys, key_of(i), last_key, p.scale_log2e,
           [&] {
-            look_up(i + 1);
-            if (more) {
-              lds_reads_done();
-              request_k(i + 1);
-            }
+            lds_reads_done();
+            request_k(i + 1);
           },
-          [&] {
-            if (more)
-              wait_loads<kLoads>();
-            else
-              wait_loads<0>();
-          });
-      if (more) {
-        lds_reads_done();
-        request_v(i + 1);
-      }
+          [] { wait_loads<kLoads>(); });
+      lds_reads_done();
+      request_v(i + 1);
     };
     int i = 0;
     for (; i < full; ++i) step(i, std::false_type());
     for (; i < mine; ++i) step(i, std::true_type());
   }
+  wait_loads<0>();
   const float z = other_half_sum(rows.z), m = rows.m;
 
   // ---- joining the four states -----------------------------------------------------------
@@ -853,50 +841,67 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, Reqs re
 }
 
 // Rows whose keys were split: the result from the segments' states.  Workgroup = (token of
-// the launch, query head), one thread per channel.
+// the launch, query head); its four wavefronts take every fourth segment, and each finds the
+// common maximum and sum by itself, a segment a lane.
+static constexpr int kMaxHeadSegments = kPlanMaxSeqLen / kPlanBlockSize / kPlanMinSegment;
+static_assert(kMaxHeadSegments <= 128, "two segments a lane");
+
 template <int D, typename Reqs>
-__global__ __launch_bounds__(D) void attention_merge_kernel(AttnParams p, AttnLaunchView l, Reqs reqs) {
+__global__ __launch_bounds__(256) void attention_merge_kernel(AttnParams p, AttnLaunchView l, Reqs reqs) {
   const int n_q = p.n_heads * p.group;
   const int t = blockIdx.x / n_q;
   const int h = blockIdx.x - t * n_q;
-  int lo = l.first_req, hi = l.first_req + l.n_req - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (reqs.req[mid].state_off <= t)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
-  const ChunkReq rq = reqs.req[lo];
+  const ChunkReq rq = reqs.req[request_of(l.first_req, l.n_req, t, [&](int i) { return reqs.req[i].state_off; })];
   const int n_seg = decode_segments((rq.seq_len + 15) >> 4, l.seg_blocks);
   if (n_seg <= 1) return;  // written by the kernel above
   constexpr int kWords = DecodeParams::state_words(D);
+  constexpr int kPer = D / 64;  // channels of a lane
   const float* states = l.states + (int64_t)blockIdx.x * l.n_seg * kWords;
-  float mm = -INFINITY, zz = 0.f, o = 0.f;
-  for (int i = 0; i < n_seg; ++i) mm = fmaxf(mm, states[(size_t)i * kWords + D]);
-#pragma unroll 4
-  for (int i = 0; i < n_seg; ++i) {
-    const float mi = states[(size_t)i * kWords + D];
-    const float f = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - mm);
-    zz += f;
-    o += states[(size_t)i * kWords + threadIdx.x] * f;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float m[2], f[2], mm = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    m[k] = lane + 64 * k < n_seg ? states[(size_t)(lane + 64 * k) * kWords + D] : -INFINITY;
+    mm = fmaxf(mm, m[k]);
   }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor(mm, d));
+#pragma unroll
+  for (int k = 0; k < 2; ++k) f[k] = m[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - mm);
+  const float zz = wave_sum(f[0] + f[1]);
+  float o[kPer] = {};
+  for (int i = wave; i < n_seg; i += 16)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {  // (four loads on their way)
+      const int at = min(i + 4 * j, n_seg - 1);
+      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(at < 64 ? f[0] : f[1]), at & 63));
+#pragma unroll
+      for (int c = 0; c < kPer; ++c)
+        o[c] += states[(size_t)at * kWords + lane * kPer + c] * (i + 4 * j < n_seg ? fi : 0.f);
+    }
+  __shared__ float sm_o[4][D];
+#pragma unroll
+  for (int c = 0; c < kPer; ++c) sm_o[wave][lane * kPer + c] = o[c];
+  __syncthreads();
   const int token = t - rq.state_off;
-  p.out.data[(int64_t)(rq.row_off + token) * p.out.token_stride + (int64_t)h * p.out.head_stride + threadIdx.x] =
-      (_Float16)(zz == 0.f ? 0.f : o / zz);
-  const int i = p.window - rq.n_new + token;
-  if (p.lse && i >= 0 && threadIdx.x == 0)
-    p.lse[(int64_t)rq.table_row * p.lse_stride + (int64_t)h * p.window + i] =
-        zz == 0.f ? -INFINITY : (mm + __builtin_amdgcn_logf(zz)) * kLn2;
+  if (threadIdx.x < D) {
+    const float sum = sm_o[0][threadIdx.x] + sm_o[1][threadIdx.x] + sm_o[2][threadIdx.x] + sm_o[3][threadIdx.x];
+    row_of(p.out, rq, token, h)[threadIdx.x] = (_Float16)(zz == 0.f ? 0.f : sum / zz);
+  }
+  if (threadIdx.x == 0) write_lse(p, rq, token, h, zz == 0.f ? -INFINITY : mm + __builtin_amdgcn_logf(zz));
 }
 
-// two tiles of many rows; four states of few (which need more than their keys)
-constexpr int lds_bytes(int head_dim) { return std::max(2 * 2 * 64 * head_dim * 2, 4 * 32 * head_dim * 4); }
+// two tiles of many rows, or four states of few; as much as the keys of few, but for the exponents
+constexpr int lds_bytes(int head_dim, int source) {
+  return 2 * 2 * 64 * head_dim * 2 + (source == ATTN_E4M3 ? 4 * 2 * 2 * kExponentBytes : 0);
+}
+static_assert(2 * 2 * 64 * 2 == 4 * 32 * 4 && 4 * 2 * 32 * 2 == 4 * 32 * 4, "per channel");
 
 template <int D, int SRC, bool kSplit, typename Reqs>
 void launch_kernel(const AttnParams& p, const Reqs& reqs, hipStream_t s) {
   const unsigned grid = (unsigned)(p.launch[0].n_units + p.launch[1].n_units) * p.n_heads;
-  attention_kernel<D, SRC, kSplit, Reqs><<<grid, 256, lds_bytes(D), s>>>(p, reqs);
+  attention_kernel<D, SRC, kSplit, Reqs><<<grid, 256, lds_bytes(D, SRC), s>>>(p, reqs);
 }
 
 template <int D, int SRC, typename Reqs>
@@ -906,7 +911,7 @@ void launch_source(const AttnParams& p, const Reqs& reqs, hipStream_t s) {
       launch_kernel<D, SRC, true>(p, reqs, s);
       for (const AttnLaunchView& l : p.launch)
         if (l.n_seg > 1)
-          attention_merge_kernel<D, Reqs><<<(unsigned)l.state_rows * p.n_heads * p.group, D, 0, s>>>(p, l, reqs);
+          attention_merge_kernel<D, Reqs><<<(unsigned)l.state_rows * p.n_heads * p.group, 256, 0, s>>>(p, l, reqs);
       return;
     }
   }
@@ -927,7 +932,7 @@ template <typename Reqs>
 hipError_t allow_lds_with() {  // (with the static words more than 64 KB)
   hipError_t e = hipSuccess;
   auto allow = [&](const void* kernel) {
-    if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(128));
+    if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(128, ATTN_E4M3));
   };
   allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_ROWS, false, Reqs>));
   allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_F16, false, Reqs>));
@@ -947,7 +952,7 @@ hipError_t attention_one_time_setup() {
 hipError_t launch_attention(const AttnParams& p, const ChunkReqs& inline_reqs, hipStream_t s) {
   if (p.head_dim != 64 && p.head_dim != 128) return hipErrorInvalidValue;
   for (const AttnLaunchView& l : p.launch)
-    if (l.n_seg < 1 || l.seg_blocks < 1 || (p.source == ATTN_ROWS && l.n_seg > 1)) return hipErrorInvalidValue;
+    if (l.n_seg < 1 || l.n_seg > kMaxHeadSegments || l.seg_blocks < 1 || (p.source == ATTN_ROWS && l.n_seg > 1)) return hipErrorInvalidValue;
   if (p.launch[0].n_units + p.launch[1].n_units == 0) return hipSuccess;
   auto with = [&](const auto& reqs) {
     if (p.head_dim == 128)

@@ -34,16 +34,8 @@ hipError_t launch_extend(const ExtendParams& p, const ExtendReqs& inline_reqs, h
 
 // the request that unit u belongs to (units ascend with the requests)
 template <typename Reqs>
-__device__ __forceinline__ int request_of(const Reqs& reqs, int n_req, int u) {
-  int lo = 0, hi = n_req - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (reqs.req[mid].unit_start <= u)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
-  return lo;
+__device__ __forceinline__ int request_of_unit(const Reqs& reqs, int n_req, int u) {
+  return request_of(0, n_req, u, [&](int i) { return reqs.req[i].unit_start; });
 }
 
 template <typename F>
@@ -62,7 +54,7 @@ static void with_chunk_reqs(const ChunkReq* on_device, const ChunkReqs& inline_r
 template <int D, bool kE4M3, typename Reqs>
 __global__ __launch_bounds__(256) void store_chunk_kernel(StoreParams p, Reqs reqs) {
   constexpr int PPR = D / 8;
-  const ChunkReq rq = reqs.req[request_of(reqs, p.n_req, blockIdx.x)];
+  const ChunkReq rq = reqs.req[request_of_unit(reqs, p.n_req, blockIdx.x)];
   const int tok = rq.seq_len - rq.n_new + ((int)blockIdx.x - rq.row_off);
   const int blk = clamp_block(p.block_tables[(size_t)rq.table_row * p.max_blocks + (tok >> 4)], p.n_blocks);
   const int slot = tok & 15;
@@ -110,7 +102,7 @@ __global__ __launch_bounds__(256) void quantise_kernel(QuantiseParams p, Reqs re
   constexpr int PPR = D / 8;
   const int layer = blockIdx.x / p.n_units;
   const int unit = blockIdx.x - layer * p.n_units;
-  const ChunkReq rq = reqs.req[request_of(reqs, p.n_req, unit)];
+  const ChunkReq rq = reqs.req[request_of_unit(reqs, p.n_req, unit)];
   const int b = unit - rq.unit_start;
   const int from = clamp_block(p.src_tables[(size_t)rq.table_row * p.src_max_blocks + b], p.src_blocks);
   const int to = clamp_block(p.dst_tables[(size_t)rq.table_row * p.dst_max_blocks + b], p.dst_blocks);

@@ -90,18 +90,33 @@ int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, in
     auto tiles = [&](const ChunkReq& q) { return ((int64_t)q.n_new * group + tile - 1) / tile; };
     const int longest = blocks_for(l.reqs.front().seq_len);
     l.seg_blocks = std::max(longest, 1);
-    int64_t total = 0;  // blocks that workgroups walk, all heads
+    int64_t total = 0, units = 0;  // blocks that workgroups walk, workgroups, all heads
     for (const ChunkReq& q : l.reqs) {
+      units += tiles(q) * pool.n_heads;
       total += tiles(q) * blocks_for(q.seq_len) * pool.n_heads;
       l.state_rows += q.n_new;
     }
-    // As the decode attention (plan_decode_segments): segments of an eighth of a CU's share,
-    // at least 16 blocks, if that is at most half of the longest head.
+    // Keys are split where workgroups are few or uneven, at least in two.  Two workgroups fit a
+    // CU.  Many rows: as many segments as make that many workgroups, of 32 blocks and more
+    // (rows x tokens cached; us, 8 heads of K and V, 4 query heads each):
+    //   whole / split     64 x 16000 (two)  256 x 20000   150 x 5000-9000 (three)
+    //                     92 / 60           204 / 109     61 / 40
+    // Few rows: segments of half of a CU's share (a CU whose neighbours are done draws more
+    // than that), of 32 blocks and more: each costs the merge as much as reading one or two.
+    //   a share's                      whole  half  third  quarter, at least 16  32  64
+    //   64 caches of 500-4000            97    102    102    105
+    //   16 of 1000-9000, 4 heads         44     36     41     38
+    //   24 of 3000-20000                209    204    188    203
+    //   the same in 8 bits              135    129    118    120
+    //   1 of 30000                                                            34  28  28
+    //   1 of 8000                                                             15  15  18
     const int64_t n_q_heads = (int64_t)group * pool.n_heads;
+    const int64_t slots = 2 * (int64_t)std::max(n_cu, 1);
     const int64_t room = states_left / (l.state_rows * n_q_heads);  // segments of a row
     if (room >= 2) {
-      const int64_t eighth = total / (8 * (int64_t)std::max(n_cu, 1));
-      const int64_t seg = std::max<int64_t>({eighth, 16, (longest + room - 1) / room});
+      const int64_t wanted = s == 0 ? (slots + units - 1) / units : 1;
+      const int64_t seg = std::max<int64_t>({s == 0 ? (longest + wanted - 1) / wanted : total / slots, kPlanMinSegment,
+                                             (longest + room - 1) / room});
       if (2 * seg <= longest) {
         l.seg_blocks = (int)seg;
         l.n_seg = decode_segments(longest, l.seg_blocks);

@@ -36,6 +36,9 @@ void plan_store_units(ChunkPlan* plan);
 static constexpr int kAttnKinds = 2;
 static constexpr int kTallRows = 128;  // rows (new tokens x query heads of a group) of a workgroup
 static constexpr int kFlatRows = 32;
+static constexpr int kPlanMinSegment = 32;  // blocks
+// Most states of a call's split rows, what the pool's buffer holds (42 MB at 128 channels).
+static constexpr int kMaxAttnStates = 65536;
 struct AttnLaunch {
   std::vector<ChunkReq> reqs;  // longest first; unit = (row tile, segment), heads not counted
   int64_t n_units = 0;

@@ -202,6 +202,24 @@ __device__ __forceinline__ void stream_tiles(int n, Load load, Use use) {
   use(i, a);
   if (two) use(i + 1, b);
 }
+// The last of n requests from `begin` on whose key (ascending, the first one at most u) is u
+// or less: a wavefront asks for 64 of them at a time, so that up to 64 requests are one load's
+// latency and 4096 two.  (As arguments they are far away: see fc_attention.hip.)
+template <typename Key>
+__device__ __forceinline__ int request_of(int begin, int n, int u, Key key) {
+  const int lane = threadIdx.x & 63;
+  int lo = begin;
+  const int end = begin + n;
+  while (n > 1) {
+    const int step = (n + 63) >> 6;
+    const int at = lo + lane * step;
+    const uint64_t below = __ballot(at < end && key(min(at, end - 1)) <= u);
+    lo += (__popcll(below) - 1) * step;
+    n = min(step, end - lo);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
 // how many of n tiles a wavefront has, every `step`-th from its own on
 __device__ __forceinline__ int own_tiles(int n, int wave, int step) { return (n - wave + step - 1) / step; }
 
