@@ -515,8 +515,9 @@ int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_b
  *               after the other in batch order ("packed"): T = sum of n_new rows.
  * fc_rows       packed rows: channel c of head h of row t is element
  *               t * token_stride + h * head_stride + c of fp16 numbers at data;
- *               data 16-byte aligned, strides multiples of 8, not negative (rows of q, k and v may
- *               be parts of one projection's rows).
+ *               data 16-byte aligned, strides multiples of 8, not
+ *               negative, at most FC_MAX_TOKEN_STRIDE and FC_MAX_HEAD_STRIDE (rows of q, k and
+ *               v may be parts of one projection's rows).
  *
  * fc_extend_batch: request r gets the blocks that n_new_r more tokens need,
  * ceil((L_r + n_new_r)/16) - ceil(L_r/16) of them, popped in batch order, the
@@ -561,6 +562,8 @@ int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_b
  * a buffer is needed.
  */
 #define FC_MAX_GROUP 64 /* most query heads that share a head of K and V */
+#define FC_MAX_TOKEN_STRIDE (1 << 24)
+#define FC_MAX_HEAD_STRIDE 0x7fffffff
 typedef struct fc_rows {
   void* data;           /* dev */
   int64_t token_stride; /* in elements */

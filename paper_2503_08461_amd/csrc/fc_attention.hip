@@ -161,18 +161,154 @@ struct Rows32 {
   floatx16 o[DT];
   float m, z;  // running maximum (log2 units), and sum of this lane's keys
 
-  template <bool kPairedSlabs>
-  __device__ __forceinline__ void start(const _Float16* from) {  // the lane's row
-    const int half = (threadIdx.x & 63) >> 5;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
-      q[kk] = load_half8(from + (kPairedSlabs ? 16 * (2 * (kk / 2) + half) + 8 * (kk % 2) : kk * 16 + half * 8));
+  __device__ __forceinline__ void start() {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
     m = -INFINITY;
     z = 0.f;
+  }
+  // The queries, through `room` in LDS (32 rows of the wavefront's own): read from memory and
+  // written there row by row, D / 8 lanes a row.  (A lane's own row straight from memory is 64
+  // addresses in 64 lines for each of its loads, which took four wavefronts 2000 cycles of a
+  // workgroup's 40000 for a prompt of 1024.)  from(row): where the wavefront's row is.
+  template <typename From>
+  __device__ __forceinline__ void request_queries(From from) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < KK; ++i) q[i] = load_half8(from((i * 64 + lane) / (D / 8)) + (lane % (D / 8)) * 8);
+  }
+  template <bool kPairedSlabs>
+  __device__ __forceinline__ void take_queries(half8* room) {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < KK; ++i) room[k_chunk<D>((i * 64 + lane) / (D / 8), lane % (D / 8))] = q[i];
+    wave_lds_barrier();
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      q[kk] = room[k_chunk<D>(lane & 31, kPairedSlabs ? 2 * (2 * (kk / 2) + half) + kk % 2 : 2 * kk + half)];
+    wave_lds_barrier();
+  }
+  // The lane's row times f, as fp16 rows in LDS (32 of the wavefront's own), then row by row to
+  // memory.  to(row): where the wavefront's row goes, NULL if nowhere.
+  template <typename To>
+  __device__ __forceinline__ void write_result(half8* room, float f, To to) const {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        half4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (_Float16)(o[dt][4 * j + e] * f);
+        reinterpret_cast<half4*>(room + k_chunk<D>(lane & 31, dt * 4 + j))[half] = x;
+      }
+    wave_lds_barrier();
+    half8 x[KK];
+#pragma unroll
+    for (int i = 0; i < KK; ++i) x[i] = room[k_chunk<D>((i * 64 + lane) / (D / 8), lane % (D / 8))];
+#pragma unroll
+    for (int i = 0; i < KK; ++i) {
+      _Float16* row = to((i * 64 + lane) / (D / 8));
+      if (row) store_half8(row + (lane % (D / 8)) * 8, x[i]);
+    }
+  }
+
+  // m follows the maximum when it falls more than kSlack behind: the numerators stay below
+  // 2^kSlack, which fp16 and the sums hold as exactly as those below 1.  top: of this lane's
+  // logits; returns what numerators are taken relative to.
+  __device__ __forceinline__ float follow(float top, float scale_log2e) {
+    const float mn = fmaxf(m, other_half_max(top) * scale_log2e);
+    if (__any(mn > m + kSlack)) {
+      // (nothing seen so far: nothing to rescale, but what was not a number, or infinite, stays)
+      const float a = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      z *= a;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] *= a;
+      m = mn;
+    }
+    return m == -INFINITY ? 0.f : m;
+  }
+
+  // 64 keys that every row sees, in the tile at `lds`: attend() with its instructions in this
+  // order.  Operands are read four products ahead, and the numerators of the next 16 keys are
+  // made between the products of these.  (Left to itself the compiler reads an operand, waits
+  // for it and multiplies, or does not, as what stands around the loop changes.)
+  struct Offsets {  // of the lane's operands in a tile, in bytes
+    int k[KK], v[DT];
+  };
+  __device__ __forceinline__ static Offsets offsets() {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    Offsets at;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) at.k[kk] = k_chunk<D>(lane & 31, 2 * kk + half) * 16;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      at.v[dt] = v_chunk<D>(half * 4 + ((lane & 15) >> 2), dt * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) * 16 +
+                 (lane & 1) * 8 + 64 * D * 2;
+    return at;
+  }
+  template <int kTileAt>
+  __device__ __forceinline__ void attend_full(const half8* sm, const Offsets& at, float scale_log2e) {
+    constexpr int kAhead = 4, kRow = D * 2;
+    const char* lds = reinterpret_cast<const char*>(sm) + kTileAt;
+    auto k_read = [&](int i) {
+      return *reinterpret_cast<const half8*>(lds + at.k[i % KK] + (i / KK) * 32 * kRow);
+    };
+    auto v_read = [&](int i) {  // product i: 16 keys i / DT, channels 32 (i % DT) and on
+      const _Float16* from = reinterpret_cast<const _Float16*>(lds + at.v[i % DT] + (i / DT) * 16 * kRow);
+      const fp16x4 lo = read_columns(from), hi = read_columns(from + 8 * D);
+      return half8{(_Float16)lo[0], (_Float16)lo[1], (_Float16)lo[2], (_Float16)lo[3],
+                   (_Float16)hi[0], (_Float16)hi[1], (_Float16)hi[2], (_Float16)hi[3]};
+    };
+    half8 a[kAhead + 1];
+    floatx16 s[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) a[i] = k_read(i);
+    __builtin_amdgcn_sched_barrier(0);
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2 * KK; ++i) {
+      if (i + kAhead < 2 * KK) a[(i + kAhead) % (kAhead + 1)] = k_read(i + kAhead);
+      s[i / KK] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i % (kAhead + 1)], q[i % KK], s[i / KK], 0, 0, 0);
+      if (i >= 2 * KK - 2) {  // (the first half is there by now)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) top = fmaxf(top, s[0][(i - (2 * KK - 2)) * 8 + r]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) a[i] = v_read(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[1][r]);
+    const float base = follow(top, scale_log2e);
+    half8 p[2];
+    auto numerator = [&](int i) {  // of the lane's key i of 32
+      const float w = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], scale_log2e, -base));
+      z += w;
+      p[(i / 8) % 2][i % 8] = (_Float16)w;
+    };
+#pragma unroll
+    for (int i = 0; i < 8; ++i) numerator(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 4 * DT; ++i) {
+      if (i + kAhead < 4 * DT) a[(i + kAhead) % (kAhead + 1)] = v_read(i + kAhead);
+      o[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i % (kAhead + 1)], p[(i / DT) % 2], o[i % DT], 0, 0, 0);
+      if (i < 3 * DT) {
+#pragma unroll
+        for (int j = 0; j < 8 / DT; ++j) numerator(8 * (i / DT + 1) + (i % DT) * (8 / DT) + j);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 
   // kSub * 32 keys, key0: the first one's number.  kMasked: the lane's row sees keys up to
@@ -203,20 +339,7 @@ struct Rows32 {
         }
         top = fmaxf(top, s[u][r]);
       }
-    // m follows the maximum when it falls more than kSlack behind: the numerators stay below
-    // 2^kSlack, which fp16 and the sums hold as exactly as those below 1.
-    const float mn = fmaxf(m, other_half_max(top) * scale_log2e);
-    if (__any(mn > m + kSlack)) {
-      // (nothing seen so far: nothing to rescale, but what was not a number, or infinite, stays)
-      const float a = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-      z *= a;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[dt][r] *= a;
-      m = mn;
-    }
-    const float base = m == -INFINITY ? 0.f : m;
+    const float base = follow(top, scale_log2e);
     before_v();
     // Where some row does not see some key, 0 * inf and 0 * NaN must not reach it: channels of V
     // that are no finite numbers are added where their key is seen, and are zeros in the product.
@@ -261,6 +384,11 @@ struct Rows32 {
   }
 };
 
+// row / group, by the inverse 2^31 / group, rounded up (exact for rows below 2^25)
+__device__ __forceinline__ int token_of(const AttnParams& p, int row) {
+  return (int)__umulhi((uint32_t)row << 1, p.group_inverse);
+}
+
 // Where a workgroup is in its request (tile: row tile of kRows) and which keys it walks.
 struct Place {
   ChunkReq rq;
@@ -278,7 +406,7 @@ __device__ __forceinline__ Place place_of(const AttnParams& p, const Reqs& reqs,
   // (the last rows see most keys: first)
   w.tile = (w.n_rows + kRows - 1) / kRows - 1 - (kSplit ? at / w.n_seg : at);
   w.key_begin = 0;
-  w.key_end = w.rq.seq_len - w.rq.n_new + (min((w.tile + 1) * kRows, w.n_rows) - 1) / p.group + 1;
+  w.key_end = w.rq.seq_len - w.rq.n_new + token_of(p, min((w.tile + 1) * kRows, w.n_rows) - 1) + 1;
   if (kSplit) {
     w.key_begin = 16 * decode_segment_begin(w.nb, w.n_seg, w.seg);
     w.key_end = min(w.key_end, 16 * decode_segment_begin(w.nb, w.n_seg, w.seg + 1));
@@ -288,20 +416,31 @@ __device__ __forceinline__ Place place_of(const AttnParams& p, const Reqs& reqs,
 
 // A lane's row: its token and query head (rows behind the last one: the last one's).
 struct LaneRow {
-  int token, q_head;
+  int token, in_group;
   bool real;
 };
-__device__ __forceinline__ LaneRow lane_row(const AttnParams& p, int row, int n_rows, int head) {
+__device__ __forceinline__ LaneRow lane_row(const AttnParams& p, int row, int n_rows) {
   LaneRow r;
   r.real = row < n_rows;
   row = min(row, n_rows - 1);
-  r.token = row / p.group;
-  r.q_head = head * p.group + row - r.token * p.group;
+  r.token = token_of(p, row);
+  r.in_group = row - r.token * p.group;
   return r;
 }
 __device__ __forceinline__ _Float16* row_of(const RowsView& v, const ChunkReq& rq, int token, int head) {
   return v.data + (int64_t)(rq.row_off + token) * v.token_stride + (int64_t)head * v.head_stride;
 }
+// Rows of a request and of the query heads that share one head of K and V: two products of 32
+// bits a row (the strides are limited to that).
+struct GroupRows {
+  _Float16* base;
+  uint32_t token_stride, head_stride;
+  __device__ __forceinline__ GroupRows(const RowsView& v, const ChunkReq& rq, const AttnParams& p, int head)
+      : base(row_of(v, rq, 0, head * p.group)), token_stride((uint32_t)v.token_stride), head_stride((uint32_t)v.head_stride) {}
+  __device__ __forceinline__ _Float16* at(const LaneRow& r) const {
+    return base + ((uint64_t)(uint32_t)r.token * token_stride + (uint64_t)(uint32_t)r.in_group * head_stride);
+  }
+};
 template <int D>
 __device__ __forceinline__ float* state_of(const AttnParams& p, const AttnLaunchView& l, const ChunkReq& rq, int token,
                                            int q_head, int seg) {
@@ -516,15 +655,16 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int first_key = w.rq.seq_len - w.rq.n_new;  // what token 0 sees last
   const int row0 = w.tile * kTallRows + wave * 32;
-  const LaneRow me = lane_row(p, row0 + (lane & 31), w.n_rows, head);
+  const LaneRow me = lane_row(p, row0 + (lane & 31), w.n_rows);
+  const int q_head = head * p.group + me.in_group;
   const int last_key = min(first_key + me.token, w.key_end - 1);  // (a segment may end inside a tile)
-  const int wave_last = min(first_key + min(row0 + 31, w.n_rows - 1) / p.group, w.key_end - 1);
+  const int wave_last = min(first_key + token_of(p, min(row0 + 31, w.n_rows - 1)), w.key_end - 1);
   const int n_tiles = w.key_end > w.key_begin ? (w.key_end - w.key_begin + kKeys - 1) / kKeys : 0;
   // tiles that every row of the workgroup sees whole
-  const int n_full = max(min(first_key + w.tile * kTallRows / p.group, w.key_end - 1) + 1 - w.key_begin, 0) / kKeys;
+  const int n_full = max(min(first_key + token_of(p, w.tile * kTallRows), w.key_end - 1) + 1 - w.key_begin, 0) / kKeys;
 
   Rows32<D> rows;
-  rows.template start<false>(row_of(p.q, w.rq, me.token, me.q_head));
+  rows.start();
 
   const int32_t* table = SRC == ATTN_ROWS ? nullptr : p.block_tables + (size_t)w.rq.table_row * p.max_blocks;
   const int k_stride = SRC == ATTN_ROWS ? (int)p.k.token_stride : D, v_stride = SRC == ATTN_ROWS ? (int)p.v.token_stride : D;
@@ -564,33 +704,47 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
     half8* to = sm + (t & 1) * 2 * kTile;
     b8.put(to, to + kTile, wave * 16);
   };
-  auto step = [&](int t, auto masked_) {
-    constexpr bool kMasked = decltype(masked_)::value;
+  // tile t, the next one on its way: work(tile's place in LDS)
+  auto step = [&](int t, auto work) {
     if constexpr (SRC != ATTN_E4M3) wait_loads<0>();
     lds_barrier();  // tile t is there, the one before has been read
     if (t + 1 < n_tiles) request(t + 1);
-    const half8* sm_k = sm + (t & 1) * 2 * kTile;
-    const int key0 = w.key_begin + t * kKeys;
-    if (!kMasked || key0 <= wave_last)  // uniform over the wavefront: else none of its rows sees these
-      rows.template attend<2, kMasked>(F16Keys<D>{sm_k, sm_k + kTile, 0}, key0, last_key, p.scale_log2e, [] {}, [] {});
+    work();
     if constexpr (SRC == ATTN_E4M3) {
       if (t + 1 < n_tiles) put8(t + 1);
     }
   };
+  const typename Rows32<D>::Offsets operands = Rows32<D>::offsets();
+  auto even = [&] { rows.template attend_full<0>(sm, operands, p.scale_log2e); };
+  auto odd = [&] { rows.template attend_full<2 * kTile * 16>(sm, operands, p.scale_log2e); };
   if (n_tiles > 0) {
+    const GroupRows from(p.q, w.rq, p, head);
+    rows.request_queries([&](int r) { return from.at(lane_row(p, row0 + r, w.n_rows)); });
     request(0);
     if constexpr (SRC == ATTN_E4M3) put8(0);
+    // (the second tile's room is free until the first barrier)
+    rows.template take_queries<false>(sm + 2 * kTile + wave * 32 * D / 8);
   }
   int t = 0;
-  for (; t < n_full; ++t) step(t, std::false_type());
-  for (; t < n_tiles; ++t) step(t, std::true_type());
+  for (; t + 1 < n_full; t += 2) {
+    step(t, even);
+    step(t + 1, odd);
+  }
+  if (t < n_full) step(t++, even);
+  for (; t < n_tiles; ++t)
+    step(t, [&] {
+      const half8* sm_k = sm + (t & 1) * 2 * kTile;
+      const int key0 = w.key_begin + t * kKeys;
+      if (key0 <= wave_last)  // uniform over the wavefront: else none of its rows sees these
+        rows.template attend<2, true>(F16Keys<D>{sm_k, sm_k + kTile, 0}, key0, last_key, p.scale_log2e, [] {}, [] {});
+    });
 
   const float z = other_half_sum(rows.z);
   const float inv = z == 0.f ? 0.f : 1.f / z;
   const float log2_sum = z == 0.f ? -INFINITY : rows.m + __builtin_amdgcn_logf(z);
-  if (!me.real) return;
   if (kSplit && w.n_seg > 1) {  // a segment's state: the normalised result and the log2 of the sum
-    float* state = state_of<D>(p, l, w.rq, me.token, me.q_head, w.seg);
+    if (!me.real) return;
+    float* state = state_of<D>(p, l, w.rq, me.token, q_head, w.seg);
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -603,17 +757,13 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
     if (half == 0) state[D] = log2_sum;
     return;
   }
-  _Float16* out = row_of(p.out, w.rq, me.token, me.q_head);
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      half4 x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = (_Float16)(rows.o[dt][4 * j + e] * inv);
-      *reinterpret_cast<half4*>(out + dt * 32 + j * 8 + half * 4) = x;
-    }
-  if (half == 0) write_lse(p, w.rq, me.token, me.q_head, log2_sum);
+  lds_barrier();  // (the last tile has been read)
+  const GroupRows to(p.out, w.rq, p, head);
+  rows.write_result(sm + wave * 32 * D / 8, inv, [&](int r) -> _Float16* {
+    const LaneRow it = lane_row(p, row0 + r, w.n_rows);
+    return it.real ? to.at(it) : nullptr;
+  });
+  if (half == 0 && me.real) write_lse(p, w.rq, me.token, q_head, log2_sum);
 }
 
 // ---------------------------------------------------------------------------
@@ -643,16 +793,19 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int first_key = w.rq.seq_len - w.rq.n_new;
   const int row0 = w.tile * kFlatRows;
-  const LaneRow me = lane_row(p, row0 + (lane & 31), w.n_rows, head);
+  const LaneRow me = lane_row(p, row0 + (lane & 31), w.n_rows);
+  const int q_head = head * p.group + me.in_group;
   const int last_key = min(first_key + me.token, w.key_end - 1);
-  const int first_seen = min(first_key + row0 / p.group, w.key_end - 1);  // all rows see keys up to this one
+  const int first_seen = min(first_key + token_of(p, row0), w.key_end - 1);  // all rows see keys up to this one
   const int n_tiles = w.key_end > w.key_begin ? (w.key_end - w.key_begin + kKeys - 1) / kKeys : 0;
   const int mine = own_tiles(n_tiles, wave, 4);
   // tiles that every row sees whole come first
   const int full = min(mine, own_tiles(max(first_seen + 1 - w.key_begin, 0) / kKeys, wave, 4));
 
   Rows32<D> rows;
-  rows.template start<SRC == ATTN_E4M3>(row_of(p.q, w.rq, me.token, me.q_head));
+  rows.start();
+  const GroupRows from(p.q, w.rq, p, head), to(p.out, w.rq, p, head);
+  rows.request_queries([&](int r) { return from.at(lane_row(p, row0 + r, w.n_rows)); });
 
   const int32_t* table = SRC == ATTN_ROWS ? nullptr : p.block_tables + (size_t)w.rq.table_row * p.max_blocks;
   half8* sm_k = sm + wave * 2 * kStages * kTile;
@@ -699,6 +852,10 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
         lds_reads_done();  // (K's loads stay ahead of V's, as the waits count on)
         request_v(i);
         lds_reads_done();
+        if (i == 0) {  // through the second tile's room
+          rows.template take_queries<true>(sm_k + 2 * kTile);
+          lds_reads_done();
+        }
       }
     }
     auto step = [&](int i, auto masked_) {
@@ -751,6 +908,8 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
       look_up(0);
       request_k(0);
       lds_reads_done();  // (K's loads stay ahead of V's, as the waits count on)
+      rows.template take_queries<false>(sm_k + kTile);  // through V's room
+      lds_reads_done();
       request_v(0);
     }
     auto step = [&](int i, auto masked_) {
@@ -805,25 +964,25 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
     }
   if (wave == 0 && half == 0 && me.real) {
     if (kSplit && w.n_seg > 1)
-      state_of<D>(p, l, w.rq, me.token, me.q_head, w.seg)[D] = log2_sum;
+      state_of<D>(p, l, w.rq, me.token, q_head, w.seg)[D] = log2_sum;
     else
-      write_lse(p, w.rq, me.token, me.q_head, log2_sum);
+      write_lse(p, w.rq, me.token, q_head, log2_sum);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < 32 * kQuads; i += 256) {
     const int r = i / kQuads, c = i % kQuads;
-    const LaneRow it = lane_row(p, row0 + r, w.n_rows, head);
+    const LaneRow it = lane_row(p, row0 + r, w.n_rows);
     if (!it.real) break;
     floatx4 x = sm_o[r * kQuads + (c ^ (r & (kQuads - 1)))];
 #pragma unroll
     for (int k = 1; k < 4; ++k) x += sm_o[(k * 32 + r) * kQuads + (c ^ (r & (kQuads - 1)))];
     if (kSplit && w.n_seg > 1) {
-      *reinterpret_cast<floatx4*>(state_of<D>(p, l, w.rq, it.token, it.q_head, w.seg) + c * 4) = x;
+      *reinterpret_cast<floatx4*>(state_of<D>(p, l, w.rq, it.token, head * p.group + it.in_group, w.seg) + c * 4) = x;
     } else {
       half4 y;
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = (_Float16)x[e];
-      *reinterpret_cast<half4*>(row_of(p.out, w.rq, it.token, it.q_head) + c * 4) = y;
+      *reinterpret_cast<half4*>(to.at(it) + c * 4) = y;
     }
   }
 }

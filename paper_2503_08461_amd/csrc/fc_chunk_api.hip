@@ -47,8 +47,8 @@ int check_rows(const fc_rows* rows, const char* name, int64_t n_rows, int n_head
   if (reinterpret_cast<uintptr_t>(rows->data) & 15) return fail(FC_EINVAL, "%s must be 16-byte aligned", name);
   const int64_t t = rows->token_stride, h = rows->head_stride;
   if ((t | h) & 7 || t < 0 || h < 0) return fail(FC_EINVAL, "strides of %s must be multiples of 8, 0 or more", name);
-  // (16 rows span less than 2^31 bytes, no product with rows or heads passes 63 bits)
-  if (t > (int64_t)1 << 24 || h > (int64_t)1 << 46) return fail(FC_EINVAL, "strides of %s are too large", name);
+  // (16 rows span less than 2^31 bytes; products with numbers of tokens and heads are of 32 bits each)
+  if (t > FC_MAX_TOKEN_STRIDE || h > FC_MAX_HEAD_STRIDE) return fail(FC_EINVAL, "strides of %s are too large", name);
   if (written && !(h >= head_dim && t >= (n_heads - 1) * h + head_dim) && !(t >= head_dim && h >= (n_rows - 1) * t + head_dim))
     return fail(FC_EINVAL, "rows of %s overlap", name);
   return FC_OK;
@@ -103,6 +103,7 @@ int attention(fc_pool* p, int layer, const int32_t* dev_block_tables, int max_bl
   ap.n_blocks = p->n_blocks;
   ap.n_heads = p->n_heads;
   ap.group = n_q_heads / p->n_heads;
+  ap.group_inverse = (uint32_t)((((uint64_t)1 << 31) + ap.group - 1) / ap.group);
   ap.head_dim = p->head_dim;
   ap.block_tables = dev_block_tables;
   ap.max_blocks = max_blocks;

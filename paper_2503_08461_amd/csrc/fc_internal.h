@@ -132,6 +132,7 @@ struct AttnParams {
   const void* kv;  // the layer's blocks
   int32_t source;  // ATTN_*
   int32_t n_blocks, n_heads, group, head_dim;
+  uint32_t group_inverse;  // 2^31 / group, rounded up
   const int32_t* block_tables;
   int32_t max_blocks;
   const ChunkReq* reqs;  // NULL: in the ChunkReqs argument
