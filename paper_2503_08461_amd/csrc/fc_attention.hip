@@ -62,13 +62,15 @@ __device__ __forceinline__ float other_half_sum(float v) {
   return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
-// Nonzero where one of the eight numbers is infinite or not a number (exponent bits all set).
-__device__ __forceinline__ uint32_t nonfinite(half8 x) {
+// The largest magnitudes of two interleaved series of numbers, as bits: infinite or not a
+// number from 0x7c00 on.
+typedef uint16_t ushort2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ ushort2v largest(half8 x, ushort2v so_far) {
   const uint4v w = __builtin_bit_cast(uint4v, x);
-  uint32_t t = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) t |= (w[i] & 0x7c007c00u) + 0x04000400u;
-  return t & 0x80008000u;
+  for (int i = 0; i < 4; ++i)
+    so_far = __builtin_elementwise_max(so_far, __builtin_bit_cast(ushort2v, w[i] & 0x7fff7fffu));
+  return so_far;
 }
 __device__ __forceinline__ half8 finite_only(half8 x) {
 #pragma unroll
@@ -136,10 +138,10 @@ struct F16Keys {
   // whether V holds anything but finite numbers
   template <int kSub>
   __device__ __forceinline__ bool dirty() const {
-    uint32_t found = 0;
+    ushort2v most = {0, 0};
 #pragma unroll
-    for (int i = 0; i < kSub * 32 * D / 8 / 64; ++i) found |= nonfinite(v[at * (D / 8) + i * 64 + (threadIdx.x & 63)]);
-    return __any(found != 0);
+    for (int i = 0; i < kSub * 32 * D / 8 / 64; ++i) most = largest(v[at * (D / 8) + i * 64 + (threadIdx.x & 63)], most);
+    return __any(max(most[0], most[1]) >= 0x7c00);
   }
   // four channels of one key, those that are no finite numbers (0 for the others)
   __device__ __forceinline__ floatx4 not_finite(int key, int channel) const {
@@ -735,8 +737,10 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
     step(t, [&] {
       const half8* sm_k = sm + (t & 1) * 2 * kTile;
       const int key0 = w.key_begin + t * kKeys;
-      if (key0 <= wave_last)  // uniform over the wavefront: else none of its rows sees these
-        rows.template attend<2, true>(F16Keys<D>{sm_k, sm_k + kTile, 0}, key0, last_key, p.scale_log2e, [] {}, [] {});
+      // 32 keys at a time, those that none of the wavefront's rows sees left out
+#pragma unroll 1
+      for (int at = 0; at < kKeys && key0 + at <= wave_last; at += 32)
+        rows.template attend<1, true>(F16Keys<D>{sm_k, sm_k + kTile, at}, key0 + at, last_key, p.scale_log2e, [] {}, [] {});
     });
 
   const float z = other_half_sum(rows.z);
