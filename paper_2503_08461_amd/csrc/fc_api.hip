@@ -1069,8 +1069,12 @@ int decode_attention_impl(fc_pool* p, const int32_t* dev_block_tables, int max_b
   dp.q = static_cast<const _Float16*>(dev_q);
   dp.out = dev_out;
   dp.kept = dev_kept;
-  plan_decode_segments(pool_view(p), p->n_cu, dev_kept != nullptr, &plan,
-                       p->decode_partial ? kMaxDecodeSegments : 0);
+  const int max_segments = p->decode_partial ? kMaxDecodeSegments : 0;
+  if (dp.e4m3)
+    plan_decode_segments_e4m3(pool_view(p), p->n_cu, &plan, max_segments);
+  else
+    plan_decode_segments(pool_view(p), p->n_cu, dev_kept != nullptr, &plan, max_segments);
+  dp.wide = plan.wide ? 1 : 0;
   dp.seg_blocks = plan.seg_blocks;
   dp.n_seg = plan.n_seg;
   dp.partial = p->decode_partial;

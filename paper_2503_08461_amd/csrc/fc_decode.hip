@@ -268,7 +268,12 @@ __global__ __launch_bounds__(kThreads) void decode_attention_kernel(DecodeParams
 // ---------------------------------------------------------------------------
 // The same over an 8-bit pool: a lane has 16 channels of a row (16 bytes), so D / 16
 // neighbouring lanes a row and 1024 / D rows a load instruction.  Codes become fp32 numbers
-// (exactly); the row's power of two multiplies the key's logit and the value's weight.
+// (exactly); the row's power of two multiplies the key's logit and the value's weight.  HBM
+// bounds it where the call has heads to offer (48 caches of 1280-7040, 2 layers: 6.4 TB/s);
+// with a block in the time of half a one the loads' latency shows earlier, so a wavefront asks
+// for the next block before it works on this one also over whole heads (4 caches of 1000-1200,
+// 32 heads: 27.2 -> 15.6 us), and its rows' states are joined by lane exchanges, not in LDS
+// (3 caches of 2000-2400, 8 heads of 64 channels: 16 -> 9.7).
 // ---------------------------------------------------------------------------
 
 // sum over the LPR neighbouring lanes of a row (4 or 8), in every one of them
@@ -278,6 +283,25 @@ __device__ __forceinline__ float short_row_sum(float s) {
   s += from_lane<0x4E>(s);
   if constexpr (LPR == 8) s += from_lane<0x141>(s);
   return s;
+}
+
+// A lane's value and that of the lane kStep away (in either order), without LDS: halves of the
+// wavefront or rows of 16 change places, or the row is rotated.  Joining by 4 (where a row of
+// the cache has that few lanes), 8, 16 and 32 leaves the whole in every lane.
+template <int kStep>
+__device__ __forceinline__ void two_lanes(float v, float& a, float& b) {
+  if constexpr (kStep == 32) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    a = __uint_as_float(x[0]);
+    b = __uint_as_float(x[1]);
+  } else if constexpr (kStep == 16) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    a = __uint_as_float(x[0]);
+    b = __uint_as_float(x[1]);
+  } else {
+    a = v;
+    b = from_lane<0x120 + kStep>(v);
+  }
 }
 
 __device__ __forceinline__ void values_of(uint4v codes, float (&f)[16]) {
@@ -292,12 +316,11 @@ __device__ __forceinline__ void values_of(uint4v codes, float (&f)[16]) {
   }
 }
 
-template <int D, bool kCut, typename Reqs>
-__global__ __launch_bounds__(kThreads) void decode_attention_e4m3_kernel(DecodeParams p, Reqs reqs) {
+template <int D, int W, bool kCut, typename Reqs>
+__global__ __launch_bounds__(64 * W) void decode_attention_e4m3_kernel(DecodeParams p, Reqs reqs) {
   constexpr int LPR = D / 16;
   constexpr int RPI = 64 / LPR;
   constexpr int IPB = 16 / RPI;
-  constexpr int NG = kWaves * RPI;
   const int n_lh = p.n_layers * p.n_heads;
   const int unit = kCut ? blockIdx.x % (p.n_req * n_lh) : blockIdx.x;
   const int seg = kCut ? blockIdx.x / (p.n_req * n_lh) : 0;
@@ -373,34 +396,48 @@ __global__ __launch_bounds__(kThreads) void decode_attention_e4m3_kernel(DecodeP
       }
     }
   };
-  if constexpr (kCut) {
-    stream_tiles<Rows>(
-        own_tiles(b1 - b0, wave, kWaves), [&](int i, Rows& x) { fetch(b0 + wave + kWaves * i, x); },
-        [&](int i, const Rows& x) { attend(b0 + wave + kWaves * i, x); });
-  } else {
-    for (int b = wave; b < nb; b += kWaves) {
-      Rows x;
-      fetch(b, x);
-      attend(b, x);
-    }
-  }
+  stream_tiles<Rows>(
+      own_tiles(b1 - b0, wave, W), [&](int i, Rows& x) { fetch(b0 + wave + W * i, x); },
+      [&](int i, const Rows& x) { attend(b0 + wave + W * i, x); });
 
-  // merge the NG states, as above
-  __shared__ float sm_m[NG], sm_z[NG];
-  __shared__ float sm_acc[NG][D];
-  const int g = wave * RPI + grp;
-  if (piece == 0) {
-    sm_m[g] = m;
-    sm_z[g] = z;
-  }
+  // merge the states: of a wavefront's rows by lane exchanges, then of the wavefronts
+  auto join = [&](auto step) {
+    constexpr int kStep = decltype(step)::value;
+    float m0, m1, z0, z1;
+    two_lanes<kStep>(m, m0, m1);
+    two_lanes<kStep>(z, z0, z1);
+    m = fmaxf(m0, m1);
+    // (a sum of zero: no token; not a number stays not a number)
+    const float f0 = z0 == 0.f ? 0.f : __builtin_amdgcn_exp2f(m0 - m), f1 = z1 == 0.f ? 0.f : __builtin_amdgcn_exp2f(m1 - m);
+    z = z0 * f0 + z1 * f1;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) sm_acc[g][piece * 16 + e] = acc[e];
+    for (int e = 0; e < 16; ++e) {
+      float x0, x1;
+      two_lanes<kStep>(acc[e], x0, x1);
+      acc[e] = x0 * f0 + x1 * f1;
+    }
+  };
+  if constexpr (LPR == 4) join(std::integral_constant<int, 4>());
+  join(std::integral_constant<int, 8>());
+  join(std::integral_constant<int, 16>());
+  join(std::integral_constant<int, 32>());
+  __shared__ float sm_m[W], sm_z[W];
+  __shared__ float sm_acc[W][D];
+  if (lane == 0) {
+    sm_m[wave] = m;
+    sm_z[wave] = z;
+  }
+  if (grp == 0) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sm_acc[wave][piece * 16 + e] = acc[e];
+  }
   __syncthreads();
   float mm = -INFINITY, zz = 0.f, o = 0.f;
   if (threadIdx.x < D) {
-    for (int i = 0; i < NG; ++i) mm = fmaxf(mm, sm_m[i]);
-    for (int i = 0; i < NG; ++i) {
-      // (a sum of zero: no token; not a number stays not a number)
+#pragma unroll
+    for (int i = 0; i < W; ++i) mm = fmaxf(mm, sm_m[i]);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
       const float f = sm_z[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(sm_m[i] - mm);
       zz += sm_z[i] * f;
       o += sm_acc[i][threadIdx.x] * f;
@@ -470,11 +507,15 @@ static void launch_decode_e4m3(const DecodeParams& p, const DecodeReqs& inline_r
   const unsigned heads = (unsigned)p.n_req * p.n_layers * p.n_heads;
   with_reqs(p, inline_reqs, [&](const auto& reqs) {
     using Reqs = std::decay_t<decltype(reqs)>;
-    if (p.n_seg == 1) {
-      decode_attention_e4m3_kernel<D, false, Reqs><<<heads, kThreads, 0, s>>>(p, reqs);
+    if (p.n_seg == 1 && p.wide) {
+      decode_attention_e4m3_kernel<D, 16, false, Reqs><<<heads, 1024, 0, s>>>(p, reqs);
       return;
     }
-    decode_attention_e4m3_kernel<D, true, Reqs><<<heads * p.n_seg, kThreads, 0, s>>>(p, reqs);
+    if (p.n_seg == 1) {
+      decode_attention_e4m3_kernel<D, 4, false, Reqs><<<heads, kThreads, 0, s>>>(p, reqs);
+      return;
+    }
+    decode_attention_e4m3_kernel<D, 4, true, Reqs><<<heads * p.n_seg, kThreads, 0, s>>>(p, reqs);
     decode_merge_kernel<D, false, Reqs><<<heads, D, 0, s>>>(p, reqs);
   });
 }

@@ -52,6 +52,7 @@ struct DecodeParams {
   float scale_log2e;
   // attention: blocks per segment of a head, segments of the longest one (1: no head is cut)
   int32_t seg_blocks, n_seg;
+  int32_t wide;            // 8-bit pool, no head cut: 16 wavefronts a head
   float* partial;          // [n_req * layers * heads][n_seg][state_words] states of the segments
   int32_t* owner;          // ownership checks (debug mode), else NULL
   int32_t* error_flag;

@@ -580,4 +580,33 @@ void plan_decode_segments(const PoolView& pool, int n_cu, bool over_kept, Decode
   plan->n_seg = decode_segments(longest, plan->seg_blocks);
 }
 
+// Half the bytes: heads that leave CUs free are taken whole by 16 wavefronts while they are
+// short, without a second launch that merges them, else segments are of a quarter of a CU's
+// share and at least 32 blocks.  The attention alone, 32 heads of 128 channels, us:
+//   8 caches of 256-1408      16 wavefronts 15.6   segments 17.9   four wavefronts 18.1
+//   4 of 1000-1200                          13.2            13.7                   15.6
+//   1 of 8000                               48              17.7                   74
+//   3 of 2000-2400 (8 heads of 64)          12.1             9.7                   24.3
+//   a share's          eighth  quarter  half     at least 16   32    64
+//   1 of 30000           54.6     49.7  47.9
+//   16 of 130-16384       186      192   210
+//   1 of 8000                                            20.7  17.6  18.7
+void plan_decode_segments_e4m3(const PoolView& pool, int n_cu, DecodePlan* plan, int max_segments) {
+  if (plan->reqs.empty()) return;
+  const int64_t units = (int64_t)plan->reqs.size() * pool.n_layers * pool.n_heads;
+  int64_t total = 0;
+  for (const DecodeReq& q : plan->reqs) total += blocks_for(q.seq_len) * (int64_t)pool.n_layers * pool.n_heads;
+  const int longest = blocks_for(plan->reqs.front().seq_len);  // (longest first)
+  plan->seg_blocks = std::max(longest, 1);
+  plan->n_seg = 1;
+  plan->wide = units <= n_cu && longest >= 16 && longest <= kPlanWideE4m3;
+  if (plan->wide) return;
+  const int64_t room = max_segments / units;  // segments per head
+  if (room < 2) return;
+  const int64_t seg = std::max<int64_t>({total / (4 * (int64_t)std::max(n_cu, 1)), 32, (longest + room - 1) / room});
+  if (2 * seg > longest) return;
+  plan->seg_blocks = (int)seg;
+  plan->n_seg = decode_segments(longest, plan->seg_blocks);
+}
+
 }  // namespace fc

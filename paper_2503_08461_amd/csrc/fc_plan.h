@@ -172,6 +172,7 @@ struct DecodePlan {
   size_t kept_entries = 0;
   // attention: blocks per segment of a head, segments of the longest one (no head has more)
   int seg_blocks = 0, n_seg = 1;
+  bool wide = false;  // of an 8-bit pool, no head cut: 16 wavefronts a head instead of four
 };
 // Attention: most segments of all heads of a call that is split (heads x n_seg), which
 // is what the pool's buffers for their states hold (10.5 MB at 128 channels).
@@ -192,5 +193,8 @@ int plan_decode_attention(const PoolView& pool, int n_req, int max_blocks, const
 // max_segments: of all heads, kMaxDecodeSegments or 0 (a pool without the buffers).
 void plan_decode_segments(const PoolView& pool, int n_cu, bool over_kept, DecodePlan* plan,
                           int max_segments = kMaxDecodeSegments);
+// The same for an 8-bit pool.
+static constexpr int kPlanWideE4m3 = 128;  // blocks of the longest head that 16 wavefronts take whole
+void plan_decode_segments_e4m3(const PoolView& pool, int n_cu, DecodePlan* plan, int max_segments);
 
 }  // namespace fc
