@@ -553,6 +553,10 @@ int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_b
  *             with n_heads heads.  The pool gives the geometry; its blocks are
  *             neither read nor written, and its dtype does not matter.
  *
+ * Captured into a graph: a replay works on the lengths of the capture and on what
+ * the tables, rows and pool hold then.  A captured call of more requests than
+ * any call on the pool before (beyond some hundred) returns FC_EINVAL.
+ *
  * All four are asynchronous on `stream`; the attentions may split long caches
  * over workgroups, whose states lie in memory of the pool.  They are not part
  * of the kernel times.

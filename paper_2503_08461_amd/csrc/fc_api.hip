@@ -129,7 +129,11 @@ int grow(T** buf, size_t* cap, size_t need) {
 int grow_meta(fc_pool* p, size_t need) {
   if (need <= p->meta_cap) return FC_OK;
   FC_HIP(hipDeviceSynchronize());
-  if (p->dev_meta) FC_HIP(hipFree(p->dev_meta));
+  if (p->dev_meta && p->meta_captured)
+    p->meta_retired.push_back(p->dev_meta);  // (replays go on writing to it)
+  else if (p->dev_meta)
+    FC_HIP(hipFree(p->dev_meta));
+  p->meta_captured = false;
   if (p->host_meta) FC_HIP(hipHostFree(p->host_meta));
   p->dev_meta = nullptr;
   p->host_meta = nullptr;
@@ -230,6 +234,7 @@ int fc_pool_destroy(fc_pool* p) {
     if (p->mlp_b2[m]) (void)hipFree(p->mlp_b2[m]);
   }
   if (p->dev_meta) (void)hipFree(p->dev_meta);
+  for (char* old : p->meta_retired) (void)hipFree(old);
   if (p->host_meta) (void)hipHostFree(p->host_meta);
   if (p->meta_event) (void)hipEventDestroy(p->meta_event);
   for (int c = 0; c < kProfRing; ++c)
@@ -732,12 +737,18 @@ int compress_batch_impl(fc_pool* p, int32_t* dev_block_tables, int max_blocks_pe
 
 int fc::meta_to_device(fc_pool* p, const void* descs, size_t n_bytes, const void** out, hipStream_t stream) {
   const size_t bytes = round_up(n_bytes, 16);
+  const bool captured = capturing(stream);
+  if (captured && bytes > p->meta_cap)
+    return fail(FC_EINVAL, "a captured call of this many requests needs one of as many before the capture");
   int rc;
   if ((rc = grow_meta(p, bytes)) != FC_OK) return rc;
   std::vector<char> image(bytes, 0);
   memcpy(image.data(), descs, n_bytes);
   *out = p->dev_meta;
-  if (capturing(stream)) return upload_meta_arguments(image.data(), bytes, p->dev_meta, stream);
+  if (captured) {
+    p->meta_captured = true;
+    return upload_meta_arguments(image.data(), bytes, p->dev_meta, stream);
+  }
   return upload_meta_pinned(p, image.data(), bytes, p->dev_meta, stream);
 }
 

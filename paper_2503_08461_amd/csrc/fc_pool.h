@@ -8,12 +8,14 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <vector>
+
 namespace fc {
 // Sets the calling thread's error text (fc_last_error) and returns `code`.
 int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 constexpr int kProfRing = 32;
 // Descriptors of a call to the pool's buffer on the device (*out): through pinned memory, in a
-// captured call as kernel arguments.
+// captured call as kernel arguments (FC_EINVAL there if the buffer would have to grow).
 int meta_to_device(fc_pool* pool, const void* image, size_t bytes, const void** out, hipStream_t stream);
 }  // namespace fc
 
@@ -78,6 +80,8 @@ struct fc_pool {
   char* dev_meta = nullptr;
   char* host_meta = nullptr;  // pinned
   size_t meta_cap = 0;
+  bool meta_captured = false;       // a graph writes and reads dev_meta
+  std::vector<char*> meta_retired;  // earlier ones that graphs use, freed with the pool
   hipEvent_t meta_event = nullptr;
   bool meta_pending = false;
 
