@@ -545,7 +545,7 @@ int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_b
  *             sees for each of the last `window` new tokens, entry window - 1 being the
  *             last one.  The call writes its layer's entries; a request with
  *             n_new < window writes its last n_new.  This is what
- *             fc_compress_batch_lse takes.
+ *             fc_compress_batch_lse takes (with n_q_heads = n_heads).
  *
  * fc_prefill_attention: the same for whole prompts whose K and V need not be in
  * the pool (yet): token i of prompt r sees tokens 0..i of its own prompt.

@@ -8,7 +8,8 @@
 namespace fc {
 
 // ---------------------------------------------------------------------------
-// extend: workgroup = request that gets blocks; pops in batch order
+// extend: workgroup = request that gets blocks; pops in batch order.  A few words a request: the
+// launch is what it costs.
 // ---------------------------------------------------------------------------
 template <typename Reqs>
 __global__ __launch_bounds__(64) void extend_kernel(ExtendParams p, Reqs reqs) {
@@ -49,7 +50,8 @@ static void with_chunk_reqs(const ChunkReq* on_device, const ChunkReqs& inline_r
 // ---------------------------------------------------------------------------
 // store: workgroup = new token; its 2 * n_heads rows of one layer go to its slot.  D / 8
 // neighbouring lanes have a row, 16 bytes each; for the 8-bit pool they find the row's
-// maximum among themselves.
+// maximum among themselves.  Memory bounds it: 3 us for 48 tokens of 8 heads (latency), 17-19 us
+// for 2293 tokens of 32 heads (75 MB read and written, 4.3 TB/s).
 // ---------------------------------------------------------------------------
 template <int D, bool kE4M3, typename Reqs>
 __global__ __launch_bounds__(256) void store_chunk_kernel(StoreParams p, Reqs reqs) {
@@ -95,7 +97,10 @@ hipError_t launch_store_chunk(const StoreParams& p, const ChunkReqs& inline_reqs
 }
 
 // ---------------------------------------------------------------------------
-// quantise: workgroup = block of a request in one layer.
+// quantise: workgroup = block of a request in one layer: 32 * n_heads rows, read once, and as many
+// rows of half the bytes written, in whole lines but for the exponents (32 * n_heads bytes, a few of
+// a line at a time, which the L2 joins).  Memory bounds it: 64 caches of 256-1408 tokens, 32 heads
+// of 128 channels, 4 layers, 1060 us = 4.85 TB/s read and written, what a large copy reaches here.
 // ---------------------------------------------------------------------------
 template <int D, typename Reqs>
 __global__ __launch_bounds__(256) void quantise_kernel(QuantiseParams p, Reqs reqs) {
