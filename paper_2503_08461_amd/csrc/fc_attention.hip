@@ -349,7 +349,7 @@ struct Rows32 {
     // that are no finite numbers are added where their key is seen, and are zeros in the product.
     bool dirty = false;
     if constexpr (kMasked) {
-      dirty = keys.template dirty<kSub>();
+      dirty = __any(key0 + kSub * 32 - 1 > last_key) && keys.template dirty<kSub>();
       if (dirty) {
 #pragma unroll 1
         for (int key = 0; key < kSub * 32; ++key) {
@@ -671,10 +671,12 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
   const LaneRow me = lane_row(p, row0 + (lane & 31), w.n_rows);
   const int q_head = head * p.group + me.in_group;
   const int last_key = min(first_key + me.token, w.key_end - 1);  // (a segment may end inside a tile)
-  const int wave_last = min(first_key + token_of(p, min(row0 + 31, w.n_rows - 1)), w.key_end - 1);
+  // the last key that any row of the wavefront sees (none if it has no row)
+  const int wave_last = row0 < w.n_rows ? min(first_key + token_of(p, min(row0 + 31, w.n_rows - 1)), w.key_end - 1) : -1;
   const int n_tiles = w.key_end > w.key_begin ? (w.key_end - w.key_begin + kKeys - 1) / kKeys : 0;
-  // tiles that every row of the workgroup sees whole
-  const int n_full = max(min(first_key + token_of(p, w.tile * kTallRows), w.key_end - 1) + 1 - w.key_begin, 0) / kKeys;
+  // tiles that every row of the wavefront sees whole (the wavefronts' differ; all meet once a tile)
+  const int n_full =
+      row0 < w.n_rows ? max(min(first_key + token_of(p, row0), w.key_end - 1) + 1 - w.key_begin, 0) / kKeys : 0;
 
   Rows32<D> rows;
   rows.start();
