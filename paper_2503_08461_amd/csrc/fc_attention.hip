@@ -19,7 +19,7 @@
 //
 // Two parts of one launch: many rows (prompts, long chunks; bound by the matrix cores) and few
 // rows of a head and request, up to 32 (single tokens, short chunks; bound by memory).  (Two launches:
-// a mixed batch of 24 chunks of 1-512 tokens 269 us, one 240; the few rows' workgroups fill what the
+// a mixed batch of 24 chunks of 1-512 tokens 269 us, one 240, now 231; the few rows' workgroups fill what the
 // many rows' leave.)
 
 #include <algorithm>
@@ -649,14 +649,15 @@ __device__ __forceinline__ BufferPtr rows_at(const _Float16* from, int stride, i
 // ---------------------------------------------------------------------------
 // Many rows: four wavefronts of 32 rows over the same keys, 64 at a time.  Two tiles in LDS:
 // while one is worked on, each wavefront brings in 16 keys of the next, straight from memory to
-// LDS (through registers: 741 us where this takes 370, see below).
+// LDS (32 prompts of 600-1200 tokens, 32 heads: 392 us, through registers 741; now 359).  Where
+// its rows see all of a tile, the loop without a mask; the border is the wavefront's own (with the
+// workgroup's 373).
 //
-// 64 KB of LDS and 256 registers: two workgroups a CU, the softmax of one beside the products of
-// the other.  Measured, 128 channels: prompts of 5900-7040 tokens, 8 heads of K and V and 32 query
+// 64 KB of LDS: two workgroups a CU, the softmax of one beside the products of the other.  Measured, 128 channels: prompts of 5900-7040 tokens, 8 heads of K and V and 32 query
 // heads, 1.03 PFLOP/s (a library product of 8192^3: 1.12); 2048 tokens behind 28 000 1.03; 32
-// prompts of 600-1200, 32 heads, 0.60; one of 640, 17.7 us.  Long prompts are bound by the card's
+// prompts of 600-1200, 32 heads, 0.61; one of 640, 17.3 us.  Long prompts are bound by the card's
 // power: the matrix pipes are busy for 60 % of the cycles, at 1.6 GHz, and with zeros for random
-// numbers the same work runs at 1.4 PFLOP/s.  Short ones (37 % of the cycles) by what does not
+// numbers the same work runs at 1.4 PFLOP/s.  Short ones (not 40 % of the cycles) by what does not
 // overlap: queries, the first tile, the tiles at the mask and the results of two workgroups at a time.
 // ---------------------------------------------------------------------------
 template <int D, int SRC, bool kSplit, typename Reqs>
