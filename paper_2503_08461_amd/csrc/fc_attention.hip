@@ -653,12 +653,13 @@ __device__ __forceinline__ BufferPtr rows_at(const _Float16* from, int stride, i
 // its rows see all of a tile, the loop without a mask; the border is the wavefront's own (with the
 // workgroup's 373).
 //
-// 64 KB of LDS: two workgroups a CU, the softmax of one beside the products of the other.  Measured, 128 channels: prompts of 5900-7040 tokens, 8 heads of K and V and 32 query
-// heads, 1.03 PFLOP/s (a library product of 8192^3: 1.12); 2048 tokens behind 28 000 1.03; 32
-// prompts of 600-1200, 32 heads, 0.61; one of 640, 17.3 us.  Long prompts are bound by the card's
-// power: the matrix pipes are busy for 60 % of the cycles, at 1.6 GHz, and with zeros for random
-// numbers the same work runs at 1.4 PFLOP/s.  Short ones (not 40 % of the cycles) by what does not
-// overlap: queries, the first tile, the tiles at the mask and the results of two workgroups at a time.
+// 64 KB of LDS: two workgroups a CU, the softmax of one beside the products of the other.  Measured,
+// 128 channels: prompts of 5900-7040 tokens, 8 heads of K and V and 32 query heads, 1.03 PFLOP/s (a
+// library product of 8192^3: 1.12); 2048 tokens behind 28 000 1.03; 32 prompts of 600-1200, 32 heads,
+// 0.61; one of 640, 17.3 us.  Long prompts are bound by the card's power: the matrix pipes are busy
+// for 60 % of the cycles, at 1.6 GHz, and with zeros for random numbers the same work runs at 1.4
+// PFLOP/s.  Short ones (not 40 % of the cycles) by what does not overlap: queries, the first tile,
+// the tiles at the mask and the results of two workgroups at a time.
 // ---------------------------------------------------------------------------
 template <int D, int SRC, bool kSplit, typename Reqs>
 __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& reqs, half8* sm, int unit, int head) {
