@@ -20,7 +20,11 @@
  * its block tables.  The library's scratch buffers (kept lists, saved ids,
  * un-pooled scores, descriptors) grow on demand: a call that needs more than
  * any earlier one waits for the device, frees and reallocates BEFORE it queues
- * anything; calls whose needs were met before are fully asynchronous.
+ * anything; calls whose needs were met before are fully asynchronous.  The
+ * calls on single tokens, chunks and prompts allocate nothing while they are
+ * captured into a graph: with more requests than fit a kernel's arguments (some
+ * 150) they return FC_EINVAL there unless a call on as many came before, and
+ * the memory that they then use stays until the pool is destroyed.
  * "dev" pointers are device (HBM) addresses, "host" pointers are ordinary
  * host memory.  All device work is issued on the hipStream_t passed as
  * `stream` (NULL = the default stream) and is asynchronous with respect to
@@ -554,8 +558,7 @@ int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_b
  *             neither read nor written, and its dtype does not matter.
  *
  * Captured into a graph: a replay works on the lengths of the capture and on what
- * the tables, rows and pool hold then.  A captured call of more requests than
- * any call on the pool before (beyond some hundred) returns FC_EINVAL.
+ * the tables, rows and pool hold then.
  *
  * All four are asynchronous on `stream`; the attentions may split long caches
  * over workgroups, whose states lie in memory of the pool.  They are not part
