@@ -20,11 +20,13 @@
  * its block tables.  The library's scratch buffers (kept lists, saved ids,
  * un-pooled scores, descriptors) grow on demand: a call that needs more than
  * any earlier one waits for the device, frees and reallocates BEFORE it queues
- * anything; calls whose needs were met before are fully asynchronous.  The
- * calls on single tokens, chunks and prompts allocate nothing while they are
- * captured into a graph: with more requests than fit a kernel's arguments (some
- * 150) they return FC_EINVAL there unless a call on as many came before, and
- * the memory that they then use stays until the pool is destroyed.
+ * anything; calls whose needs were met before are fully asynchronous.  A call
+ * that is captured into a graph allocates nothing: it returns FC_EINVAL unless
+ * a call of its size came before (on single tokens, chunks and prompts up to
+ * some 150 requests, which fit a kernel's arguments, none has to, nor before
+ * fc_compress_batch_noalloc).  The memory that it uses stays until the pool is
+ * destroyed, also the weights of fc_mlp_set_weights: replays go on with those
+ * of the capture.  A replay counts as a call where calls have to be ordered.
  * "dev" pointers are device (HBM) addresses, "host" pointers are ordinary
  * host memory.  All device work is issued on the hipStream_t passed as
  * `stream` (NULL = the default stream) and is asynchronous with respect to
@@ -319,7 +321,7 @@ typedef struct fc_mlp_weights {
 /* Copies the weights into library-owned device memory in the operand order of
  * the kernel (the caller's buffers may be released after the stream has run
  * past this call).  FC_EINVAL for unsupported sizes, an unknown activation or
- * NULL pointers. */
+ * NULL pointers, and in a call that is captured into a graph. */
 int fc_mlp_set_weights(fc_pool* pool, const fc_mlp_weights* weights, void* stream);
 
 /*

@@ -101,28 +101,31 @@ int release_verdict(fc_pool* p, hipStream_t stream, const char* what);
 namespace {
 
 template <typename T>
-hipError_t try_grow(T** buf, size_t* cap, size_t need) {
-  if (need <= *cap) return hipSuccess;
+hipError_t try_grow(fc_pool* p, Scratch<T>* s, size_t need) {
+  if (need <= s->cap) return hipSuccess;
   // the old buffer may still be in use by queued work
   hipError_t e = hipDeviceSynchronize();
-  if (e == hipSuccess && *buf) e = hipFree(*buf);
   if (e != hipSuccess) return e;
-  *buf = nullptr;
-  *cap = 0;
+  if (s->captured)
+    p->retired.push_back(s->data);
+  else if (s->data)
+    e = hipFree(s->data);
+  if (e != hipSuccess) return e;
+  *s = Scratch<T>();
   const size_t n = round_up(need + need / 8, 4096);
-  e = hipMalloc(reinterpret_cast<void**>(buf), n * sizeof(T));
+  e = hipMalloc(reinterpret_cast<void**>(&s->data), n * sizeof(T));
   if (e != hipSuccess) {
-    *buf = nullptr;
+    s->data = nullptr;
     (void)hipGetLastError();  // (a later launch must not report it)
     return e;
   }
-  *cap = n;
+  s->cap = n;
   return hipSuccess;
 }
 
 template <typename T>
-int grow(T** buf, size_t* cap, size_t need) {
-  FC_HIP(try_grow(buf, cap, need));
+int grow(fc_pool* p, Scratch<T>* s, size_t need) {
+  FC_HIP(try_grow(p, s, need));
   return FC_OK;
 }
 
@@ -223,9 +226,10 @@ int fc_pool_destroy(fc_pool* p) {
   if (p->stack) (void)hipFree(p->stack);
   if (p->owner) (void)hipFree(p->owner);
   if (p->check_word) (void)hipFree(p->check_word);
-  if (p->raw_scores) (void)hipFree(p->raw_scores);
-  if (p->kept) (void)hipFree(p->kept);
-  if (p->ids) (void)hipFree(p->ids);
+  if (p->raw_scores.data) (void)hipFree(p->raw_scores.data);
+  if (p->kept.data) (void)hipFree(p->kept.data);
+  if (p->ids.data) (void)hipFree(p->ids.data);
+  for (void* old : p->retired) (void)hipFree(old);
   if (p->decode_partial) (void)hipFree(p->decode_partial);
   if (p->error_flag) (void)hipFree(p->error_flag);
   for (int m = 0; m < 2; ++m) {
@@ -460,6 +464,10 @@ bool capturing(hipStream_t stream) {
   (void)hipGetLastError();  // (the default stream, while another one is captured)
   return false;
 }
+// ... and allocates nothing: what it needs has to be there, and stays for its replays.
+int refuse_growing_capture() {
+  return fail(FC_EINVAL, "a captured call needs one of its size before the capture: it cannot allocate its scratch memory");
+}
 int upload_meta(fc_pool* p, const char* image, size_t bytes, char* dev_dst, bool no_alloc,
                 hipStream_t stream) {
   if (no_alloc || bytes <= kMaxArgumentMeta || capturing(stream))
@@ -484,10 +492,9 @@ bool fits_inline(const fc_pool* p, const char* image, size_t bytes, MetaChunk* c
 // allocates nothing, and a size that was refused is not asked for again: each attempt
 // waits for the device.
 bool have_split_scratch(fc_pool* p, size_t raw_floats, size_t kept_entries, hipStream_t stream) {
-  if (raw_floats <= p->raw_cap && kept_entries <= p->kept_cap) return true;
+  if (raw_floats <= p->raw_scores.cap && kept_entries <= p->kept.cap) return true;
   if (raw_floats >= p->split_refused || capturing(stream)) return false;
-  if (try_grow(&p->raw_scores, &p->raw_cap, raw_floats) == hipSuccess &&
-      try_grow(&p->kept, &p->kept_cap, kept_entries) == hipSuccess)
+  if (try_grow(p, &p->raw_scores, raw_floats) == hipSuccess && try_grow(p, &p->kept, kept_entries) == hipSuccess)
     return true;
   p->split_refused = raw_floats;
   return false;
@@ -591,15 +598,21 @@ int compress_batch_impl(fc_pool* p, int32_t* dev_block_tables, int max_blocks_pe
     dev_meta = reinterpret_cast<char*>(p->fixed_scratch + kNoAllocMetaOff);
   } else {
     // (growth waits for the device and frees: it happens before anything is queued)
-    // (the fused kernels keep their lists in LDS)
-    if (!dev_kept_out && separate && (rc = grow(&p->kept, &p->kept_cap, plan.kept_entries)) != FC_OK)
-      return rc;
-    if ((rc = grow(&p->ids, &p->ids_cap, n_ids)) != FC_OK) return rc;
-    if (separate && (rc = grow(&p->raw_scores, &p->raw_cap, raw_floats)) != FC_OK) return rc;
+    // (the fused kernels keep their lists in LDS, and split heads' scratch is there by now)
+    const size_t kept_need = !dev_kept_out && separate ? plan.kept_entries : 0, raw_need = separate ? raw_floats : 0;
+    if (capturing(stream)) {
+      if (kept_need > p->kept.cap || n_ids > p->ids.cap || raw_need > p->raw_scores.cap || meta_bytes > p->meta_cap)
+        return refuse_growing_capture();
+      p->ids.captured = p->meta_captured = true;
+      if (separate || n_split) p->kept.captured = p->raw_scores.captured = true;
+    }
+    if ((rc = grow(p, &p->kept, kept_need)) != FC_OK) return rc;
+    if ((rc = grow(p, &p->ids, n_ids)) != FC_OK) return rc;
+    if ((rc = grow(p, &p->raw_scores, raw_need)) != FC_OK) return rc;
     if ((rc = grow_meta(p, meta_bytes)) != FC_OK) return rc;
-    if (!kept_buf) kept_buf = p->kept;
-    raw_buf = p->raw_scores;
-    ids_buf = p->ids;
+    if (!kept_buf) kept_buf = p->kept.data;
+    raw_buf = p->raw_scores.data;
+    ids_buf = p->ids.data;
     dev_meta = p->dev_meta;
   }
   std::vector<char> image(meta_bytes, 0);
@@ -738,8 +751,7 @@ int compress_batch_impl(fc_pool* p, int32_t* dev_block_tables, int max_blocks_pe
 int fc::meta_to_device(fc_pool* p, const void* descs, size_t n_bytes, const void** out, hipStream_t stream) {
   const size_t bytes = round_up(n_bytes, 16);
   const bool captured = capturing(stream);
-  if (captured && bytes > p->meta_cap)
-    return fail(FC_EINVAL, "a captured call of this many requests needs one of as many before the capture");
+  if (captured && bytes > p->meta_cap) return refuse_growing_capture();
   int rc;
   if ((rc = grow_meta(p, bytes)) != FC_OK) return rc;
   std::vector<char> image(bytes, 0);
@@ -824,6 +836,10 @@ int fc_window_lse(fc_pool* p, const int32_t* dev_block_tables, int max_blocks_pe
   const size_t desc_bytes = round_up((size_t)n * sizeof(ReqDesc), 16);
   const size_t meta_bytes = desc_bytes + round_up((size_t)n * sizeof(int32_t), 16);
   int rc;
+  if (capturing(stream)) {
+    if (meta_bytes > p->meta_cap) return refuse_growing_capture();
+    p->meta_captured = true;
+  }
   if ((rc = grow_meta(p, meta_bytes)) != FC_OK) return rc;
   std::vector<char> image(meta_bytes, 0);
   memcpy(image.data(), plan.descs.data(), (size_t)n * sizeof(ReqDesc));
@@ -872,17 +888,23 @@ int fc_mlp_set_weights(fc_pool* p, const fc_mlp_weights* w, void* stream_) {
   for (int m = 0; m < 2; ++m)
     if (!w->w1[m] || !w->b1[m] || !w->w2[m] || !w->b2[m])
       return fail(FC_EINVAL, "NULL weight pointer");
+  if (capturing(stream)) return fail(FC_EINVAL, "fc_mlp_set_weights allocates: it cannot be captured");
   FC_HIP(hipDeviceSynchronize());  // earlier calls may still read the old copies
   const size_t n1 = mlp_w1p_elems(p->head_dim, w->hidden, w->k);
   const size_t n2 = mlp_w2p_elems(p->head_dim, w->hidden);
   for (int m = 0; m < 2; ++m) {
-    if (p->mlp_w1p[m]) FC_HIP(hipFree(p->mlp_w1p[m]));  // w2p lies in the same allocation
-    if (p->mlp_b1[m]) FC_HIP(hipFree(p->mlp_b1[m]));
-    if (p->mlp_b2[m]) FC_HIP(hipFree(p->mlp_b2[m]));
+    // (w2p lies in the same allocation as w1p)
+    for (void* old : {static_cast<void*>(p->mlp_w1p[m]), static_cast<void*>(p->mlp_b1[m]), static_cast<void*>(p->mlp_b2[m])}) {
+      if (old && p->mlp_captured)
+        p->retired.push_back(old);  // (replays go on with the weights of their capture)
+      else if (old)
+        FC_HIP(hipFree(old));
+    }
     p->mlp_w1p[m] = p->mlp_w2p[m] = nullptr;
     p->mlp_b1[m] = p->mlp_b2[m] = nullptr;
   }
   p->mlp_k = p->mlp_hidden = 0;
+  p->mlp_captured = false;
   for (int m = 0; m < 2; ++m) {
     // one allocation: the kernel streams W1 and then W2 through the same ring
     FC_HIP(hipMalloc(reinterpret_cast<void**>(&p->mlp_w1p[m]), (n1 + n2) * sizeof(_Float16)));
@@ -921,9 +943,14 @@ int fc_compress_batch_mlp(fc_pool* p, int32_t* dev_block_tables, int max_blocks_
   if (n_comp == 0) return FC_OK;
 
   int rc;
-  if ((rc = grow(&p->ids, &p->ids_cap, (size_t)plan.total_old + plan.total_new)) != FC_OK) return rc;
+  const size_t n_ids = (size_t)plan.total_old + plan.total_new;
   const size_t desc_bytes = round_up((size_t)n_comp * sizeof(ReqDesc), 16);
   const size_t job_bytes = round_up(plan.jobs.size() * sizeof(MlpJob), 16);
+  if (capturing(stream)) {
+    if (n_ids > p->ids.cap || desc_bytes + job_bytes > p->meta_cap) return refuse_growing_capture();
+    p->ids.captured = p->meta_captured = p->mlp_captured = true;
+  }
+  if ((rc = grow(p, &p->ids, n_ids)) != FC_OK) return rc;
   if ((rc = grow_meta(p, desc_bytes + job_bytes)) != FC_OK) return rc;
   std::vector<char> image(desc_bytes + job_bytes, 0);
   memcpy(image.data(), plan.descs.data(), (size_t)n_comp * sizeof(ReqDesc));
@@ -948,8 +975,8 @@ int fc_compress_batch_mlp(fc_pool* p, int32_t* dev_block_tables, int max_blocks_
   bp.n_comp = n_comp;
   bp.block_tables = dev_block_tables;
   bp.max_blocks = max_blocks_per_req;
-  bp.old_ids = p->ids;
-  bp.new_ids = p->ids + plan.total_old;
+  bp.old_ids = p->ids.data;
+  bp.new_ids = p->ids.data + plan.total_old;
   bp.error_flag = p->error_flag;
   bp.owner = p->debug_checks ? p->owner : nullptr;
   MlpParams mp = {};

@@ -55,6 +55,17 @@ int meta_to_device(fc_pool* pool, const void* image, size_t bytes, const void** 
       return fail(FC_EINVAL, "%s takes a pool of FC_DTYPE_F16", what);              \
   } while (0)
 
+namespace fc {
+// A device buffer that calls share and that grows on demand.  captured: a graph's replays use it;
+// what replaces it then leaves it to the pool, to be freed with it.
+template <typename T>
+struct Scratch {
+  T* data = nullptr;
+  size_t cap = 0;  // elements
+  bool captured = false;
+};
+}  // namespace fc
+
 struct fc_pool {
   _Float16* kv = nullptr;    // (an 8-bit pool's bytes: see dtype)
   int dtype = FC_DTYPE_F16;
@@ -70,13 +81,11 @@ struct fc_pool {
   int32_t* check_word = nullptr;  // device: what the last release check found
 
   // scratch, grown on demand
-  float* raw_scores = nullptr;
-  size_t raw_cap = 0;  // floats
-  int32_t* kept = nullptr;
-  size_t kept_cap = 0;  // ints
+  fc::Scratch<float> raw_scores;
+  fc::Scratch<int32_t> kept;
   size_t split_refused = ~(size_t)0;  // least score scratch of split heads that could not be had
-  int32_t* ids = nullptr;
-  size_t ids_cap = 0;  // ints (old ids then new ids)
+  fc::Scratch<int32_t> ids;  // old ids then new ids
+  std::vector<void*> retired;  // buffers that graphs use and calls do not any more
   char* dev_meta = nullptr;
   char* host_meta = nullptr;  // pinned
   size_t meta_cap = 0;
@@ -99,6 +108,7 @@ struct fc_pool {
   _Float16* mlp_w2p[2] = {nullptr, nullptr};
   float* mlp_b1[2] = {nullptr, nullptr};
   float* mlp_b2[2] = {nullptr, nullptr};
+  bool mlp_captured = false;  // a graph reads them
 
   bool profiling = false;
   // event ring: the last kProfRing profiled calls, [call][kernel][start, stop]
