@@ -199,13 +199,18 @@ int fc_pool_create(fc_pool** out, void* kv_base, size_t kv_bytes, int n_blocks, 
   if (e == hipSuccess) e = launch_zero_ints(p->error_flag, 2, nullptr);
   p->arrivals = p->error_flag ? p->error_flag + 1 : nullptr;
   // (a fixed size, here and not on demand: no decode step waits for an allocation, and a
-  // captured one finds it where it was; without it no head is cut into segments)
-  if (e == hipSuccess &&
-      hipMalloc(reinterpret_cast<void**>(&p->decode_partial),
-                (size_t)std::max(kMaxDecodeSegments, kMaxAttnStates) * DecodeParams::state_words(head_dim) * sizeof(float)) !=
-          hipSuccess) {
-    p->decode_partial = nullptr;
-    (void)hipGetLastError();  // (a later launch must not report it)
+  // captured one finds it where it was.  On a card that is nearly full what a decode step can
+  // use, a quarter of it; without that no head is cut into segments)
+  static_assert(kMaxDecodeSegments <= kMaxAttnStates, "the larger one first");
+  for (const int states : {kMaxAttnStates, kMaxDecodeSegments}) {
+    if (e != hipSuccess || p->max_states) break;
+    const size_t bytes = (size_t)states * DecodeParams::state_words(head_dim) * sizeof(float);
+    if (hipMalloc(reinterpret_cast<void**>(&p->decode_partial), bytes) == hipSuccess) {
+      p->max_states = states;
+    } else {
+      p->decode_partial = nullptr;
+      (void)hipGetLastError();  // (a later launch must not report it)
+    }
   }
   if (e == hipSuccess) e = hipEventCreateWithFlags(&p->meta_event, hipEventDisableTiming);
   for (int c = 0; c < kProfRing && e == hipSuccess; ++c)
@@ -1107,7 +1112,7 @@ int decode_attention_impl(fc_pool* p, const int32_t* dev_block_tables, int max_b
   dp.q = static_cast<const _Float16*>(dev_q);
   dp.out = dev_out;
   dp.kept = dev_kept;
-  const int max_segments = p->decode_partial ? kMaxDecodeSegments : 0;
+  const int max_segments = std::min(kMaxDecodeSegments, p->max_states);
   if (dp.e4m3)
     plan_decode_segments_e4m3(pool_view(p), p->n_cu, &plan, max_segments);
   else

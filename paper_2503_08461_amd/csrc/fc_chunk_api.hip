@@ -93,8 +93,7 @@ int attention(fc_pool* p, int layer, const int32_t* dev_block_tables, int max_bl
                  (rc = check_rows(v, "v", plan.n_rows, p->n_heads, p->head_dim, false))))
     return rc;
   AttnLaunch launches[ATTN_KINDS];
-  if (plan_attention(geometry(p), p->n_cu, n_q_heads / p->n_heads, paged, p->decode_partial ? kMaxAttnStates : 0, &plan,
-                     launches) != PLAN_OK)
+  if (plan_attention(geometry(p), p->n_cu, n_q_heads / p->n_heads, paged, p->max_states, &plan, launches) != PLAN_OK)
     return fail(plan.code, "%s", plan.message);
 
   AttnParams ap = {};

@@ -37,7 +37,8 @@ static constexpr int kAttnKinds = 2;
 static constexpr int kTallRows = 128;  // rows (new tokens x query heads of a group) of a workgroup
 static constexpr int kFlatRows = 32;
 static constexpr int kPlanMinSegment = 32;  // blocks
-// Most states of a call's split rows, what the pool's buffer holds (42 MB at 128 channels).
+// Most states of a call's split rows, what the pool's buffer holds if the card has the room (42 MB
+// at 128 channels; else kMaxDecodeSegments, or none).
 static constexpr int kMaxAttnStates = 65536;
 struct AttnLaunch {
   std::vector<ChunkReq> reqs;  // longest first; unit = (row tile, segment), heads not counted

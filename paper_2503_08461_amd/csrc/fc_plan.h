@@ -190,7 +190,7 @@ int plan_append(const PoolView& pool, int n_req, int max_blocks, const int32_t* 
 int plan_decode_attention(const PoolView& pool, int n_req, int max_blocks, const int32_t* seq_lens,
                           const int32_t* budget /* NULL: whole cache */, DecodePlan* plan);
 // Sets seg_blocks and n_seg of a planned attention (over_kept: of the kept lists);
-// max_segments: of all heads, kMaxDecodeSegments or 0 (a pool without the buffers).
+// max_segments: of all heads, kMaxDecodeSegments or 0 (a pool without the memory).
 void plan_decode_segments(const PoolView& pool, int n_cu, bool over_kept, DecodePlan* plan,
                           int max_segments = kMaxDecodeSegments);
 // The same for an 8-bit pool.

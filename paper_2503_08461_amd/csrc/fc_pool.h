@@ -95,7 +95,8 @@ struct fc_pool {
   bool meta_pending = false;
 
   int n_cu = 0;                   // compute units of the pool's device
-  float* decode_partial = nullptr;  // states of the segments of a split attention
+  float* decode_partial = nullptr;  // states of the segments of a split attention, ...
+  int max_states = 0;               // ... and how many it holds
   int32_t* error_flag = nullptr;  // device, one int, zero unless a kernel found something wrong
   int32_t* arrivals = nullptr;    // device, the int after it: zero between calls (BatchParams)
   int score_mode = FC_SCORE_AUTO;
