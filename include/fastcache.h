@@ -429,7 +429,7 @@ const char* fc_last_error(void);
  * L_r + 1 before the call returns; the device work is asynchronous on stream.
  *   dev_new_kv  dev, fp16 [n_req][n_layers][2][n_heads][head_dim], 16-byte aligned
  * FC_EINVAL: L_r < 0 or >= FC_MAX_SEQ_LEN, table row full (L_r/16 >=
- * max_blocks_per_req); FC_ENOMEM: more blocks needed than are free.  Nothing
+ * max_blocks_per_req), 2^24 or more requests times layers; FC_ENOMEM: more blocks needed than are free.  Nothing
  * is modified on error.
  *
  * fc_decode_attention: the single-query attention of one decode step over
@@ -439,6 +439,8 @@ const char* fc_last_error(void);
  * 1/sqrt(head_dim)).  Reads every cached K and V row once.
  *   dev_q    dev, fp16 [n_req][n_layers][n_heads][head_dim], 16-byte aligned
  *   dev_out  dev, fp32 [n_req][n_layers][n_heads][head_dim]
+ * FC_EINVAL: a length outside 0..FC_MAX_SEQ_LEN or beyond the table, NULL or
+ * misaligned buffers, 2^24 or more heads of all requests and layers.
  */
 int fc_append_batch(fc_pool* pool, int32_t* dev_block_tables, int max_blocks_per_req,
                     int32_t* host_seq_lens, const void* dev_new_kv, const int32_t* host_enable,
@@ -502,7 +504,7 @@ int fc_decode_attention_kept(fc_pool* pool, const int32_t* dev_block_tables,
  * the blocks before, fc_pool_free releases the old ones afterwards.
  * Asynchronous on `stream`.
  * FC_EINVAL: dtypes or geometries that do not match, a length outside
- * 0..FC_MAX_SEQ_LEN or beyond either table.
+ * 0..FC_MAX_SEQ_LEN or beyond either table, 2^24 or more blocks of all layers.
  */
 int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_blocks_per_req,
                       fc_pool* src, const int32_t* dev_src_tables, int src_max_blocks_per_req,
@@ -568,7 +570,8 @@ int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_b
  * FC_EINVAL: layer outside 0..n_layers-1, n_new_r outside 0..L_r, L_r >
  * FC_MAX_SEQ_LEN or beyond the table, n_q_heads not a multiple of n_heads or
  * more than FC_MAX_GROUP times it, window < 0 (or < 1 with dev_lse), bad alignment or strides, NULL where
- * a buffer is needed.
+ * a buffer is needed, 2^24 or more workgroups in a launch (one a token stored, one
+ * per 128 rows of a head attended).
  */
 #define FC_MAX_GROUP 64 /* most query heads that share a head of K and V */
 #define FC_MAX_TOKEN_STRIDE (1 << 24)

@@ -193,7 +193,7 @@ int fc_store_chunk(fc_pool* p, int layer, const int32_t* dev_block_tables, int m
     if ((rc = check_rows(k, "k", plan.n_rows, p->n_heads, p->head_dim, false)) ||
         (rc = check_rows(v, "v", plan.n_rows, p->n_heads, p->head_dim, false)))
       return rc;
-    plan_store_units(&plan);
+    if (plan_store_units(&plan) != PLAN_OK) return fail(plan.code, "%s", plan.message);
     StoreParams sp = {};
     ChunkReqs inline_reqs;
     if ((rc = pass_reqs(p, plan.reqs, &inline_reqs, &sp.reqs, stream))) return rc;
@@ -253,7 +253,7 @@ int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_b
     if (plan_quantise(n_req, dst_max_blocks_per_req, src_max_blocks_per_req, host_seq_lens, host_enable, &plan) != PLAN_OK)
       return fail(plan.code, "%s", plan.message);
     if (plan.reqs.empty()) return FC_OK;
-    if (plan.n_rows * src->n_layers > 0x7fffffff) return fail(FC_EINVAL, "batch too large for one launch");
+    if (plan.n_rows * src->n_layers > kPlanMaxWorkgroups) return fail(FC_EINVAL, "batch too large for one launch");
     QuantiseParams qp = {};
     ChunkReqs inline_reqs;
     if (int rc = pass_reqs(dst, plan.reqs, &inline_reqs, &qp.reqs, stream)) return rc;

@@ -71,8 +71,10 @@ int plan_chunk(int n_req, int max_blocks, const int32_t* seq_lens, const int32_t
   return PLAN_OK;
 }
 
-void plan_store_units(ChunkPlan* plan) {
+int plan_store_units(ChunkPlan* plan) {
+  if (plan->n_rows > kPlanMaxWorkgroups) return fail(plan, PLAN_EINVAL, "batch too large for one launch");
   for (ChunkReq& q : plan->reqs) q.unit_start = q.row_off;
+  return PLAN_OK;
 }
 
 int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, int64_t max_states,
@@ -130,7 +132,7 @@ int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, in
       q.state_off = (int32_t)state_off;
       state_off += q.n_new;
       l.n_units += tiles(q) * decode_segments(blocks_for(q.seq_len), l.seg_blocks);
-      if ((launches[0].n_units + launches[1].n_units) * pool.n_heads > kMaxRows)
+      if ((launches[0].n_units + launches[1].n_units) * pool.n_heads > kPlanMaxWorkgroups)
         return fail(plan, PLAN_EINVAL, "batch too large for one launch");
     }
   }

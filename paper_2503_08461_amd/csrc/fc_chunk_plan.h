@@ -27,8 +27,8 @@ struct ChunkPlan {
 };
 // n_new NULL: whole prompts (every token is new); max_blocks -1: no table.
 int plan_chunk(int n_req, int max_blocks, const int32_t* seq_lens, const int32_t* n_new, ChunkPlan* plan);
-// fc_store_chunk: a unit is a packed row.
-void plan_store_units(ChunkPlan* plan);
+// fc_store_chunk: a unit is a packed row.  FC_EINVAL (plan->code) where they are too many for a launch.
+int plan_store_units(ChunkPlan* plan);
 
 // The requests of an attention by kind: those with many rows to a head of K and V take
 // workgroups whose wavefronts have rows of their own, those with few rows wavefronts that

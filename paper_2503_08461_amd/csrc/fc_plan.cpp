@@ -505,6 +505,8 @@ int plan_append(const PoolView& pool, int n_req, int max_blocks, const int32_t* 
     DecodeReq q = {r, L, (L % kPlanBlockSize == 0) ? plan->n_pop++ : -1, 0, 0};
     plan->reqs.push_back(q);
   }
+  if ((int64_t)plan->reqs.size() * pool.n_layers > kPlanMaxWorkgroups)
+    return fail(plan, PLAN_EINVAL, "batch too large for one launch");
   if (plan->n_pop > pool.n_free)
     return fail(plan, PLAN_ENOMEM, "append needs %d new blocks, %d free", plan->n_pop,
                 pool.n_free);
@@ -519,6 +521,8 @@ int plan_decode_attention(const PoolView& pool, int n_req, int max_blocks, const
   if (!seq_lens) return fail(plan, PLAN_EINVAL, "NULL argument");
   if (max_blocks < 1) return fail(plan, PLAN_EINVAL, "max_blocks_per_req < 1");
   const size_t n_lh = (size_t)pool.n_layers * pool.n_heads;
+  if (n_lh * (size_t)n_req > (size_t)kPlanMaxWorkgroups)
+    return fail(plan, PLAN_EINVAL, "batch too large for one launch");
   plan->reqs.resize(n_req);
   for (int r = 0; r < n_req; ++r) {
     const int L = seq_lens[r];

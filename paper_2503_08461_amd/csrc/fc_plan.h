@@ -24,6 +24,8 @@ static constexpr int kPlanMaxWindow = 64;
 static constexpr int kPlanMaxSeqLen = 32768;
 static constexpr int kPlanMaxPoolKernel = 63;
 static constexpr int kPlanFusedMaxLen = 8192;   // longest head of narrow workgroups of the fused kernels
+// Most workgroups of 256 threads in a launch: HIP takes fewer than 2^32 threads.
+static constexpr int64_t kPlanMaxWorkgroups = 0xffffffffLL / 256;
 static constexpr int kPlanClasses = 5;          // query-tile counts 0..4 (0: no queries)
 
 // LDS of a head's per-token words: stage[0 .. n) plus room in front and behind
