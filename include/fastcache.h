@@ -20,7 +20,11 @@
  * its block tables.  The library's scratch buffers (kept lists, saved ids,
  * un-pooled scores, descriptors) grow on demand: a call that needs more than
  * any earlier one waits for the device, frees and reallocates BEFORE it queues
- * anything; calls whose needs were met before are fully asynchronous.  A call
+ * anything; calls whose needs were met before are asynchronous, but for one wait:
+ * the descriptors of many requests (more than some 150 single tokens, chunks or
+ * prompts, more than 10 KB of a compression's) go through one pinned buffer of the
+ * pool, and the next such call waits on the host until they have been copied, that
+ * is for the work on the stream before them.  A call
  * that is captured into a graph allocates nothing: it returns FC_EINVAL unless
  * a call of its size came before (on single tokens, chunks and prompts up to
  * some 150 requests, which fit a kernel's arguments, none has to, nor before
