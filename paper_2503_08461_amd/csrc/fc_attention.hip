@@ -119,7 +119,7 @@ __device__ __forceinline__ void lds_barrier() {
 // 32-key subtiles of fp16 rows in LDS, from row `at` of tiles k and v.
 template <int D>
 struct F16Keys {
-  static constexpr bool kPairedSlabs = false;
+  static constexpr bool kPairedSlabs = false;  // (of the queries that its slabs meet: take_queries)
   const half8 *k, *v;
   int at;
   // A operands: of a slab of K (lane: key, eight channels by half), ...
@@ -740,7 +740,7 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
     request(0);
     if constexpr (SRC == ATTN_E4M3) put8(0);
     // (the second tile's room is free until the first barrier)
-    rows.template take_queries<false>(sm + 2 * kTile + wave * 32 * D / 8);
+    rows.template take_queries<F16Keys<D>::kPairedSlabs>(sm + 2 * kTile + wave * 32 * D / 8);
   }
   int t = 0;
   for (; t + 1 < n_full; t += 2) {
@@ -878,7 +878,7 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
         request_v(i);
         lds_reads_done();
         if (i == 0) {  // through the second tile's room
-          rows.template take_queries<true>(sm_k + 2 * kTile);
+          rows.template take_queries<E4m3Keys<D>::kPairedSlabs>(sm_k + 2 * kTile);
           lds_reads_done();
         }
       }
@@ -933,7 +933,7 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
       look_up(0);
       request_k(0);
       lds_reads_done();  // (K's loads stay ahead of V's, as the waits count on)
-      rows.template take_queries<false>(sm_k + kTile);  // through V's room
+      rows.template take_queries<F16Keys<D>::kPairedSlabs>(sm_k + kTile);  // through V's room
       lds_reads_done();
       request_v(0);
     }

@@ -122,7 +122,6 @@ int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, in
       if (2 * seg <= longest) {
         l.seg_blocks = (int)seg;
         l.n_seg = decode_segments(longest, l.seg_blocks);
-        while (l.n_seg > room) l.n_seg = decode_segments(longest, ++l.seg_blocks);
         states_left -= l.state_rows * n_q_heads * l.n_seg;
       }
     }
