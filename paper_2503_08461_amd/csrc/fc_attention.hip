@@ -1029,7 +1029,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, Reqs re
 // common maximum and sum by itself, a segment a lane.  Latency bounds it: 4-5 us for 1536 rows of up
 // to three segments, 5.5-7 for 5000 rows.
 static constexpr int kMaxHeadSegments = kPlanMaxSeqLen / kPlanBlockSize / kPlanMinSegment;
-static_assert(kMaxHeadSegments <= 128, "two segments a lane");
+static_assert(kMaxHeadSegments <= 64, "a segment a lane");
 
 template <int D, typename Reqs>
 __global__ __launch_bounds__(256) void attention_merge_kernel(AttnParams p, AttnLaunchView l, Reqs reqs) {
@@ -1044,23 +1044,18 @@ __global__ __launch_bounds__(256) void attention_merge_kernel(AttnParams p, Attn
   const float* states = l.states + (int64_t)blockIdx.x * l.n_seg * kWords;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  float m[2], f[2], mm = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    m[k] = lane + 64 * k < n_seg ? states[(size_t)(lane + 64 * k) * kWords + D] : -INFINITY;
-    mm = fmaxf(mm, m[k]);
-  }
+  const float m = lane < n_seg ? states[(size_t)lane * kWords + D] : -INFINITY;
+  float mm = m;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor(mm, d));
-#pragma unroll
-  for (int k = 0; k < 2; ++k) f[k] = m[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - mm);
-  const float zz = wave_sum(f[0] + f[1]);
+  const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mm);
+  const float zz = wave_sum(f);
   float o[kPer] = {};
   for (int i = wave; i < n_seg; i += 16)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {  // (four loads on their way)
       const int at = min(i + 4 * j, n_seg - 1);
-      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(at < 64 ? f[0] : f[1]), at & 63));
+      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), at));
 #pragma unroll
       for (int c = 0; c < kPer; ++c)
         o[c] += states[(size_t)at * kWords + lane * kPer + c] * (i + 4 * j < n_seg ? fi : 0.f);
