@@ -71,7 +71,7 @@ enum { FC_DTYPE_F16 = 0, FC_DTYPE_E4M3 = 1 };
  *           into it; token j of a request lives in block table[j / 16],
  *           slot j % 16, for every layer and head.
  * kv_bytes  size of that memory; must be >= n_layers*n_blocks*2*n_heads*16*
- *           head_dim*2.
+ *           head_dim*2 (8-bit rows: *(head_dim+1)).
  * block_size must be 16, head_dim 64 or 128, dtype FC_DTYPE_F16 or
  * FC_DTYPE_E4M3 (8-bit rows, see "The 8-bit pool" below: another layout, and
  * not every call takes such a pool).
@@ -116,8 +116,8 @@ int fc_pool_free(fc_pool* pool, const int32_t* dev_ids, int n_blocks, void* stre
  *     double free, a foreign or free id, or a duplicate gives FC_EINVAL and
  *     nothing is changed.  These calls then wait for the device once (the
  *     verdict is read on the host), so they are no longer asynchronous;
- *   - every pop (fc_pool_alloc, the new blocks of a compression, fc_append_batch)
- *     marks its blocks handed out and raises a flag if one of them was not
+ *   - every pop (fc_pool_alloc, the new blocks of a compression, fc_append_batch,
+ *     fc_extend_batch) marks its blocks handed out and raises a flag if one of them was not
  *     free; fc_pool_export_state reports the flag as FC_EDEVICE.
  * Switching the checks on takes what is on the free stack as free and every
  * other block as handed out (so does fc_pool_import_state); it waits for the
