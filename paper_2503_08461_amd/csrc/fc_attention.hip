@@ -19,7 +19,7 @@
 //
 // Two parts of one launch: many rows (prompts, long chunks; bound by the matrix cores) and few
 // rows of a head and request, up to 32 (single tokens, short chunks; bound by memory).  (Two launches:
-// a mixed batch of 24 chunks of 1-512 tokens 269 us, one 240, now 231; the few rows' workgroups fill what the
+// a mixed batch of 24 chunks of 1-512 tokens 269 us, one 240, now 230; the few rows' workgroups fill what the
 // many rows' leave.)
 
 #include <algorithm>
@@ -649,16 +649,17 @@ __device__ __forceinline__ BufferPtr rows_at(const _Float16* from, int stride, i
 // ---------------------------------------------------------------------------
 // Many rows: four wavefronts of 32 rows over the same keys, 64 at a time.  Two tiles in LDS:
 // while one is worked on, each wavefront brings in 16 keys of the next, straight from memory to
-// LDS (32 prompts of 600-1200 tokens, 32 heads: 392 us, through registers 741; now 359).  Where
-// its rows see all of a tile, the loop without a mask; the border is the wavefront's own (with the
-// workgroup's 373).
+// LDS (32 prompts of 600-1200 tokens, 32 heads: 392 us, through registers 741; now 358-397, by
+// process and box).  Where its rows see all of a tile, the loop without a mask; the border is the
+// wavefront's own (with the workgroup's 373 beside 359).
 //
 // 64 KB of LDS: two workgroups a CU, the softmax of one beside the products of the other.  Measured,
-// 128 channels: prompts of 5900-7040 tokens, 8 heads of K and V and 32 query heads, 1.03 PFLOP/s (a
-// library product of 8192^3: 1.12); 2048 tokens behind 28 000 1.03; 32 prompts of 600-1200, 32 heads,
-// 0.61; one of 640, 17.3 us.  Long prompts are bound by the card's power: the matrix pipes are busy
-// for 60 % of the cycles, at 1.6 GHz, and with zeros for random numbers the same work runs at 1.4
-// PFLOP/s.  Short ones (not 40 % of the cycles) by what does not overlap: queries, the first tile,
+// 128 channels: prompts of 5900-7040 tokens, 8 heads of K and V and 32 query heads, 0.82-1.04 PFLOP/s by
+// box (a library product of 8192^3: 1.09-1.18); 2048 tokens behind 30 000 0.82-1.05, over 8 bits (keys
+// through registers) 1.02 beside 1.05; 32 prompts of 600-1200, 32 heads, 0.56-0.61; one of 640, 17-19
+// us; 64 channels: the 2048 tokens 0.85.  Long prompts are bound by the card's power: the matrix pipes
+// are busy for 60 % of the cycles, at 1.6 GHz, and with zeros for random numbers the same work runs at
+// 1.2-1.4 PFLOP/s.  Short ones (34 % of the cycles) by what does not overlap: queries, the first tile,
 // the tiles at the mask and the results of two workgroups at a time.
 // ---------------------------------------------------------------------------
 template <int D, int SRC, bool kSplit, typename Reqs>
@@ -793,9 +794,10 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
 //
 // Every row of K and V is read once per head, whatever the group.  Measured, 128 channels, fp16:
 // single tokens of 48 caches of 1280-7040, 8 heads, 4 query heads each, 5.9 TB/s with the store
-// and the merge (135 us, 124 at the card's 6.4 TB/s for reads); 16 caches of 8192, 32 heads, 6.4.
-// 8-bit: 5.7-6.2 TB/s at those sizes, the conversion to fp16 beside the loads; 5 drafted tokens of 32
-// caches of 256-1408: 19 us and 6 for the merge, latency.
+// and the merge (135 us, 124 at the card's 6.4 TB/s for reads); 32 heads of their own, 6.4 (491 us).
+// 8-bit: 32 heads 6.2 TB/s (259 us), 8 heads of four 4.8 with the merge (84 us of attention and merge,
+// 62 at 6.4), the conversion to fp16 beside the loads (16 vector instructions a product, fp16 rows
+// 6.6); 5 drafted tokens of 32 caches of 256-1408: 19 us and 6 for the merge, latency.
 // ---------------------------------------------------------------------------
 
 // Bytes of one row of K or V in the LDS of such a wavefront.

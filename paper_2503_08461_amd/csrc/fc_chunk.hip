@@ -50,8 +50,9 @@ static void with_chunk_reqs(const ChunkReq* on_device, const ChunkReqs& inline_r
 // ---------------------------------------------------------------------------
 // store: workgroup = new token; its 2 * n_heads rows of one layer go to its slot.  D / 8
 // neighbouring lanes have a row, 16 bytes each; for the 8-bit pool they find the row's
-// maximum among themselves.  Memory bounds it: 3 us for 48 tokens of 8 heads (latency), 17-19 us
-// for 2293 tokens of 32 heads (75 MB read and written, 4.3 TB/s).
+// maximum among themselves.  Memory bounds it: 3-5 us for 48 tokens of 8 heads (latency), 17-19 us
+// for 2293 tokens of 32 heads (75 MB read and written, 4.3 TB/s), 48 us for 8377 (275 MB, 5.7); 8-bit
+// 16-18 us (56 MB, 3.3 TB/s) and 45-47 us (206 MB, 4.5).
 // ---------------------------------------------------------------------------
 template <int D, bool kE4M3, typename Reqs>
 __global__ __launch_bounds__(256) void store_chunk_kernel(StoreParams p, Reqs reqs) {

@@ -80,6 +80,16 @@ int plan_store_units(ChunkPlan* plan) {
 int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, int64_t max_states,
                    ChunkPlan* plan, AttnLaunch launches[kAttnKinds]) {
   for (int s = 0; s < kAttnKinds; ++s) launches[s] = AttnLaunch();
+  // Few rows of a head are those of one tile that shares the keys.  What 33-127 rows cost as many
+  // rows / as two to four tiles of few, each of which reads the keys again (the attention, us):
+  //                                            fp16             8-bit
+  //   40 rows, 48 caches of 1280-7040, 8 heads  179 / 195        138 / 110
+  //   120 rows                                  189 / 332        165 / 180
+  //   40 rows, 32 of 256-1408, 8 heads         31.6 / 31.9      34.4 / 22.6
+  //   96 rows                                  49.2 / 43.0      50.1 / 33.5
+  //   40 rows, 1 of 30000, 8 heads             31.6 / 45.3      29.7 / 31.0
+  //   40 rows, 24 of 256-4000, 32 heads         169 / 222        124 / 128
+  // (one border for both: 8-bit caches of grouped heads would gain with one of two tiles)
   for (const ChunkReq& q : plan->reqs)
     launches[(int64_t)q.n_new * group <= kFlatRows ? 1 : 0].reqs.push_back(q);
   int64_t states_left = may_split ? max_states : 0;
