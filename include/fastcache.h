@@ -115,7 +115,8 @@ int fc_pool_free(fc_pool* pool, const int32_t* dev_ids, int n_blocks, void* stre
  *     about to push: inside the pool, currently handed out, named once.  A
  *     double free, a foreign or free id, or a duplicate gives FC_EINVAL and
  *     nothing is changed.  These calls then wait for the device once (the
- *     verdict is read on the host), so they are no longer asynchronous;
+ *     verdict is read on the host), so they are no longer asynchronous, and
+ *     FC_EINVAL where they are captured into a graph;
  *   - every pop (fc_pool_alloc, the new blocks of a compression, fc_append_batch,
  *     fc_extend_batch) marks its blocks handed out and raises a flag if one of them was not
  *     free; fc_pool_export_state reports the flag as FC_EDEVICE.

@@ -96,7 +96,24 @@ int fixed_scratch_of_current_device(unsigned char** out) {
 
 namespace {
 int release_verdict(fc_pool* p, hipStream_t stream, const char* what);
+
+// A call that is captured into a graph takes its descriptors as arguments: they are captured
+// by value, the staging buffer would be read again at every replay.
+bool capturing(hipStream_t stream) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(stream, &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();  // (the default stream, while another one is captured)
+  return false;
 }
+// It allocates nothing: what it needs has to be there, and stays for its replays.
+int refuse_growing_capture() {
+  return fail(FC_EINVAL, "a captured call needs one of its size before the capture: it cannot allocate its scratch memory");
+}
+// It waits for nothing.
+int refuse_checked_capture() {
+  return fail(FC_EINVAL, "a call that releases blocks cannot be captured with ownership checks on: they wait for the device");
+}
+}  // namespace
 
 namespace {
 
@@ -277,6 +294,7 @@ int fc_pool_free(fc_pool* p, const int32_t* dev_ids, int n, void* stream) {
   if (p->debug_checks) {
     // every id in range, handed out, and named once: checked before anything is pushed
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (capturing(st)) return refuse_checked_capture();
     FC_HIP(launch_zero_ints(p->check_word, 1, st));
     FC_HIP(launch_owner_check_ids(dev_ids, n, p->n_blocks, p->owner, p->check_word, false, st));
     if (int rc = release_verdict(p, st, "fc_pool_free")) {
@@ -461,18 +479,6 @@ int upload_meta_pinned(fc_pool* p, const char* image, size_t bytes, char* dev_ds
   p->meta_pending = true;
   return FC_OK;
 }
-// A call that is captured into a graph takes arguments: they are captured by value,
-// the staging buffer would be read again at every replay.
-bool capturing(hipStream_t stream) {
-  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(stream, &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
-  (void)hipGetLastError();  // (the default stream, while another one is captured)
-  return false;
-}
-// ... and allocates nothing: what it needs has to be there, and stays for its replays.
-int refuse_growing_capture() {
-  return fail(FC_EINVAL, "a captured call needs one of its size before the capture: it cannot allocate its scratch memory");
-}
 int upload_meta(fc_pool* p, const char* image, size_t bytes, char* dev_dst, bool no_alloc,
                 hipStream_t stream) {
   if (no_alloc || bytes <= kMaxArgumentMeta || capturing(stream))
@@ -539,6 +545,7 @@ int compress_batch_impl(fc_pool* p, int32_t* dev_block_tables, int max_blocks_pe
   if (plan_compress(pv, a, &plan) != PLAN_OK) return fail(plan.code, "%s", plan.message);
   const int n_comp = (int)plan.descs.size();
   if (n_comp == 0) return FC_OK;
+  if (p->debug_checks && capturing(stream)) return refuse_checked_capture();
 
   // ---- launches: the fused kernels, or (FC_SCORE_TWO_PASS) the separate ones ---
   // or, with few long heads, kernels that split them over workgroups
@@ -946,6 +953,7 @@ int fc_compress_batch_mlp(fc_pool* p, int32_t* dev_block_tables, int max_blocks_
     return fail(plan.code, "%s", plan.message);
   const int n_comp = (int)plan.descs.size();
   if (n_comp == 0) return FC_OK;
+  if (p->debug_checks && capturing(stream)) return refuse_checked_capture();
 
   int rc;
   const size_t n_ids = (size_t)plan.total_old + plan.total_new;

@@ -123,5 +123,23 @@ int main() {
   weights("weights_replaced_again");
   call("mlp", "mlp_grows", false, 4000, 800);
   destroy("mlp_end");
+
+  // ownership checks read their verdict on the host
+  create();
+  weights("weights_checked");
+  call("compress", "checked_eager", false, 64, 800);
+  call("mlp", "checked_mlp_eager", false, 64, 800);
+  fc_set_debug_checks(p, 1);
+  g_launched.clear();
+  g_made = g_freed = 0;
+  call("compress", "checked_first", true, 64, 800);
+  call("mlp", "checked_mlp", true, 64, 800);
+  fc_pool_import_state_dev(p, somewhere<int32_t>(), 100, nullptr);
+  g_launched.clear();
+  g_capturing = true;
+  line("checked_free", fc_pool_free(p, somewhere<int32_t>(), 5, nullptr));
+  g_capturing = false;
+  printf("checked_free_left %d 1\n", fc_pool_num_free(p) == 100);
+  destroy("checked_end");
   return 0;
 }

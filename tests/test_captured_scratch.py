@@ -41,6 +41,12 @@ def test_a_capture_that_would_have_to_allocate(steps, what):
         assert steps[what + "_left"] == ["1", "1"]
 
 
+@pytest.mark.parametrize("what", ["checked_first", "checked_mlp", "checked_free"])
+def test_a_capture_with_ownership_checks(steps, what):
+    """The checks wait for the device: refused before anything is queued."""
+    assert _counts(steps, what) == (-1, 0, 0) and steps[what][3:] == [] and steps[what + "_left"] == ["1", "1"]
+
+
 @pytest.mark.parametrize("what", ["lse_captured", "fused_noalloc", "fused_captured", "split_captured", "separate_captured",
                                   "mlp_captured"])
 def test_a_capture_that_finds_what_it_needs(steps, what):
