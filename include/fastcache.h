@@ -549,7 +549,8 @@ int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_b
  * head h reads head h / (n_q_heads / n_heads) of K and V.
  *   out = softmax(scale * K q) . V      (fp16 rows, fp32 sums, fp16 out;
  *                                        scale <= 0 means 1/sqrt(head_dim))
- * The soft-max numerators are rounded to fp16 for the product with V.  A key
+ * The soft-max numerators are rounded to fp16 for the product with V (a result that
+ * this would carry past fp16's largest number is that number).  A key
  * that a row does not see has no influence on it, whatever its K and V hold.
  *   q         packed rows, n_q_heads heads
  *   out       packed rows, n_q_heads heads, written (no two rows share memory)
