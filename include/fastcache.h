@@ -553,7 +553,8 @@ int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_b
  * this would carry past fp16's largest number is that number).  A key
  * that a row does not see has no influence on it, whatever its K and V hold.
  *   q         packed rows, n_q_heads heads
- *   out       packed rows, n_q_heads heads, written (no two rows share memory)
+ *   out       packed rows, n_q_heads heads, written (no two rows share memory);
+ *             may be q itself, and overlaps nothing else that the call reads
  *   dev_lse   NULL, or fp32 [n_req][n_layers][n_q_heads][window] (4-byte
  *             aligned): the natural log-sum-exp of scale * q.k over the keys it
  *             sees for each of the last `window` new tokens, entry window - 1 being the
@@ -568,7 +569,8 @@ int fc_quantise_batch(fc_pool* dst, const int32_t* dev_dst_tables, int dst_max_b
  *             neither read nor written, and its dtype does not matter.
  *
  * Captured into a graph: a replay works on the lengths of the capture and on what
- * the tables, rows and pool hold then.
+ * the tables, rows and pool hold then.  fc_extend_batch pops once, at its capture;
+ * a replay writes the ids that lie at the same places of the free stack by then.
  *
  * All four are asynchronous on `stream`; the attentions may split long caches
  * over workgroups, whose states lie in memory of the pool.  They are not part
