@@ -160,7 +160,7 @@ def cpu_baseline(dw, seconds=15.0, seed=0):
         units += 1
     one = {"value": token_heads / n_lh / spent, "unit": "tokens/s", "cores": 1,
            "sample": "%d units = %d token-heads in %.1f s" % (units, token_heads, spent)}
-    # ---- all cores (the GPU machine gives a one-GPU job 16 of them, whatever nproc says)
+    # ---- all cores (a one-GPU job has 16 of them here, whatever nproc says)
     n_workers = max(1, min(16, len(os.sched_getaffinity(0))))
     spent, token_heads, units = 0.0, 0, 0
     with mp.get_context("spawn").Pool(n_workers) as pool:

@@ -24,8 +24,8 @@
  * the descriptors of many requests (more than some 150 single tokens, chunks or
  * prompts, more than 10 KB of a compression's) go through one pinned buffer of the
  * pool, and the next such call waits on the host until they have been copied, that
- * is for the work on the stream before them.  A call
- * that is captured into a graph allocates nothing: it returns FC_EINVAL unless
+ * is for the work on the stream before them.
+ * A call that is captured into a graph allocates nothing: it returns FC_EINVAL unless
  * a call of its size came before (on single tokens, chunks and prompts up to
  * some 150 requests, which fit a kernel's arguments, none has to, nor before
  * fc_compress_batch_noalloc).  The memory that it uses stays until the pool is
@@ -118,8 +118,8 @@ int fc_pool_free(fc_pool* pool, const int32_t* dev_ids, int n_blocks, void* stre
  *     verdict is read on the host), so they are no longer asynchronous, and
  *     FC_EINVAL where they are captured into a graph;
  *   - every pop (fc_pool_alloc, the new blocks of a compression, fc_append_batch,
- *     fc_extend_batch) marks its blocks handed out and raises a flag if one of them was not
- *     free; fc_pool_export_state reports the flag as FC_EDEVICE.
+ *     fc_extend_batch) marks its blocks handed out and raises a flag if one of
+ *     them was not free; fc_pool_export_state reports the flag as FC_EDEVICE.
  * Switching the checks on takes what is on the free stack as free and every
  * other block as handed out (so does fc_pool_import_state); it waits for the
  * device.  Off by default: block ids are then only clamped into the pool.
@@ -434,8 +434,8 @@ const char* fc_last_error(void);
  * L_r + 1 before the call returns; the device work is asynchronous on stream.
  *   dev_new_kv  dev, fp16 [n_req][n_layers][2][n_heads][head_dim], 16-byte aligned
  * FC_EINVAL: L_r < 0 or >= FC_MAX_SEQ_LEN, table row full (L_r/16 >=
- * max_blocks_per_req), 2^24 or more requests times layers; FC_ENOMEM: more blocks needed than are free.  Nothing
- * is modified on error.
+ * max_blocks_per_req), 2^24 or more requests times layers; FC_ENOMEM: more
+ * blocks needed than are free.  Nothing is modified on error.
  *
  * fc_decode_attention: the single-query attention of one decode step over
  * the paged cache, for every request, layer and head:

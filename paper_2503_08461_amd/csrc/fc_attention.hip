@@ -670,12 +670,12 @@ __device__ __forceinline__ BufferPtr rows_at(const _Float16* from, int stride, i
 // Many rows: four wavefronts of 32 rows over the same keys, 64 at a time.  Two tiles in LDS:
 // while one is worked on, each wavefront brings in 16 keys of the next, straight from memory to
 // LDS (32 prompts of 600-1200 tokens, 32 heads: 392 us, through registers 741; now 358-397, by
-// process and box).  Where its rows see all of a tile, the loop without a mask; the border is the
+// process and card).  Where its rows see all of a tile, the loop without a mask; the border is the
 // wavefront's own (with the workgroup's 373 beside 359).
 //
 // 64 KB of LDS: two workgroups a CU, the softmax of one beside the products of the other.  Measured,
 // 128 channels: prompts of 5900-7040 tokens, 8 heads of K and V and 32 query heads, 0.82-1.04 PFLOP/s by
-// box (a library product of 8192^3: 1.09-1.18); 2048 tokens behind 30 000 0.82-1.05, over 8 bits (keys
+// card (a library product of 8192^3: 1.09-1.18); 2048 tokens behind 30 000 0.82-1.05, over 8 bits (keys
 // through registers) 1.02 beside 1.05; 32 prompts of 600-1200, 32 heads, 0.56-0.61; one of 640, 17-19
 // us; 64 channels: the 2048 tokens 0.85.  Long prompts are bound by the card's power: the matrix pipes
 // are busy for 60 % of the cycles, at 1.6 GHz, and with zeros for random numbers the same work runs at

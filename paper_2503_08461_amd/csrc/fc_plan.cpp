@@ -296,7 +296,7 @@ std::vector<FusedLaunch> plan_fused_launches(const PoolView& pool, const Compres
   // workgroups would leave most of the chip's wavefronts idle.  One launch per
   // shape, whatever windows its requests have: a launch per window class ends in a
   // tail of its own (24 requests with windows 1..64, 2 layers of 32 heads: 776 us
-  // as four launches, 661-715 as one, by box).
+  // as four launches, 661-715 as one, by card).
   FusedLaunch wide, narrow;
   auto add = [](FusedLaunch& to, const std::vector<int32_t>& list) {
     to.units.insert(to.units.end(), list.begin(), list.end());
