@@ -52,7 +52,7 @@ typedef struct fc_pool fc_pool; /* opaque, owned by the library */
 
 enum { FC_OK = 0, FC_EINVAL = -1, FC_ENOMEM = -2, FC_EDEVICE = -3 };
 enum { FC_METHOD_NONE = 0, FC_METHOD_SNAPKV = 1, FC_METHOD_KNORM = 2, FC_METHOD_STREAMING = 3 };
-enum { FC_DTYPE_F16 = 0, FC_DTYPE_E4M3 = 1 };
+enum { FC_DTYPE_F16 = 0, FC_DTYPE_E4M3 = 1, FC_DTYPE_E2M1 = 3 };
 
 #define FC_BLOCK_SIZE 16      /* tokens per pool block (the only supported value) */
 #define FC_MAX_WINDOW 64      /* largest observation window */
@@ -71,10 +71,10 @@ enum { FC_DTYPE_F16 = 0, FC_DTYPE_E4M3 = 1 };
  *           into it; token j of a request lives in block table[j / 16],
  *           slot j % 16, for every layer and head.
  * kv_bytes  size of that memory; must be >= n_layers*n_blocks*2*n_heads*16*
- *           head_dim*2 (8-bit rows: *(head_dim+1)).
- * block_size must be 16, head_dim 64 or 128, dtype FC_DTYPE_F16 or
- * FC_DTYPE_E4M3 (8-bit rows, see "The 8-bit pool" below: another layout, and
- * not every call takes such a pool).
+ *           head_dim*2 (8-bit rows: *(head_dim+1); 4-bit ones: *head_dim*17/32).
+ * block_size must be 16, head_dim 64 or 128, dtype FC_DTYPE_F16,
+ * FC_DTYPE_E4M3 or FC_DTYPE_E2M1 (8- and 4-bit rows, see "The 8-bit pool" and "The
+ * 4-bit pool" below: other layouts, and not every call takes such a pool).
  *
  * The free list is a LIFO stack of block ids held in device memory; a fresh
  * pool holds stack[i] = n_blocks-1-i, top = n_blocks, so that the first
@@ -496,16 +496,35 @@ int fc_decode_attention_kept(fc_pool* pool, const int32_t* dev_block_tables,
  * Calls that take such a pool: fc_pool_* (all), fc_set_debug_checks,
  * fc_append_batch (the new fp16 rows are quantised as they are written),
  * fc_decode_attention (reads the 8-bit rows), fc_extend_batch, fc_store_chunk,
- * fc_chunk_attention, fc_prefill_attention and fc_quantise_batch.  The
- * compression calls, fc_window_lse and fc_decode_attention_kept return
+ * fc_chunk_attention, fc_prefill_attention, fc_quantise_batch, fc_rotate_store_chunk,
+ * fc_block_bounds and fc_sparse_attention.  The compression calls, fc_window_lse and fc_decode_attention_kept return
  * FC_EINVAL: select and compact in an fp16 pool, then quantise what is kept.
  *
+ * The 4-bit pool: the same in a quarter of the bytes and a little more.  A row's
+ * channels 32 g .. 32 g + 31 are a group, held as e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4,
+ * 6: codes 0 to 7, the sign is the fourth bit) times one power of two 2^e per group.
+ * e is the smallest integer with max |x_c| <= 6 * 2^e over the group, at least -23
+ * and at most 13, and the codes are x_c / 2^e rounded to the nearest e2m1 number,
+ * ties to the even code, at most 6 (with e = 13 magnitudes from 49152 on are that).
+ * Every value a group stands for is an fp16 number.  A group that holds a channel
+ * that is infinite or not a number is not a number throughout (exponent byte 255,
+ * codes 0).  A value differs from the written one by at most 2^-2 of it, or
+ * 2^-2 * 2^e where it is smaller than 2^e.
+ *
+ * Memory (kv_base of a pool of FC_DTYPE_E2M1, 1-byte elements):
+ *     kv[layer][block]{ codes[kv: 0=K, 1=V][head][slot 0..15][head_dim / 2],
+ *                       exponents[kv][head][slot][head_dim / 32] } (e + 127, unsigned)
+ * the code of channel 2 i in the low half of a row's byte i, that of 2 i + 1 in the
+ * high one: 17 * n_heads * head_dim bytes per layer and block.  What is said of the
+ * 8-bit pool and of pools of FC_DTYPE_E4M3 below holds for this one: the same calls take
+ * it, the same ones refuse it.
+ *
  * fc_quantise_batch: the cached rows of a batch, from a pool of FC_DTYPE_F16 to
- * one of FC_DTYPE_E4M3 with the same layers, heads and head_dim.  For every
+ * one of FC_DTYPE_E4M3 or FC_DTYPE_E2M1 with the same layers, heads and head_dim.  For every
  * request r (with host_enable[r] != 0 if it is given) tokens 0..L_r-1 of all
  * layers and heads are read through dev_src_tables and written through
  * dev_dst_tables; slots behind them are left as they are.  No block is popped or
- * released: fc_extend_batch on the 8-bit pool (lengths 0, n_new = L_r) hands out
+ * released: fc_extend_batch on that pool (lengths 0, n_new = L_r) hands out
  * the blocks before, fc_pool_free releases the old ones afterwards.
  * Asynchronous on `stream`.
  * FC_EINVAL: dtypes or geometries that do not match, a length outside
@@ -603,6 +622,86 @@ int fc_chunk_attention(fc_pool* pool, int layer, const int32_t* dev_block_tables
 int fc_prefill_attention(fc_pool* pool, int layer, const int32_t* host_seq_lens, const fc_rows* q,
                          const fc_rows* k, const fc_rows* v, int n_q_heads, const fc_rows* out,
                          float* dev_lse, int window, int n_req, float scale, void* stream);
+
+/*
+ * fc_store_chunk for a model with rotary positions: the new tokens' q and k are
+ * rotated by their positions on the way, k and v written to the pool.  One call
+ * instead of a rotation of q, one of k, and the store; the positions are an argument
+ * because a compressed cache is shorter than the position of its next token.
+ *
+ * fc_rotation   table: dev, fp32 [n_positions][2][rotary_dim / 2], 16-byte aligned: the
+ *               cosines, then the sines, of a position's angles, one a pair.  Channels
+ *               0 .. rotary_dim - 1 of a row are rotated, the others copied; channels c and
+ *               c + rotary_dim / 2 are pair c, or, interleaved, 2 c and 2 c + 1.
+ *               rotary_dim: a multiple of 16, 16 .. head_dim.
+ *                 (a, b) -> (a cos - b sin, b cos + a sin)
+ *               in 64 bits, rounded to fp32 and then to fp16; in a pool of fewer
+ *               bits the fp16 row is quantised.
+ * host_positions  host, int32 [n_req]: position of each request's first new token, the
+ *               others follow it; entries of requests without new tokens are not looked
+ *               at.  NULL: L_r - n_new_r, as in a cache that holds every token.
+ * q, q_out      packed rows, n_q_heads heads (any number up to n_heads * FC_MAX_GROUP; 0: none,
+ *               q and q_out are not looked at).  q_out is written (no two rows share memory); it
+ *               may be q itself, and overlaps nothing else that the call reads.
+ * Everything else, with the errors, as for fc_store_chunk; additionally FC_EINVAL: a NULL or
+ * misaligned table, a rotary_dim that is none of the above, a token whose position is
+ * negative or not in the table.  A captured call's replays work on the capture's positions.
+ */
+typedef struct fc_rotation {
+  const float* table; /* dev */
+  int n_positions;
+  int rotary_dim;
+  int interleaved; /* 0, or not 0 */
+} fc_rotation;
+int fc_rotate_store_chunk(fc_pool* pool, int layer, const int32_t* dev_block_tables,
+                          int max_blocks_per_req, const int32_t* host_seq_lens,
+                          const int32_t* host_n_new, const int32_t* host_positions,
+                          const fc_rotation* rotation, const fc_rows* q, int n_q_heads,
+                          const fc_rows* q_out, const fc_rows* k, const fc_rows* v, int n_req,
+                          void* stream);
+
+/*
+ * Attention over selected blocks: for caches that are kept whole, a step that reads only
+ * the blocks of 16 tokens that matter to its queries (the pool's blocks are its
+ * unit: "KV-cache Memory Pool" paragraph; nothing is evicted, the next query selects anew).
+ *
+ * fc_block_bounds: for the blocks that hold the last n_new_r tokens of every request, one
+ * layer, all heads: the smallest and the largest value of each channel of K over the
+ * block's tokens (those before L_r; of rows of fewer bits, what they stand for).  Called after
+ * fc_store_chunk or fc_rotate_store_chunk with its arguments, or with n_new = L_r for
+ * whole caches (after a prefill, a compression, a copy into fewer bits).
+ *   dev_bounds  dev, fp16 [n_layers][n_blocks][n_heads][2: smallest, largest][head_dim],
+ *               16-byte aligned, caller-owned: 1/16 of an fp16 pool.  The entries of other blocks
+ *               are left as they are.  A channel with a key that is not a number is none.
+ *
+ * fc_sparse_attention: fc_chunk_attention in which every new token reads, of the blocks that
+ * it sees, at most n_select, for each head of K and V its own choice:
+ *   - the block that holds the token itself, always;
+ *   - of the others the n_select - 1 with the best scores, ties to the lower entry of the
+ *     table.  The score of a block is the largest over the query heads that
+ *     share the head of  sum_c max(q_c * smallest_c, q_c * largest_c),  which no logit of the
+ *     block exceeds (scale aside).  It is summed in 64 bits; a score that is not a
+ *     number counts as larger than all others.
+ * All of them where they are no more than n_select.  Over what it reads the
+ * attention is that of fc_chunk_attention, whose arguments these are.
+ *   dev_bounds    as fc_block_bounds left it (the token's own block is read whatever its entry)
+ *   n_select      1 .. FC_MAX_SEQ_LEN / 16
+ *   dev_selected  NULL, or dev, int32 [T][n_heads][n_select] (4-byte aligned): the table entries
+ *                 that were read, ascending, -1 behind the last one
+ * The order of scores and the selection lie in scratch memory of the pool, which grows on demand.
+ *
+ * Both are asynchronous on `stream` and not part of the kernel times.  FC_EINVAL as for
+ * fc_store_chunk and fc_chunk_attention; n_select outside its range, NULL or misaligned
+ * dev_bounds, 2^24 or more blocks (fc_block_bounds) or tokens times heads.
+ */
+int fc_block_bounds(fc_pool* pool, int layer, const int32_t* dev_block_tables,
+                    int max_blocks_per_req, const int32_t* host_seq_lens,
+                    const int32_t* host_n_new, void* dev_bounds, int n_req, void* stream);
+int fc_sparse_attention(fc_pool* pool, int layer, const int32_t* dev_block_tables,
+                        int max_blocks_per_req, const int32_t* host_seq_lens,
+                        const int32_t* host_n_new, const void* dev_bounds, int n_select,
+                        const fc_rows* q, int n_q_heads, const fc_rows* out,
+                        int32_t* dev_selected, int n_req, float scale, void* stream);
 
 /*
  * Host-side scheduler of the compress queue (Algorithm 1, ServeRequests:

@@ -181,13 +181,11 @@ int fc_pool_create(fc_pool** out, void* kv_base, size_t kv_bytes, int n_blocks, 
   if (!kv_base || (reinterpret_cast<uintptr_t>(kv_base) & 255))
     return fail(FC_EINVAL, "kv_base must be a 256-byte aligned device pointer");
   if (block_size != FC_BLOCK_SIZE) return fail(FC_EINVAL, "block_size must be 16");
-  if (dtype != FC_DTYPE_F16 && dtype != FC_DTYPE_E4M3)
-    return fail(FC_EINVAL, "dtype must be FC_DTYPE_F16 or FC_DTYPE_E4M3");
+  if (dtype != FC_DTYPE_F16 && dtype != FC_DTYPE_E4M3 && dtype != FC_DTYPE_E2M1)
+    return fail(FC_EINVAL, "dtype must be FC_DTYPE_F16, FC_DTYPE_E4M3 or FC_DTYPE_E2M1");
   if (head_dim != 64 && head_dim != 128) return fail(FC_EINVAL, "head_dim must be 64 or 128");
   if (n_blocks < 1 || n_layers < 1 || n_heads < 1) return fail(FC_EINVAL, "bad pool geometry");
-  // (an 8-bit row is a code a channel and one exponent)
-  const size_t row_bytes = dtype == FC_DTYPE_E4M3 ? head_dim + 1 : 2 * head_dim;
-  const size_t need = (size_t)n_layers * n_blocks * 2 * n_heads * FC_BLOCK_SIZE * row_bytes;
+  const size_t need = (size_t)n_layers * n_blocks * block_bytes(dtype, n_heads, head_dim);
   if (kv_bytes < need)
     return fail(FC_EINVAL, "kv_bytes %zu is smaller than the pool geometry needs (%zu)", kv_bytes,
                 need);
@@ -251,6 +249,7 @@ int fc_pool_destroy(fc_pool* p) {
   if (p->raw_scores.data) (void)hipFree(p->raw_scores.data);
   if (p->kept.data) (void)hipFree(p->kept.data);
   if (p->ids.data) (void)hipFree(p->ids.data);
+  if (p->sparse.data) (void)hipFree(p->sparse.data);
   for (void* old : p->retired) (void)hipFree(old);
   if (p->decode_partial) (void)hipFree(p->decode_partial);
   if (p->error_flag) (void)hipFree(p->error_flag);
@@ -776,6 +775,14 @@ int fc::meta_to_device(fc_pool* p, const void* descs, size_t n_bytes, const void
   return upload_meta_pinned(p, image.data(), bytes, p->dev_meta, stream);
 }
 
+int fc::scratch_for(fc_pool* p, Scratch<char>* s, size_t bytes, hipStream_t stream) {
+  const bool captured = capturing(stream);
+  if (captured && bytes > s->cap) return refuse_growing_capture();
+  if (int rc = grow(p, s, bytes)) return rc;
+  if (captured) s->captured = true;
+  return FC_OK;
+}
+
 extern "C" {
 
 int fc_compress_batch(fc_pool* p, int32_t* dev_block_tables, int max_blocks_per_req,
@@ -1083,7 +1090,7 @@ int pass_decode_reqs(fc_pool* p, const std::vector<DecodeReq>& reqs, DecodeParam
 DecodeParams decode_params(fc_pool* p) {
   DecodeParams dp = {};
   dp.kv = p->kv;
-  dp.e4m3 = p->dtype == FC_DTYPE_E4M3 ? 1 : 0;
+  dp.e4m3 = p->dtype == FC_DTYPE_E4M3 ? ROWS_E4M3 : p->dtype == FC_DTYPE_E2M1 ? ROWS_E2M1 : ROWS_F16;
   dp.n_blocks = p->n_blocks;
   dp.n_layers = p->n_layers;
   dp.n_heads = p->n_heads;

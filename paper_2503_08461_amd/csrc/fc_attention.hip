@@ -1,5 +1,5 @@
 // Attention of many query rows: whole prompts (K and V as packed rows) and chunks of new
-// tokens over the paged cache (fp16 or 8-bit), causal, with grouped heads.
+// tokens over the paged cache (fp16, 8-bit or 4-bit), causal, with grouped heads.
 //
 // A row is one (new token, query head); the rows that read the same head of K and V lie one
 // after the other, row = token * group + head of the group, and are worked on together: a
@@ -26,7 +26,7 @@
 #include <type_traits>
 
 #include "fc_chunk_plan.h"
-#include "fc_e4m3.h"
+#include "fc_e2m1.h"
 
 namespace fc {
 
@@ -535,6 +535,43 @@ struct Block8 {
   }
 };
 
+// Sixteen keys of a 4-bit pool through registers.  A lane has 16 bytes, a group of 32 channels of one
+// row; at 64 channels K's rows are with the first half of the wavefront and V's with the other.
+template <int D>
+struct Block4 {
+  static constexpr int kLanes = D / kE2m1Group;  // lanes of a row
+  static constexpr bool kBoth = D == 128;        // every lane has a part of K and one of V
+  uint4v c[kBoth ? 2 : 1];
+  uint32_t e[kBoth ? 2 : 1];
+  __device__ __forceinline__ void request(const uint8_t* block, int n_heads, int head) {
+    const int lane = threadIdx.x & 63;
+    const size_t codes = (size_t)n_heads * 8 * D, exps = (size_t)n_heads * D / 2;  // of K, and of V
+    const int at = kBoth ? lane : lane & 31;  // = row * kLanes + group
+    const size_t v = kBoth ? 0 : lane >> 5;
+    const uint8_t* c_from = block + v * codes + (size_t)head * 8 * D + at * 16;
+    const uint8_t* e_from = block + 2 * codes + v * exps + (size_t)head * D / 2 + at;
+#pragma unroll
+    for (int i = 0; i < (kBoth ? 2 : 1); ++i) {
+      c[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4v*>(c_from + i * codes));
+      e[i] = e_from[i * exps];
+    }
+  }
+  __device__ __forceinline__ void put(half8* sm_k, half8* sm_v, int at) const {
+    const int lane = threadIdx.x & 63;
+    const int r = at + (kBoth ? lane : lane & 31) / kLanes, first = lane % kLanes * 4;
+#pragma unroll
+    for (int i = 0; i < (kBoth ? 2 : 1); ++i) {
+      const float scale = e4m3_scale(e[i]);
+      const bool is_v = kBoth ? i == 1 : lane >= 32;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        half8* to = is_v ? sm_v + v_chunk<D>(r, first + w) : sm_k + k_chunk<D>(r, first + w);
+        *to = e2m1_values(c[i][w], scale);
+      }
+    }
+  }
+};
+
 // The same as codes for a wavefront that works on them alone: they go straight to LDS and
 // become fp16 numbers as they are read.  Rows of D bytes, 16-byte chunks permuted for K's
 // reads (32 rows at one chunk) and V's transposing ones (eight rows, of two blocks of
@@ -649,6 +686,11 @@ struct E4m3Keys {
   }
 };
 
+// The request's block table, or its head's own one.
+__device__ __forceinline__ const int32_t* table_of(const AttnParams& p, const ChunkReq& rq, int head) {
+  const int own = p.table_heads > 1 ? head : 0;
+  return p.block_tables + ((size_t)rq.table_row * p.table_heads + own) * p.max_blocks;
+}
 // Block b of the request's cache (behind the last one: the last one, whose rows nobody sees there).
 __device__ __forceinline__ int block_id(const AttnParams& p, const int32_t* table, int b, int nb) {
   return clamp_block(load_uniform(table + min(b, nb - 1)), p.n_blocks);
@@ -704,7 +746,7 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
   Rows32<D> rows;
   rows.start();
 
-  const int32_t* table = SRC == ATTN_ROWS ? nullptr : p.block_tables + (size_t)w.rq.table_row * p.max_blocks;
+  const int32_t* table = SRC == ATTN_ROWS ? nullptr : table_of(p, w.rq, head);
   const int k_stride = SRC == ATTN_ROWS ? (int)p.k.token_stride : D, v_stride = SRC == ATTN_ROWS ? (int)p.v.token_stride : D;
   const BlockLoader<D, false> loader(2 * k_stride, 2 * v_stride);
   half8* to_mine = sm + wave * 16 * D / 8;
@@ -718,7 +760,8 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
   } else if (n_tiles > 0) {
     next_id = block_id(p, table, block, w.nb);
   }
-  Block8<D> b8;
+  constexpr bool kCodes = SRC == ATTN_E4M3 || SRC == ATTN_E2M1;  // through registers
+  std::conditional_t<SRC == ATTN_E2M1, Block4<D>, Block8<D>> b8;
   auto request = [&](int t) {
     half8* to = to_mine + (t & 1) * 2 * kTile;
     if constexpr (SRC == ATTN_ROWS) {
@@ -732,7 +775,8 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
         loader.k(f16_block<D>(p, next_id, head, 0), to);
         loader.v(f16_block<D>(p, next_id, head, 1), to + kTile);
       } else {
-        b8.request(static_cast<const uint8_t*>(p.kv) + (size_t)next_id * e4m3_block_bytes(p.n_heads, D), p.n_heads, head);
+        const size_t bytes = SRC == ATTN_E2M1 ? e2m1_block_bytes(p.n_heads, D) : e4m3_block_bytes(p.n_heads, D);
+        b8.request(static_cast<const uint8_t*>(p.kv) + (size_t)next_id * bytes, p.n_heads, head);
       }
       block += kKeys / 16;
       next_id = block_id(p, table, block, w.nb);
@@ -744,11 +788,11 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
   };
   // tile t, the next one on its way: work(tile's place in LDS)
   auto step = [&](int t, auto work) {
-    if constexpr (SRC != ATTN_E4M3) wait_loads<0>();
+    if constexpr (!kCodes) wait_loads<0>();
     lds_barrier();  // tile t is there, the one before has been read
     if (t + 1 < n_tiles) request(t + 1);
     work();
-    if constexpr (SRC == ATTN_E4M3) {
+    if constexpr (kCodes) {
       if (t + 1 < n_tiles) put8(t + 1);
     }
   };
@@ -759,7 +803,7 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
     const GroupRows from(p.q, w.rq, p, head);
     rows.request_queries([&](int r) { return from.at(lane_row(p, row0 + r, w.n_rows)); });
     request(0);
-    if constexpr (SRC == ATTN_E4M3) put8(0);
+    if constexpr (kCodes) put8(0);
     // (the second tile's room is free until the first barrier)
     rows.template take_queries<F16Keys<D>::kPairedSlabs>(sm + 2 * kTile + wave * 32 * D / 8);
   }
@@ -854,7 +898,7 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
   const GroupRows from(p.q, w.rq, p, head), to(p.out, w.rq, p, head);
   rows.request_queries([&](int r) { return from.at(lane_row(p, row0 + r, w.n_rows)); });
 
-  const int32_t* table = SRC == ATTN_ROWS ? nullptr : p.block_tables + (size_t)w.rq.table_row * p.max_blocks;
+  const int32_t* table = SRC == ATTN_ROWS ? nullptr : table_of(p, w.rq, head);
   half8* sm_k = sm + wave * 2 * kStages * kTile;
   int ids[2] = {0, 0};
   auto block_of = [&](int i, int j) { return (w.key_begin >> 4) + 2 * (wave + 4 * i) + j; };
@@ -925,6 +969,32 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
       lds_reads_done();
       request_v(i + kStages);
     };
+    int i = 0;
+    for (; i < full; ++i) step(i, std::false_type());
+    for (; i < mine; ++i) step(i, std::true_type());
+  } else if constexpr (SRC == ATTN_E2M1) {
+    // The next tile's codes in registers while one is worked on as fp16 rows in LDS.
+    const F16Keys<D> keys{sm_k, sm_k + kTile, 0};
+    Block4<D> next[2];
+    auto request = [&](int i) {
+      look_up(i);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        next[j].request(static_cast<const uint8_t*>(p.kv) + (size_t)ids[j] * e2m1_block_bytes(p.n_heads, D), p.n_heads, head);
+      requests_first();
+    };
+    auto step = [&](int i, auto masked_) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) next[j].put(sm_k, sm_k + kTile, 16 * j);
+      wave_lds_barrier();
+      request(i + 1);  // (behind the last one: the last block again)
+      rows.template attend<1, decltype(masked_)::value>(keys, key_of(i), last_key, p.scale_log2e, [] {}, [] {});
+      wave_lds_barrier();
+    };
+    if (mine > 0) {
+      request(0);
+      rows.template take_queries<F16Keys<D>::kPairedSlabs>(sm_k);
+    }
     int i = 0;
     for (; i < full; ++i) step(i, std::false_type());
     for (; i < mine; ++i) step(i, std::true_type());
@@ -1126,8 +1196,10 @@ void launch_shape(const AttnParams& p, const Reqs& reqs, hipStream_t s) {
     launch_source<D, ATTN_ROWS>(p, reqs, s);
   else if (p.source == ATTN_F16)
     launch_source<D, ATTN_F16>(p, reqs, s);
-  else
+  else if (p.source == ATTN_E4M3)
     launch_source<D, ATTN_E4M3>(p, reqs, s);
+  else
+    launch_source<D, ATTN_E2M1>(p, reqs, s);
 }
 
 template <typename Reqs>
@@ -1141,6 +1213,8 @@ hipError_t allow_lds_with() {  // (with the static words more than 64 KB)
   allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_F16, true, Reqs>));
   allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_E4M3, false, Reqs>));
   allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_E4M3, true, Reqs>));
+  allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_E2M1, false, Reqs>));
+  allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_E2M1, true, Reqs>));
   return e;
 }
 

@@ -1,9 +1,9 @@
 // Chunks of new tokens on their way into the pool: the blocks they need, their K and V rows,
-// and the copy of a cache from an fp16 pool into an 8-bit one.  All of it is memory traffic.
+// and the copy of a cache from an fp16 pool into one of 8 or 4 bits.  All of it is memory traffic.
 
 #include <type_traits>
 
-#include "fc_e4m3.h"
+#include "fc_e2m1.h"
 
 namespace fc {
 
@@ -54,7 +54,7 @@ static void with_chunk_reqs(const ChunkReq* on_device, const ChunkReqs& inline_r
 // for 2293 tokens of 32 heads (75 MB read and written, 4.3 TB/s), 48 us for 8377 (275 MB, 5.7); 8-bit
 // 16-18 us (56 MB, 3.3 TB/s) and 45-47 us (206 MB, 4.5).
 // ---------------------------------------------------------------------------
-template <int D, bool kE4M3, typename Reqs>
+template <int D, int kFormat, typename Reqs>
 __global__ __launch_bounds__(256) void store_chunk_kernel(StoreParams p, Reqs reqs) {
   constexpr int PPR = D / 8;
   const ChunkReq rq = reqs.req[request_of_unit(reqs, p.n_req, blockIdx.x)];
@@ -68,15 +68,7 @@ __global__ __launch_bounds__(256) void store_chunk_kernel(StoreParams p, Reqs re
     const RowsView& from = rh < p.n_heads ? p.k : p.v;
     const int head = rh < p.n_heads ? rh : rh - p.n_heads;
     const half8 x = load_half8(from.data + (int64_t)blockIdx.x * from.token_stride + head * from.head_stride + piece * 8);
-    if constexpr (kE4M3) {
-      uint8_t* block = static_cast<uint8_t*>(p.kv) + (size_t)blk * e4m3_block_bytes(p.n_heads, D);
-      const int e = e4m3_exponent(row_max_u32<PPR>(finite_max(x)));
-      *reinterpret_cast<uint2v*>(block + ((size_t)rh * 16 + slot) * D + piece * 8) = e4m3_codes(x, e);
-      if (piece == 0) block[(size_t)n_rows * 16 * D + rh * 16 + slot] = (uint8_t)e;
-    } else {
-      _Float16* block = static_cast<_Float16*>(p.kv) + (size_t)blk * n_rows * 16 * D;
-      store_half8(block + ((size_t)rh * 16 + slot) * D + piece * 8, x);
-    }
+    write_piece<D, kFormat>(p.kv, blk, p.n_heads, rh, slot, piece, x);
   }
 }
 
@@ -85,14 +77,10 @@ hipError_t launch_store_chunk(const StoreParams& p, const ChunkReqs& inline_reqs
   if (p.head_dim != 64 && p.head_dim != 128) return hipErrorInvalidValue;
   with_chunk_reqs(p.reqs, inline_reqs, [&](const auto& reqs) {
     using Reqs = std::decay_t<decltype(reqs)>;
-    if (p.head_dim == 128 && p.e4m3)
-      store_chunk_kernel<128, true, Reqs><<<p.n_rows, 256, 0, s>>>(p, reqs);
-    else if (p.head_dim == 128)
-      store_chunk_kernel<128, false, Reqs><<<p.n_rows, 256, 0, s>>>(p, reqs);
-    else if (p.e4m3)
-      store_chunk_kernel<64, true, Reqs><<<p.n_rows, 256, 0, s>>>(p, reqs);
-    else
-      store_chunk_kernel<64, false, Reqs><<<p.n_rows, 256, 0, s>>>(p, reqs);
+    auto launch = [&](auto dim, auto format) {
+      store_chunk_kernel<decltype(dim)::value, decltype(format)::value, Reqs><<<p.n_rows, 256, 0, s>>>(p, reqs);
+    };
+    with_row_format(p.head_dim, p.e4m3, launch);
   });
   return hipGetLastError();
 }
@@ -103,7 +91,7 @@ hipError_t launch_store_chunk(const StoreParams& p, const ChunkReqs& inline_reqs
 // a line at a time, which the L2 joins).  Memory bounds it: 64 caches of 256-1408 tokens, 32 heads
 // of 128 channels, 4 layers, 1060 us = 4.85 TB/s read and written, what a large copy reaches here.
 // ---------------------------------------------------------------------------
-template <int D, typename Reqs>
+template <int D, int kFormat, typename Reqs>
 __global__ __launch_bounds__(256) void quantise_kernel(QuantiseParams p, Reqs reqs) {
   constexpr int PPR = D / 8;
   const int layer = blockIdx.x / p.n_units;
@@ -115,14 +103,11 @@ __global__ __launch_bounds__(256) void quantise_kernel(QuantiseParams p, Reqs re
   const int slots = min(16, rq.seq_len - b * 16);
   const int n_rows = 2 * p.n_heads;
   const _Float16* src = p.src + ((size_t)layer * p.src_blocks + from) * n_rows * 16 * D;
-  uint8_t* dst = p.dst + ((size_t)layer * p.dst_blocks + to) * e4m3_block_bytes(p.n_heads, D);
+  uint8_t* dst = p.dst + (size_t)layer * p.dst_blocks * (kFormat == ROWS_E2M1 ? e2m1_block_bytes(p.n_heads, D) : e4m3_block_bytes(p.n_heads, D));
   for (int i = threadIdx.x; i < n_rows * 16 * PPR; i += 256) {
     const int row = i / PPR, piece = i % PPR;  // row = (kv * n_heads + head) * 16 + slot
     if ((row & 15) >= slots) continue;         // (all lanes of the row)
-    const half8 x = load_half8_nt(src + (size_t)row * D + piece * 8);
-    const int e = e4m3_exponent(row_max_u32<PPR>(finite_max(x)));
-    *reinterpret_cast<uint2v*>(dst + (size_t)row * D + piece * 8) = e4m3_codes(x, e);
-    if (piece == 0) dst[(size_t)n_rows * 16 * D + row] = (uint8_t)e;
+    write_piece<D, kFormat>(dst, to, p.n_heads, row >> 4, row & 15, piece, load_half8_nt(src + (size_t)row * D + piece * 8));
   }
 }
 
@@ -132,10 +117,11 @@ hipError_t launch_quantise(const QuantiseParams& p, const ChunkReqs& inline_reqs
   const unsigned grid = (unsigned)p.n_units * p.n_layers;
   with_chunk_reqs(p.reqs, inline_reqs, [&](const auto& reqs) {
     using Reqs = std::decay_t<decltype(reqs)>;
-    if (p.head_dim == 128)
-      quantise_kernel<128, Reqs><<<grid, 256, 0, s>>>(p, reqs);
-    else
-      quantise_kernel<64, Reqs><<<grid, 256, 0, s>>>(p, reqs);
+    auto launch = [&](auto dim, auto format) {
+      if constexpr (decltype(format)::value != ROWS_F16)
+        quantise_kernel<decltype(dim)::value, decltype(format)::value, Reqs><<<grid, 256, 0, s>>>(p, reqs);
+    };
+    with_row_format(p.head_dim, p.e2m1 ? ROWS_E2M1 : ROWS_E4M3, launch);
   });
   return hipGetLastError();
 }

@@ -148,6 +148,64 @@ int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, in
   return PLAN_OK;
 }
 
+int plan_positions(const int32_t* positions, int n_positions, ChunkPlan* plan) {
+  for (ChunkReq& q : plan->reqs) {
+    const int first = positions ? positions[q.table_row] : q.seq_len - q.n_new;
+    if (first < 0 || first > n_positions - q.n_new)
+      return fail(plan, PLAN_EINVAL, "request %d: %d tokens from position %d on, the table has %d", q.table_row, q.n_new, first, n_positions);
+    q.state_off = first;
+  }
+  return PLAN_OK;
+}
+
+int plan_bounds(ChunkPlan* plan) {
+  plan->n_rows = 0;
+  for (ChunkReq& q : plan->reqs) {
+    q.row_off = (q.seq_len - q.n_new) / kPlanBlockSize;
+    q.unit_start = (int32_t)plan->n_rows;
+    plan->n_rows += blocks_for(q.seq_len) - q.row_off;
+    if (plan->n_rows > kPlanMaxWorkgroups) return fail(plan, PLAN_EINVAL, "batch too large for one launch");
+  }
+  return PLAN_OK;
+}
+
+int plan_sparse(const PoolView& pool, int n_cu, int n_select, const ChunkPlan& chunk, SparsePlan* plan) {
+  *plan = SparsePlan();
+  if (n_select < 1 || n_select > kPlanMaxSeqLen / kPlanBlockSize)
+    return fail(plan, PLAN_EINVAL, "n_select %d outside 1..%d", n_select, kPlanMaxSeqLen / kPlanBlockSize);
+  if (chunk.n_rows * pool.n_heads > kPlanMaxWorkgroups) return fail(plan, PLAN_EINVAL, "batch too large for one launch");
+  int longest = 0;
+  int64_t scored = 0;  // blocks, of one head
+  for (const ChunkReq& q : chunk.reqs)
+    for (int i = 0; i < q.n_new; ++i) {
+      const int seen = q.seq_len - q.n_new + i + 1, nb = blocks_for(seen), row = q.row_off + i;
+      plan->tokens.push_back({q.table_row, seen, 1, row, 0, 0});
+      // (whole blocks, but for the token's own, the last one)
+      const int read = (std::min(nb, n_select) - 1) * kPlanBlockSize + (seen - 1) % kPlanBlockSize + 1;
+      plan->attention.reqs.push_back({row, read, 1, row, 0, 0});
+      if (nb > n_select) {
+        longest = std::max(longest, nb);
+        scored += nb - 1;
+      }
+    }
+  plan->attention.n_rows = chunk.n_rows;
+  plan->key_stride = std::max(longest - 1, 1);
+  // Few heads leave CUs free, and one draws only so much: their scores are made by as many
+  // workgroups as fill the card, in a launch of its own.
+  const int64_t heads = chunk.n_rows * pool.n_heads;
+  if (longest > 64 && heads < 2 * (int64_t)std::max(n_cu, 1)) {
+    const int64_t wanted = 4 * (int64_t)std::max(n_cu, 1);
+    plan->part_blocks = (int)std::max<int64_t>(32, (scored * pool.n_heads + wanted - 1) / wanted);
+    for (ChunkReq& t : plan->tokens) {
+      t.unit_start = (int32_t)plan->n_units;
+      const int nb = blocks_for(t.seq_len);
+      if (nb > n_select) plan->n_units += (nb - 1 + plan->part_blocks - 1) / plan->part_blocks;
+    }
+    if (plan->n_units * pool.n_heads > kPlanMaxWorkgroups) return fail(plan, PLAN_EINVAL, "batch too large for one launch");
+  }
+  return PLAN_OK;
+}
+
 int plan_quantise(int n_req, int dst_max_blocks, int src_max_blocks, const int32_t* seq_lens,
                   const int32_t* enable, ChunkPlan* plan) {
   *plan = ChunkPlan();

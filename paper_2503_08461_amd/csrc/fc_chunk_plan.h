@@ -51,6 +51,26 @@ struct AttnLaunch {
 int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, int64_t max_states,
                    ChunkPlan* plan, AttnLaunch launches[kAttnKinds]);
 
+// fc_rotate_store_chunk: plan->reqs get the position of their first new token (state_off), by
+// default that of the cache.  FC_EINVAL (plan->code) for one outside the table.
+int plan_positions(const int32_t* positions, int n_positions, ChunkPlan* plan);
+
+// fc_block_bounds: a unit is a block that holds new tokens, the first one's number in the table is
+// row_off.  n_rows becomes the number of units.
+int plan_bounds(ChunkPlan* plan);
+
+// fc_sparse_attention.
+struct SparsePlan {
+  int code = PLAN_OK;
+  char message[256] = "";
+  std::vector<ChunkReq> tokens;  // one a new token, row_off its packed row, unit_start its first part
+  ChunkPlan attention;           // the same as requests of their own, of the blocks that they read
+  int part_blocks = 0;           // 0: a workgroup scores and selects, else blocks a workgroup that scores
+  int64_t n_units = 0;           // parts of all tokens
+  int key_stride = 0;            // scores kept of a token's head
+};
+int plan_sparse(const PoolView& pool, int n_cu, int n_select, const ChunkPlan& chunk, SparsePlan* plan);
+
 // fc_quantise_batch: a unit is a block of a request.
 int plan_quantise(int n_req, int dst_max_blocks, int src_max_blocks, const int32_t* seq_lens,
                   const int32_t* enable, ChunkPlan* plan);

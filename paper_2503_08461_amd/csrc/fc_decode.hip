@@ -7,7 +7,7 @@
 
 #include <type_traits>
 
-#include "fc_e4m3.h"
+#include "fc_e2m1.h"
 
 namespace fc {
 
@@ -21,9 +21,9 @@ namespace fc {
 // Reqs (here and below): DecodeReqs, the requests in the arguments, or DecodeReqList,
 // on the device.  Kernels of their own: 3.6 KB of arguments that nobody reads cost a
 // launch of small caches several us.
-// kE4M3: an 8-bit pool (fc_e4m3.h); the lanes of a row find its largest magnitude among
-// themselves and write codes and the row's exponent.
-template <int D, bool kE4M3, typename Reqs>
+// kFormat: how the pool holds its rows; of 8 and 4 bits the lanes of a row (of a group of channels)
+// find its largest magnitude among themselves and write codes and the exponent.
+template <int D, int kFormat, typename Reqs>
 __global__ __launch_bounds__(kThreads) void append_kernel(DecodeParams p, Reqs reqs) {
   const int r = blockIdx.x / p.n_layers;
   const int layer = blockIdx.x - r * p.n_layers;
@@ -44,25 +44,14 @@ __global__ __launch_bounds__(kThreads) void append_kernel(DecodeParams p, Reqs r
     blk = clamp_block(row[L >> 4], p.n_blocks);
   }
   constexpr int PPR = D / 8;  // 16-byte pieces of a row
-  const size_t blk_stride = (size_t)2 * p.n_heads * 16 * D;
   const _Float16* src = p.new_kv + ((size_t)rq.table_row * p.n_layers + layer) * 2 * p.n_heads * D;
-  if constexpr (kE4M3) {
-    uint8_t* block = reinterpret_cast<uint8_t*>(p.kv) +
-                     ((size_t)layer * p.n_blocks + blk) * e4m3_block_bytes(p.n_heads, D);
-    for (int i = threadIdx.x; i < 2 * p.n_heads * PPR; i += kThreads) {  // (whole rows)
-      const int rh = i / PPR, piece = i - rh * PPR;
-      const half8 x = load_half8(src + (size_t)rh * D + piece * 8);
-      const int e = e4m3_exponent(row_max_u32<PPR>(finite_max(x)));
-      const size_t at = (size_t)rh * 16 + (L & 15);
-      *reinterpret_cast<uint2v*>(block + at * D + piece * 8) = e4m3_codes(x, e);
-      if (piece == 0) block[blk_stride + at] = (uint8_t)e;
-    }
-    return;
-  }
-  _Float16* dst = p.kv + ((size_t)layer * p.n_blocks + blk) * blk_stride + (size_t)(L & 15) * D;
-  for (int i = threadIdx.x; i < 2 * p.n_heads * PPR; i += kThreads) {
-    const int rh = i / PPR, piece = i - rh * PPR;  // rh = kv * n_heads + head
-    store_half8(dst + (size_t)rh * 16 * D + piece * 8, load_half8(src + (size_t)rh * D + piece * 8));
+  const size_t block = kFormat == ROWS_E4M3   ? e4m3_block_bytes(p.n_heads, D)
+                       : kFormat == ROWS_E2M1 ? e2m1_block_bytes(p.n_heads, D)
+                                              : (size_t)2 * p.n_heads * 16 * D * sizeof(_Float16);
+  void* blocks = reinterpret_cast<char*>(p.kv) + (size_t)layer * p.n_blocks * block;
+  for (int i = threadIdx.x; i < 2 * p.n_heads * PPR; i += kThreads) {  // (whole rows)
+    const int rh = i / PPR, piece = i - rh * PPR;                      // rh = kv * n_heads + head
+    write_piece<D, kFormat>(blocks, blk, p.n_heads, rh, L & 15, piece, load_half8(src + (size_t)rh * D + piece * 8));
   }
 }
 
@@ -81,14 +70,9 @@ hipError_t launch_append(const DecodeParams& p, const DecodeReqs& inline_reqs, h
   const unsigned grid = (unsigned)p.n_req * p.n_layers;
   with_reqs(p, inline_reqs, [&](const auto& reqs) {
     using Reqs = std::decay_t<decltype(reqs)>;
-    if (p.head_dim == 128 && p.e4m3)
-      append_kernel<128, true, Reqs><<<grid, kThreads, 0, s>>>(p, reqs);
-    else if (p.head_dim == 128)
-      append_kernel<128, false, Reqs><<<grid, kThreads, 0, s>>>(p, reqs);
-    else if (p.e4m3)
-      append_kernel<64, true, Reqs><<<grid, kThreads, 0, s>>>(p, reqs);
-    else
-      append_kernel<64, false, Reqs><<<grid, kThreads, 0, s>>>(p, reqs);
+    with_row_format(p.head_dim, p.e4m3, [&](auto dim, auto format) {
+      append_kernel<decltype(dim)::value, decltype(format)::value, Reqs><<<grid, kThreads, 0, s>>>(p, reqs);
+    });
   });
   return hipGetLastError();
 }
@@ -266,27 +250,28 @@ __global__ __launch_bounds__(kThreads) void decode_attention_kernel(DecodeParams
 }
 
 // ---------------------------------------------------------------------------
-// The same over an 8-bit pool: a lane has 16 channels of a row (16 bytes), so D / 16
-// neighbouring lanes a row and 1024 / D rows a load instruction.  Codes become fp32 numbers
-// (exactly); the row's power of two multiplies the key's logit and the value's weight.  HBM
-// bounds it where the call has heads to offer (48 caches of 1280-7040, 2 layers: 6.4 TB/s);
+// The same over a pool of 8 or 4 bits: a lane has 16 bytes of a row, so D / 16 (D / 32)
+// neighbouring lanes a row and 1024 / D (2048 / D) rows a load instruction, of 4 bits and 64
+// channels two blocks.  Codes become fp32 numbers (exactly); a row's power of two multiplies the
+// key's logit and the value's weight, a group's, which is the lane's own, goes into the conversion.
+// 8 bits: HBM bounds it where the call has heads to offer (48 caches of 1280-7040, 2 layers: 6.4 TB/s);
 // with a block in the time of half a one the loads' latency shows earlier, so a wavefront asks
 // for the next block before it works on this one also over whole heads (4 caches of 1000-1200,
 // 32 heads: 27.2 -> 15.6 us), and its rows' states are joined by lane exchanges, not in LDS
 // (3 caches of 2000-2400, 8 heads of 64 channels: 16 -> 9.7).
 // ---------------------------------------------------------------------------
 
-// sum over the LPR neighbouring lanes of a row (4 or 8), in every one of them
+// sum over the LPR neighbouring lanes of a row (2, 4 or 8), in every one of them
 template <int LPR>
 __device__ __forceinline__ float short_row_sum(float s) {
   s += from_lane<0xB1>(s);
-  s += from_lane<0x4E>(s);
+  if constexpr (LPR >= 4) s += from_lane<0x4E>(s);
   if constexpr (LPR == 8) s += from_lane<0x141>(s);
   return s;
 }
 
 // A lane's value and that of the lane kStep away (in either order), without LDS: halves of the
-// wavefront or rows of 16 change places, or the row is rotated.  Joining by 4 (where a row of
+// wavefront or rows of 16 change places, or the row is rotated.  Joining by 2 and 4 (where a row of
 // the cache has that few lanes), 8, 16 and 32 leaves the whole in every lane.
 template <int kStep>
 __device__ __forceinline__ void two_lanes(float v, float& a, float& b) {
@@ -304,7 +289,9 @@ __device__ __forceinline__ void two_lanes(float v, float& a, float& b) {
   }
 }
 
-__device__ __forceinline__ void values_of(uint4v codes, float (&f)[16]) {
+// What a lane's 16 bytes of a row stand for: 16 channels of 8 bits, without the row's power of two,
+// or a group of 32 of 4 bits, with the group's.
+__device__ __forceinline__ void values_of(uint4v codes, float, float (&f)[16]) {
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[w], false);
@@ -315,12 +302,20 @@ __device__ __forceinline__ void values_of(uint4v codes, float (&f)[16]) {
     f[4 * w + 3] = hi[1];
   }
 }
+__device__ __forceinline__ void values_of(uint4v codes, float scale, float (&f)[32]) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) e2m1_floats(codes[w], scale, f + 8 * w);
+}
 
-template <int D, int W, bool kCut, typename Reqs>
-__global__ __launch_bounds__(64 * W) void decode_attention_e4m3_kernel(DecodeParams p, Reqs reqs) {
-  constexpr int LPR = D / 16;
+template <int D, int kFormat, int W, bool kCut, typename Reqs>
+__global__ __launch_bounds__(64 * W) void decode_attention_codes_kernel(DecodeParams p, Reqs reqs) {
+  constexpr bool k4 = kFormat == ROWS_E2M1;
+  constexpr int CPL = k4 ? 32 : 16;  // channels of a lane
+  constexpr int LPR = D / CPL;
   constexpr int RPI = 64 / LPR;
-  constexpr int IPB = 16 / RPI;
+  constexpr int BPT = RPI > 16 ? RPI / 16 : 1;  // blocks of a tile
+  constexpr int IPT = 16 * BPT / RPI;           // load instructions of a tile
+  constexpr int kRowBytes = D * 16 / CPL;
   const int n_lh = p.n_layers * p.n_heads;
   const int unit = kCut ? blockIdx.x % (p.n_req * n_lh) : blockIdx.x;
   const int seg = kCut ? blockIdx.x / (p.n_req * n_lh) : 0;
@@ -338,67 +333,92 @@ __global__ __launch_bounds__(64 * W) void decode_attention_e4m3_kernel(DecodePar
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = lane / LPR;    // which row of a load instruction
-  const int piece = lane % LPR;  // which 16 channels
+  const int piece = lane % LPR;  // which channels
   float* out = p.out + ((size_t)rq.table_row * n_lh + lh) * D;
 
-  const _Float16* qp = p.q + ((size_t)rq.table_row * n_lh + lh) * D + piece * 16;
-  float qf[16];
+  const _Float16* qp = p.q + ((size_t)rq.table_row * n_lh + lh) * D + piece * CPL;
+  float qf[CPL];
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const half8 qh = load_half8(qp + 8 * half);
+  for (int part = 0; part < CPL / 8; ++part) {
+    const half8 qh = load_half8(qp + 8 * part);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) qf[8 * half + e] = (float)qh[e] * p.scale_log2e;
+    for (int e = 0; e < 8; ++e) qf[8 * part + e] = (float)qh[e] * p.scale_log2e;
   }
   const int32_t* row = p.block_tables + (size_t)rq.table_row * p.max_blocks;
-  const size_t blk_stride = e4m3_block_bytes(p.n_heads, D);
-  const size_t v_off = (size_t)p.n_heads * 16 * D;
+  const size_t blk_stride = k4 ? e2m1_block_bytes(p.n_heads, D) : e4m3_block_bytes(p.n_heads, D);
+  const size_t v_off = (size_t)p.n_heads * 16 * kRowBytes;
   const uint8_t* base = reinterpret_cast<const uint8_t*>(p.kv) + (size_t)layer * p.n_blocks * blk_stride;
-  const size_t code_at = ((size_t)head * 16 + grp) * D + piece * 16;
-  const size_t exp_at = 2 * v_off + (size_t)head * 16 + grp;
+  // of the lane's row and channels in a block: codes, exponent (of 4 bits the lane's own group's)
+  const int in_block = BPT > 1 ? grp & 15 : grp;
+  constexpr int kExps = k4 ? D / kE2m1Group : 1;  // exponents of a row
+  const size_t code_at = ((size_t)head * 16 + in_block) * kRowBytes + piece * 16;
+  const size_t exp_at = 2 * v_off + ((size_t)head * 16 + in_block) * kExps + (k4 ? piece : 0);
 
-  float m = -INFINITY, z = 0.f, acc[16];
+  float m = -INFINITY, z = 0.f, acc[CPL];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  for (int e = 0; e < CPL; ++e) acc[e] = 0.f;
   struct Rows {
-    uint4v k[IPB], v[IPB];
-    uint32_t ke[IPB], ve[IPB];
+    uint4v k[IPT], v[IPT];
+    uint32_t ke[IPT], ve[IPT];
   };
-  auto fetch = [&](int b, Rows& x) {
+  auto fetch = [&](int t, Rows& x) {
+    // (behind the last block: the last one, whose rows are not looked at there)
+    const int b = BPT > 1 ? min(b0 + t * BPT + (grp >> 4), b1 - 1) : b0 + t;
     const uint8_t* block = base + (size_t)clamp_block(row[b], p.n_blocks) * blk_stride;
 #pragma unroll
-    for (int i = 0; i < IPB; ++i) {
-      x.k[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4v*>(block + code_at + (size_t)i * RPI * D));
-      x.v[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4v*>(block + code_at + v_off + (size_t)i * RPI * D));
-      x.ke[i] = block[exp_at + i * RPI];
-      x.ve[i] = block[exp_at + (size_t)p.n_heads * 16 + i * RPI];
+    for (int i = 0; i < IPT; ++i) {
+      x.k[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4v*>(block + code_at + (size_t)i * RPI * kRowBytes));
+      x.v[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4v*>(block + code_at + v_off + (size_t)i * RPI * kRowBytes));
+      x.ke[i] = block[exp_at + i * RPI * kExps];
+      x.ve[i] = block[exp_at + (size_t)p.n_heads * 16 * kExps + i * RPI * kExps];
     }
   };
-  auto attend = [&](int b, const Rows& x) {
+  const int last = kCut ? min(L, b1 * 16) : L;  // (a tile of two blocks may reach into the next segment)
+  auto attend = [&](int t, const Rows& x) {
 #pragma unroll
-    for (int i = 0; i < IPB; ++i) {
-      float f[16];
-      values_of(x.k[i], f);
+    for (int i = 0; i < IPT; ++i) {
+      float f[CPL];
+      values_of(x.k[i], e4m3_scale(x.ke[i]), f);
       float s = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s += qf[e] * f[e];
-      s = short_row_sum<LPR>(s) * e4m3_scale(x.ke[i]);
-      const int tok = b * 16 + i * RPI + grp;
-      if (tok < L) {  // the whole lane group takes the same branch
-        const float mn = fmaxf(m, s);
-        const float a = __builtin_amdgcn_exp2f(m - mn);  // 0 for the first token (m = -inf)
-        const float w = __builtin_amdgcn_exp2f(s - mn);
-        z = z * a + w;
-        const float wv = w * e4m3_scale(x.ve[i]);
-        values_of(x.v[i], f);
+      for (int e = 0; e < CPL; ++e) s += qf[e] * f[e];
+      s = short_row_sum<LPR>(s);
+      if constexpr (!k4) s *= e4m3_scale(x.ke[i]);
+      const int tok = (b0 + t * BPT) * 16 + i * RPI + grp;
+      if (tok < last) {  // the whole lane group takes the same branch
+        if constexpr (k4) {
+          // the maximum follows when it has fallen 2^8 behind: half of the bytes leave no time for
+          // a multiplication of every sum for every row
+          if (__any(s > m + 8.f)) {
+            const float mn = fmaxf(m, s);
+            const float a = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);  // 0 for the first token (m = -inf)
+            z *= a;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[e] = acc[e] * a + wv * f[e];
-        m = mn;
+            for (int e = 0; e < CPL; ++e) acc[e] *= a;
+            m = mn;
+          }
+          const float w = __builtin_amdgcn_exp2f(s - (m == -INFINITY ? 0.f : m));
+          z += w;
+          values_of(x.v[i], e4m3_scale(x.ve[i]), f);
+#pragma unroll
+          for (int e = 0; e < CPL; ++e) acc[e] += w * f[e];
+        } else {
+          const float mn = fmaxf(m, s);
+          const float a = __builtin_amdgcn_exp2f(m - mn);  // 0 for the first token (m = -inf)
+          const float w = __builtin_amdgcn_exp2f(s - mn);
+          z = z * a + w;
+          const float wv = w * e4m3_scale(x.ve[i]);
+          values_of(x.v[i], 1.f, f);
+#pragma unroll
+          for (int e = 0; e < CPL; ++e) acc[e] = acc[e] * a + wv * f[e];
+          m = mn;
+        }
       }
     }
   };
   stream_tiles<Rows>(
-      own_tiles(b1 - b0, wave, W), [&](int i, Rows& x) { fetch(b0 + wave + W * i, x); },
-      [&](int i, const Rows& x) { attend(b0 + wave + W * i, x); });
+      own_tiles((b1 - b0 + BPT - 1) / BPT, wave, W), [&](int i, Rows& x) { fetch(wave + W * i, x); },
+      [&](int i, const Rows& x) { attend(wave + W * i, x); });
 
   // merge the states: of a wavefront's rows by lane exchanges, then of the wavefronts
   auto join = [&](auto step) {
@@ -411,13 +431,14 @@ __global__ __launch_bounds__(64 * W) void decode_attention_e4m3_kernel(DecodePar
     const float f0 = z0 == 0.f ? 0.f : __builtin_amdgcn_exp2f(m0 - m), f1 = z1 == 0.f ? 0.f : __builtin_amdgcn_exp2f(m1 - m);
     z = z0 * f0 + z1 * f1;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
+    for (int e = 0; e < CPL; ++e) {
       float x0, x1;
       two_lanes<kStep>(acc[e], x0, x1);
       acc[e] = x0 * f0 + x1 * f1;
     }
   };
-  if constexpr (LPR == 4) join(std::integral_constant<int, 4>());
+  if constexpr (LPR <= 2) join(std::integral_constant<int, 2>());
+  if constexpr (LPR <= 4) join(std::integral_constant<int, 4>());
   join(std::integral_constant<int, 8>());
   join(std::integral_constant<int, 16>());
   join(std::integral_constant<int, 32>());
@@ -429,7 +450,7 @@ __global__ __launch_bounds__(64 * W) void decode_attention_e4m3_kernel(DecodePar
   }
   if (grp == 0) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sm_acc[wave][piece * 16 + e] = acc[e];
+    for (int e = 0; e < CPL; ++e) sm_acc[wave][piece * CPL + e] = acc[e];
   }
   __syncthreads();
   float mm = -INFINITY, zz = 0.f, o = 0.f;
@@ -502,20 +523,21 @@ static void launch_decode_one(const DecodeParams& p, const DecodeReqs& inline_re
   });
 }
 
-template <int D>
-static void launch_decode_e4m3(const DecodeParams& p, const DecodeReqs& inline_reqs, hipStream_t s) {
+template <int D, int kFormat>
+static void launch_decode_codes(const DecodeParams& p, const DecodeReqs& inline_reqs, hipStream_t s) {
   const unsigned heads = (unsigned)p.n_req * p.n_layers * p.n_heads;
   with_reqs(p, inline_reqs, [&](const auto& reqs) {
     using Reqs = std::decay_t<decltype(reqs)>;
     if (p.n_seg == 1 && p.wide) {
-      decode_attention_e4m3_kernel<D, 16, false, Reqs><<<heads, 1024, 0, s>>>(p, reqs);
+      constexpr int kWide = kFormat == ROWS_E2M1 ? 8 : 16;  // (16 have 128 registers each, too few here)
+      decode_attention_codes_kernel<D, kFormat, kWide, false, Reqs><<<heads, 64 * kWide, 0, s>>>(p, reqs);
       return;
     }
     if (p.n_seg == 1) {
-      decode_attention_e4m3_kernel<D, 4, false, Reqs><<<heads, kThreads, 0, s>>>(p, reqs);
+      decode_attention_codes_kernel<D, kFormat, 4, false, Reqs><<<heads, kThreads, 0, s>>>(p, reqs);
       return;
     }
-    decode_attention_e4m3_kernel<D, 4, true, Reqs><<<heads * p.n_seg, kThreads, 0, s>>>(p, reqs);
+    decode_attention_codes_kernel<D, kFormat, 4, true, Reqs><<<heads * p.n_seg, kThreads, 0, s>>>(p, reqs);
     decode_merge_kernel<D, false, Reqs><<<heads, D, 0, s>>>(p, reqs);
   });
 }
@@ -524,14 +546,12 @@ hipError_t launch_decode_attention(const DecodeParams& p, const DecodeReqs& inli
   if (p.n_req == 0) return hipSuccess;
   if (p.n_seg < 1 || p.n_seg > kMaxHeadSegments || p.seg_blocks < 1) return hipErrorInvalidValue;
   const bool indexed = p.kept != nullptr;
-  if (p.e4m3) {  // (whole caches only)
-    if (indexed) return hipErrorInvalidValue;
-    if (p.head_dim == 128)
-      launch_decode_e4m3<128>(p, inline_reqs, s);
-    else if (p.head_dim == 64)
-      launch_decode_e4m3<64>(p, inline_reqs, s);
-    else
-      return hipErrorInvalidValue;
+  if (p.e4m3 != ROWS_F16) {  // (whole caches only)
+    if (indexed || (p.head_dim != 64 && p.head_dim != 128)) return hipErrorInvalidValue;
+    with_row_format(p.head_dim, p.e4m3, [&](auto dim, auto format) {
+      if constexpr (decltype(format)::value != ROWS_F16)
+        launch_decode_codes<decltype(dim)::value, decltype(format)::value>(p, inline_reqs, s);
+    });
     return hipGetLastError();
   }
   if (p.head_dim == 128 && !indexed)

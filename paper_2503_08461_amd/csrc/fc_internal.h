@@ -35,9 +35,12 @@ struct DecodeReqList {  // requests on the device
 static_assert(sizeof(DecodeReq) == 24, "tests count on the sizes of descriptors and argument blocks");
 static constexpr size_t kMaxArgumentBytes = 4096;  // what the arguments of a kernel may take
 
+// How a pool holds its rows (the members `e4m3` below): fp16, in 8 bits (fc_e4m3.h), in 4 (fc_e2m1.h).
+enum { ROWS_F16 = 0, ROWS_E4M3 = 1, ROWS_E2M1 = 2 };
+
 struct DecodeParams {
   _Float16* kv;
-  int32_t e4m3;  // 1: the pool's rows are 8-bit (fc_e4m3.h), kv counts bytes
+  int32_t e4m3;  // ROWS_*; not fp16: kv counts bytes
   int32_t n_blocks, n_layers, n_heads, head_dim;
   const int32_t* stack;  // free stack (append: new blocks are stack[top_before - 1 - pop_index])
   int32_t top_before;
@@ -52,7 +55,7 @@ struct DecodeParams {
   float scale_log2e;
   // attention: blocks per segment of a head, segments of the longest one (1: no head is cut)
   int32_t seg_blocks, n_seg;
-  int32_t wide;            // 8-bit pool, no head cut: 16 wavefronts a head
+  int32_t wide;            // 8- or 4-bit pool, no head cut: 16 wavefronts a head
   float* partial;          // [n_req * layers * heads][n_seg][state_words] states of the segments
   int32_t* owner;          // ownership checks (debug mode), else NULL
   int32_t* error_flag;
@@ -98,7 +101,7 @@ struct RowsView {  // packed rows (fc_rows)
 
 struct StoreParams {
   void* kv;  // the layer's blocks
-  int32_t e4m3;
+  int32_t e4m3;  // ROWS_*
   int32_t n_blocks, n_heads, head_dim;
   const int32_t* block_tables;
   int32_t max_blocks;
@@ -108,9 +111,53 @@ struct StoreParams {
   RowsView k, v;
 };
 
+// Rows on their way into the pool, q and k rotated (fc_rotate.hip).  The requests' state_off is
+// the position of their first new token.
+struct RotateParams {
+  StoreParams store;
+  RowsView q, q_out;     // (n_q_heads 0: none)
+  int32_t n_q_heads;
+  const float* table;    // [position][cosines, sines][rotary / 2]
+  int32_t rotary;        // channels that are rotated
+  int32_t interleaved;
+};
+
+// Smallest and largest of each channel of K, block by block (fc_sparse.hip).
+struct BoundsParams {
+  const void* kv;  // the layer's blocks
+  int32_t format;  // ROWS_*
+  int32_t n_blocks, n_heads, head_dim;
+  const int32_t* block_tables;
+  int32_t max_blocks;
+  const ChunkReq* reqs;  // NULL: in the ChunkReqs argument; units are blocks, from row_off of the request on
+  int32_t n_req, n_units;
+  _Float16* bounds;      // the layer's [block][head][2][d]
+};
+
+// Blocks with the best scores, of every token and head (fc_sparse.hip).  The requests: one a
+// token, table_row its request's, seq_len the tokens it sees, row_off its packed row.
+struct SelectParams {
+  const _Float16* bounds;  // the layer's
+  int32_t n_blocks, n_heads, group, head_dim;
+  const int32_t* block_tables;
+  int32_t max_blocks;
+  const ChunkReq* reqs;    // NULL: in the ChunkReqs argument; a token's unit_start: its first part
+  int32_t n_tokens;
+  RowsView q;
+  int32_t n_select;
+  int32_t part_blocks;     // scores in a launch of their own: blocks a workgroup, else 0
+  int32_t n_units;         // ... and parts of all tokens
+  uint64_t* keys;          // ... and their scores' order, [token][head][key_stride]
+  int32_t key_stride;
+  int32_t lds_keys;        // no launch of their own: keys of the longest cache
+  int32_t* ids;            // [token][head][n_select] blocks of the pool, ascending in the request's table
+  int32_t* selected;       // nullable: the same as entries of the table, -1 behind the last
+};
+
 struct QuantiseParams {
   const _Float16* src;
   uint8_t* dst;
+  int32_t e2m1;  // 1: dst holds 4 bits
   int32_t src_blocks, dst_blocks, n_layers, n_heads, head_dim;
   const int32_t *src_tables, *dst_tables;
   int32_t src_max_blocks, dst_max_blocks;
@@ -120,7 +167,7 @@ struct QuantiseParams {
 };
 
 enum { ATTN_TALL = 0, ATTN_FLAT = 1, ATTN_KINDS = 2 };  // many rows a request, few (fc_chunk_plan.h)
-enum { ATTN_ROWS = 0, ATTN_F16 = 1, ATTN_E4M3 = 2 };  // where K and V are: packed rows, a pool
+enum { ATTN_ROWS = 0, ATTN_F16 = 1, ATTN_E4M3 = 2, ATTN_E2M1 = 3 };  // where K and V are: packed rows, a pool
 // The requests of one kind (ATTN_TALL, ATTN_FLAT) among those of a launch.
 struct AttnLaunchView {
   int32_t first_req, n_req;
@@ -136,6 +183,7 @@ struct AttnParams {
   uint32_t group_inverse;  // 2^31 / group, rounded up
   const int32_t* block_tables;
   int32_t max_blocks;
+  int32_t table_heads;   // rows of the tables a request: 1, or every head of K and V has its own
   const ChunkReq* reqs;  // NULL: in the ChunkReqs argument
   AttnLaunchView launch[ATTN_KINDS];
   RowsView q, k, v, out;
@@ -146,6 +194,9 @@ struct AttnParams {
 };
 static_assert(sizeof(AttnParams) + sizeof(AttnLaunchView) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
                   sizeof(StoreParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
+                  sizeof(RotateParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
+                  sizeof(BoundsParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
+                  sizeof(SelectParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
                   sizeof(QuantiseParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
                   sizeof(ExtendParams) + sizeof(ExtendReqs) <= kMaxArgumentBytes,
               "kernels of chunks");
@@ -280,7 +331,12 @@ hipError_t launch_decode_attention(const DecodeParams& p, const DecodeReqs& inli
 hipError_t launch_extend(const ExtendParams& p, const ExtendReqs& inline_reqs, hipStream_t s);
 hipError_t launch_store_chunk(const StoreParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
 hipError_t launch_quantise(const QuantiseParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
-// ... and their attention (fc_attention.hip)
+// ... with q and k rotated (fc_rotate.hip)
+hipError_t launch_rotate_store(const RotateParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
+// bounds of blocks, and the blocks that queries select by them (fc_sparse.hip)
+hipError_t launch_bounds(const BoundsParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
+hipError_t launch_select_blocks(const SelectParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
+// attention of chunks (fc_attention.hip)
 hipError_t attention_one_time_setup();
 hipError_t launch_attention(const AttnParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
 // chunk-MLP compressor (fc_mlp.hip)

@@ -17,6 +17,13 @@ constexpr int kProfRing = 32;
 // Descriptors of a call to the pool's buffer on the device (*out): through pinned memory, in a
 // captured call as kernel arguments (FC_EINVAL there if the buffer would have to grow).
 int meta_to_device(fc_pool* pool, const void* image, size_t bytes, const void** out, hipStream_t stream);
+// Bytes of a layer's block.
+inline size_t block_bytes(int dtype, int n_heads, int head_dim) {
+  const size_t rows = (size_t)2 * n_heads * FC_BLOCK_SIZE;
+  if (dtype == FC_DTYPE_E4M3) return rows * (head_dim + 1);                 // a code a channel and one exponent
+  if (dtype == FC_DTYPE_E2M1) return rows * (head_dim / 2 + head_dim / 32);  // half a byte, an exponent for 32
+  return rows * 2 * head_dim;
+}
 }  // namespace fc
 
 #define FC_HIP(call)                                                            \
@@ -64,6 +71,8 @@ struct Scratch {
   size_t cap = 0;  // elements
   bool captured = false;
 };
+// At least `bytes` for a call on `stream`; FC_EINVAL in a captured call that would have to allocate.
+int scratch_for(fc_pool* pool, Scratch<char>* s, size_t bytes, hipStream_t stream);
 }  // namespace fc
 
 struct fc_pool {
@@ -85,6 +94,7 @@ struct fc_pool {
   fc::Scratch<int32_t> kept;
   size_t split_refused = ~(size_t)0;  // least score scratch of split heads that could not be had
   fc::Scratch<int32_t> ids;  // old ids then new ids
+  fc::Scratch<char> sparse;  // scores' order and selected blocks of fc_sparse_attention
   std::vector<void*> retired;  // buffers that graphs use and calls do not any more
   char* dev_meta = nullptr;
   char* host_meta = nullptr;  // pinned

@@ -13,7 +13,7 @@ import numpy as np
 
 FC_OK, FC_EINVAL, FC_ENOMEM, FC_EDEVICE = 0, -1, -2, -3
 FC_METHOD_NONE, FC_METHOD_SNAPKV, FC_METHOD_KNORM, FC_METHOD_STREAMING = 0, 1, 2, 3
-FC_DTYPE_F16, FC_DTYPE_E4M3 = 0, 1
+FC_DTYPE_F16, FC_DTYPE_E4M3, FC_DTYPE_E2M1 = 0, 1, 3
 FC_BLOCK_SIZE = 16
 FC_N_KERNELS = 11
 FC_SCORE_AUTO, FC_SCORE_TWO_PASS = 0, 1
@@ -30,6 +30,7 @@ EXPORTS = [
     "fc_append_batch", "fc_decode_attention",
     "fc_decode_attention_kept",
     "fc_extend_batch", "fc_store_chunk", "fc_chunk_attention", "fc_prefill_attention", "fc_quantise_batch",
+    "fc_rotate_store_chunk", "fc_block_bounds", "fc_sparse_attention",
     "fc_mlp_set_weights", "fc_compress_batch_mlp", "fc_set_compaction_mode", "fc_set_streaming_sinks", "fc_set_score_mode", "fc_set_score_pruning", "fc_set_debug_checks", "fc_set_profiling", "fc_get_kernel_times",
     "fc_kernel_name", "fc_last_error",
     "fc_sched_create", "fc_sched_destroy", "fc_sched_submit", "fc_sched_pending",
@@ -51,6 +52,12 @@ class Rows(ctypes.Structure):
     """struct fc_rows"""
     _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
                 ("head_stride", ctypes.c_int64)]
+
+
+class RotationTable(ctypes.Structure):
+    """struct fc_rotation"""
+    _fields_ = [("table", ctypes.c_void_p), ("n_positions", ctypes.c_int), ("rotary_dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int)]
 
 
 class FastCacheError(RuntimeError):
@@ -114,6 +121,10 @@ def load_library():
     lib.fc_prefill_attention.argtypes = [vp, i, i32p, rows, rows, rows, i, rows, vp, i, i,
                                          ctypes.c_float, vp]
     lib.fc_quantise_batch.argtypes = [vp, vp, i, vp, vp, i, i32p, i32p, i, vp]
+    rotation = ctypes.POINTER(RotationTable)
+    lib.fc_rotate_store_chunk.argtypes = [vp, i, vp, i, i32p, i32p, i32p, rotation, rows, i, rows, rows, rows, i, vp]
+    lib.fc_block_bounds.argtypes = [vp, i, vp, i, i32p, i32p, vp, i, vp]
+    lib.fc_sparse_attention.argtypes = [vp, i, vp, i, i32p, i32p, vp, i, rows, i, rows, vp, i, ctypes.c_float, vp]
     lib.fc_mlp_set_weights.argtypes = [vp, ctypes.POINTER(MlpWeights), vp]
     lib.fc_compress_batch_mlp.argtypes = [vp, vp, i, i32p, i32p, i32p, i32p, i, vp]
     lib.fc_set_score_mode.argtypes = [vp, i]
@@ -222,11 +233,12 @@ def fc_pool_create(kv, n_blocks, n_layers, n_heads, head_dim, block_size=FC_BLOC
                    dtype=FC_DTYPE_F16):
     """kv: torch fp16 device tensor holding kv[layer][block][2][head][16][head_dim]; with
     dtype FC_DTYPE_E4M3 a uint8 one, per layer and block the codes [2][head][16][head_dim]
-    and then the exponents [2][head][16]."""
+    and then the exponents [2][head][16]; with FC_DTYPE_E2M1 one of codes
+    [2][head][16][head_dim / 2] and exponents [2][head][16][head_dim / 32]."""
     import torch
     lib = load_library()
     out = ctypes.c_void_p()
-    want = torch.uint8 if dtype == FC_DTYPE_E4M3 else torch.float16
+    want = torch.uint8 if dtype in (FC_DTYPE_E4M3, FC_DTYPE_E2M1) else torch.float16
     _check(lib.fc_pool_create(ctypes.byref(out), _dev_ptr(kv, want),
                               kv.numel() * kv.element_size(), n_blocks, block_size,
                               n_layers, n_heads, head_dim, int(dtype)))
@@ -573,7 +585,7 @@ def fc_prefill_attention(pool, layer, q, k, v, seq_lens, out=None, lse_out=None,
 
 def fc_quantise_batch(pool, block_tables, src_pool, src_block_tables, seq_lens, enable=None, stream=None):
     """Copies the cached rows of a batch from an fp16 pool (src_pool, through src_block_tables)
-    into an 8-bit one (pool, through block_tables, whose blocks the caller has from
+    into an 8- or 4-bit one (pool, through block_tables, whose blocks the caller has from
     fc_extend_batch); seq_lens, enable: int32 numpy arrays [n_req]."""
     import torch
     lib = load_library()
@@ -588,6 +600,90 @@ def fc_quantise_batch(pool, block_tables, src_pool, src_block_tables, seq_lens, 
         src_pool.ptr, _dev_ptr(src_block_tables, torch.int32), int(src_block_tables.shape[1]),
         _host_i32(seq_lens), _host_i32(enable) if enable is not None else None, n_req,
         _stream_ptr(stream)))
+
+
+class Rotation:
+    """The rotation of rows by their positions.  table: fp32 device tensor
+    [n_positions][2][rotary_dim / 2], cosines and sines; interleaved: pairs are neighbours."""
+
+    def __init__(self, table, interleaved=False):
+        import torch
+        if table.dim() != 3 or table.shape[1] != 2:
+            raise ValueError("table must be [n_positions][2][rotary_dim / 2]")
+        self.table = table  # keeps the caller's tensor alive
+        self.args = RotationTable(_dev_ptr(table, torch.float32), table.shape[0], 2 * table.shape[2], int(bool(interleaved)))
+
+
+def fc_rotate_store_chunk(pool, layer, block_tables, seq_lens, n_new, rotation, q, k, v, positions=None,
+                          q_out=None, stream=None):
+    """fc_store_chunk with q and k rotated by their positions (rotation: a Rotation; positions:
+    int32 numpy [n_req], those of each request's first new token, or None: as in a cache that
+    holds every token).  q: fp16 device tensor [sum n_new][n_q_heads][head_dim] or None, strided
+    like k; returns q_out, fp16 of the same shape (created if None)."""
+    import torch
+    lib = load_library()
+    n_req, n_rows = _new_rows(block_tables, seq_lens, n_new)
+    if positions is not None and positions.shape != (n_req,):
+        raise ValueError("positions must have n_req entries")
+    f16, d = torch.float16, pool.head_dim
+    kv_rows = (n_rows, pool.n_heads, d)
+    n_q, q_rows, out_rows = 0, None, None
+    if q is not None:
+        n_q = q.shape[1]
+        rows = (n_rows, n_q, d)
+        if q_out is None:
+            q_out = q.new_empty(rows)
+        q_rows, out_rows = ctypes.byref(_rows(q, "q", rows, f16)), ctypes.byref(_rows(q_out, "q_out", rows, f16))
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _check(lib.fc_rotate_store_chunk(
+        pool.ptr, int(layer), _dev_ptr(block_tables, torch.int32), int(block_tables.shape[1]),
+        _host_i32(seq_lens), _host_i32(n_new), _host_i32(positions) if positions is not None else None,
+        ctypes.byref(rotation.args), q_rows, n_q, out_rows, ctypes.byref(_rows(k, "k", kv_rows, f16)),
+        ctypes.byref(_rows(v, "v", kv_rows, f16)), n_req, _stream_ptr(stream)))
+    return q_out
+
+
+def _bounds_ptr(pool, bounds):
+    import torch
+    if tuple(bounds.shape) != (pool.n_layers, pool.n_blocks, pool.n_heads, 2, pool.head_dim):
+        raise ValueError("bounds must be [n_layers][n_blocks][n_heads][2][head_dim]")
+    return _dev_ptr(bounds, torch.float16)
+
+
+def fc_block_bounds(pool, layer, block_tables, seq_lens, n_new, bounds, stream=None):
+    """The smallest and largest value of each channel of K, for the blocks of one layer that hold
+    the last n_new tokens of every request.  bounds: fp16 device tensor
+    [n_layers][n_blocks][n_heads][2][head_dim], written there."""
+    import torch
+    lib = load_library()
+    n_req, _ = _new_rows(block_tables, seq_lens, n_new)
+    _check(lib.fc_block_bounds(
+        pool.ptr, int(layer), _dev_ptr(block_tables, torch.int32), int(block_tables.shape[1]),
+        _host_i32(seq_lens), _host_i32(n_new), _bounds_ptr(pool, bounds), n_req, _stream_ptr(stream)))
+
+
+def fc_sparse_attention(pool, layer, block_tables, seq_lens, n_new, bounds, n_select, q, out=None,
+                        selected=None, scale=0.0, stream=None):
+    """fc_chunk_attention over the n_select blocks that each new token's queries select by
+    `bounds` (fc_block_bounds), the token's own among them.  selected: int32 device tensor
+    [sum n_new][n_heads][n_select], the table entries that were read, or None."""
+    import torch
+    lib = load_library()
+    n_req, n_rows = _new_rows(block_tables, seq_lens, n_new)
+    n_q = q.shape[1]
+    rows = (n_rows, n_q, pool.head_dim)
+    if out is None:
+        out = q.new_empty(rows)
+    if selected is not None and tuple(selected.shape) != (n_rows, pool.n_heads, n_select):
+        raise ValueError("selected must be [sum n_new][n_heads][n_select]")
+    _check(lib.fc_sparse_attention(
+        pool.ptr, int(layer), _dev_ptr(block_tables, torch.int32), int(block_tables.shape[1]),
+        _host_i32(seq_lens), _host_i32(n_new), _bounds_ptr(pool, bounds), int(n_select),
+        ctypes.byref(_rows(q, "q", rows, torch.float16)), n_q,
+        ctypes.byref(_rows(out, "out", rows, torch.float16)), _dev_ptr(selected, torch.int32), n_req,
+        float(scale), _stream_ptr(stream)))
+    return out
 
 
 def fc_mlp_set_weights(pool, k, w1, b1, w2, b2, activation=FC_ACT_GELU_ERF, stream=None):

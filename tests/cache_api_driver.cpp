@@ -1,0 +1,187 @@
+// The entry points on rotated rows, bounds of blocks and selected blocks (csrc/fc_cache_api.hip) and a 4-bit
+// pool's calls on the CPU: the HIP runtime and the launchers of api_host_driver.cpp, and these.  Built and
+// checked by test_cache_api.py; every line says what was called, its code and what was launched.
+#define main api_host_main
+#include "api_host_driver.cpp"
+#undef main
+
+#include "../paper_2503_08461_amd/csrc/fc_cache_api.hip"
+#include "../paper_2503_08461_amd/csrc/fc_chunk_api.hip"
+
+static std::vector<ChunkReq> g_attended;
+namespace fc {
+hipError_t launch_extend(const ExtendParams& p, const ExtendReqs&, hipStream_t) { return launched("extend"); }
+hipError_t launch_store_chunk(const StoreParams& p, const ChunkReqs&, hipStream_t) { return launched(("store" + std::to_string(p.e4m3)).c_str()); }
+hipError_t launch_quantise(const QuantiseParams& p, const ChunkReqs&, hipStream_t) { return launched(("quantise" + std::to_string(p.e2m1)).c_str()); }
+hipError_t launch_attention(const AttnParams& p, const ChunkReqs& reqs, hipStream_t) {
+  std::string s = "attention" + std::to_string(p.source) + "x" + std::to_string(p.table_heads);
+  g_attended.clear();
+  if (!p.reqs) g_attended.assign(reqs.req, reqs.req + p.launch[0].n_req + p.launch[1].n_req);
+  return launched(s.c_str());
+}
+hipError_t launch_rotate_store(const RotateParams& p, const ChunkReqs& reqs, hipStream_t) {
+  std::string s = "rotate" + std::to_string(p.store.e4m3) + (p.store.reqs ? "" : "_inline") + ":" + std::to_string(p.store.n_rows) + "x" +
+                  std::to_string(p.n_q_heads);
+  if (!p.store.reqs)
+    for (int i = 0; i < p.store.n_req; ++i) s += ":" + std::to_string(reqs.req[i].state_off);
+  return launched(s.c_str());
+}
+hipError_t launch_bounds(const BoundsParams& p, const ChunkReqs&, hipStream_t) {
+  return launched(("bounds" + std::to_string(p.format) + ":" + std::to_string(p.n_units)).c_str());
+}
+hipError_t launch_select_blocks(const SelectParams& p, const ChunkReqs& reqs, hipStream_t) {
+  std::string s = "select" + std::string(p.reqs ? "" : "_inline") + ":" + std::to_string(p.n_tokens) + ":" + std::to_string(p.part_blocks ? 1 : 0) +
+                  ":" + std::to_string(p.lds_keys);
+  return launched(s.c_str());
+}
+}  // namespace fc
+
+int main() {
+  int32_t* table = somewhere<int32_t>();
+  float* out32 = somewhere<float>();
+  auto pool_of = [&](int dtype, int heads, int dim, size_t bytes) {
+    fc_pool* p = nullptr;
+    const int rc = fc_pool_create(&p, somewhere<void>(), bytes, 64, 16, 2, heads, dim, dtype);
+    g_launched.clear();
+    return rc == FC_OK ? p : nullptr;
+  };
+  // sizes: 17 / 32 bytes a channel
+  for (int dim : {64, 128}) {
+    const size_t bytes = (size_t)2 * 64 * 17 * 4 * dim;
+    fc_pool *none = pool_of(FC_DTYPE_E2M1, 4, dim, bytes - 1), *some = pool_of(FC_DTYPE_E2M1, 4, dim, bytes);
+    report("create4_small", none ? 0 : -1);
+    report("create4", some ? 0 : -1);
+    fc_pool_destroy(some);
+  }
+  fc_pool *p4 = pool_of(FC_DTYPE_E2M1, 4, 128, ~(size_t)0), *p8 = pool_of(FC_DTYPE_E4M3, 4, 128, ~(size_t)0);
+  fc_pool *p16 = pool_of(FC_DTYPE_F16, 4, 128, ~(size_t)0), *other = pool_of(FC_DTYPE_F16, 4, 64, ~(size_t)0);
+
+  // what a 4-bit pool refuses, before anything is launched
+  int32_t lens[2] = {100, 40}, method[2] = {FC_METHOD_KNORM, FC_METHOD_SNAPKV}, budget[2] = {40, 40}, width[2] = {7, 7}, window[2] = {16, 16};
+  const int32_t zeros[2] = {0, 0}, news[2] = {1, 33};
+  report("compress4", fc_compress_batch(p4, table, 8, lens, table, 16, method, budget, 2, 7, 0.f, nullptr, nullptr, nullptr));
+  report("noalloc4", fc_compress_batch_noalloc(p4, table, 8, lens, table, 16, method, budget, 2, 7, 0.f, nullptr, nullptr, nullptr));
+  report("var4", fc_compress_batch_var(p4, table, 8, lens, table, window, method, budget, width, 2, 0.f, nullptr, nullptr, nullptr));
+  report("lse4", fc_compress_batch_lse(p4, table, 8, lens, table, out32, 16, method, budget, 2, 7, 0.f, nullptr, nullptr, nullptr));
+  report("window4", fc_window_lse(p4, table, 8, lens, table, 16, nullptr, 2, 0.f, out32, nullptr));
+  report("kept4", fc_decode_attention_kept(p4, table, 8, lens, budget, table, table, out32, 2, 0.f, nullptr));
+  report("mlp4", fc_compress_batch_mlp(p4, table, 8, lens, zeros, zeros, nullptr, 2, nullptr));
+  // ... and takes
+  const fc_rows ok = {somewhere<void>(), 12 * 128, 128};
+  report("append4", fc_append_batch(p4, table, 8, lens, table, nullptr, 2, nullptr));
+  report("decode4", fc_decode_attention(p4, table, 8, lens, table, out32, 2, 0.f, nullptr));
+  report("store4", fc_store_chunk(p4, 0, table, 8, lens, news, &ok, &ok, 2, nullptr));
+  report("attend4", fc_chunk_attention(p4, 0, table, 8, lens, news, &ok, 8, &ok, nullptr, 0, 2, 0.f, nullptr));
+  report("prefill4", fc_prefill_attention(p4, 0, news, &ok, &ok, &ok, 8, &ok, nullptr, 0, 2, 0.f, nullptr));
+  report("quantise4", fc_quantise_batch(p4, table, 8, p16, table, 8, lens, nullptr, 2, nullptr));
+  report("quantise8", fc_quantise_batch(p8, table, 8, p16, table, 8, lens, nullptr, 2, nullptr));
+  report("quantise4_from8", fc_quantise_batch(p4, table, 8, p8, table, 8, lens, nullptr, 2, nullptr));
+  report("quantise4_back", fc_quantise_batch(p16, table, 8, p4, table, 8, lens, nullptr, 2, nullptr));
+  report("quantise4_other", fc_quantise_batch(p4, table, 8, other, table, 8, lens, nullptr, 2, nullptr));
+
+  // rotated rows
+  const fc_rotation turn = {out32, 1000, 128, 0};
+  auto rotate = [&](const char* what, const fc_rotation* r, const int32_t* positions = nullptr, const fc_rows* q = nullptr, int n_q = 0,
+                    const fc_rows* o = nullptr, const fc_rows* k = nullptr, const fc_rows* v = nullptr, int layer = 0, fc_pool* p = nullptr,
+                    const int32_t* n = nullptr, const int32_t* t = nullptr) {
+    report(what, fc_rotate_store_chunk(p ? p : p16, layer, t ? t : table, 8, lens, n ? n : news, positions, r, q, n_q, o, k ? k : &ok, v ? v : &ok, 2,
+                                       nullptr));
+  };
+  rotate("rotate", &turn);
+  rotate("rotate4", &turn, nullptr, &ok, 8, &ok, &ok, &ok, 1, p4);
+  rotate("rotate8", &turn, nullptr, &ok, 1, &ok, &ok, &ok, 1, p8);
+  int32_t last[2] = {999, 967}, past[2] = {999, 968}, before[2] = {-1, 0}, far[2] = {0, 0x7fffffff};
+  rotate("rotate_last", &turn, last);
+  rotate("rotate_past", &turn, past);
+  rotate("rotate_before", &turn, before);
+  rotate("rotate_far", &turn, far);
+  const int32_t only[2] = {0, 33};
+  rotate("rotate_unused", &turn, before, nullptr, 0, nullptr, nullptr, nullptr, 0, nullptr, only);
+  rotate("rotate_nothing", nullptr, nullptr, nullptr, 0, nullptr, nullptr, nullptr, 0, nullptr, zeros);
+  rotate("rotate_null", nullptr);
+  const fc_rotation no_table = {nullptr, 1000, 128, 0}, askew = {out32 + 1, 1000, 128, 0}, odd = {out32, 1000, 40, 0}, wide = {out32, 1000, 144, 0},
+                    none = {out32, 1000, 0, 0}, empty = {out32, 0, 128, 0}, part = {out32, 1000, 48, 1};
+  rotate("rotate_no_table", &no_table);
+  rotate("rotate_askew", &askew);
+  rotate("rotate_odd", &odd);
+  rotate("rotate_wide", &wide);
+  rotate("rotate_none", &none);
+  rotate("rotate_empty", &empty);
+  rotate("rotate_part", &part);
+  rotate("rotate_q", &turn, nullptr, nullptr, 8, &ok);
+  rotate("rotate_q_out", &turn, nullptr, &ok, 8, nullptr);
+  rotate("rotate_heads", &turn, nullptr, &ok, -1, &ok);
+  rotate("rotate_many_heads", &turn, nullptr, &ok, 4 * 64 + 1, &ok);
+  const fc_rows same = {somewhere<void>(), 0, 0}, crooked = {somewhere<char>() + 8, 512, 128}, uneven = {somewhere<void>(), 12 * 128 + 4, 128};
+  rotate("rotate_broadcast", &turn, nullptr, &same, 8, &ok, &same, &same);
+  rotate("rotate_overlap", &turn, nullptr, &ok, 8, &same);
+  rotate("rotate_k", &turn, nullptr, &ok, 8, &ok, &crooked);
+  rotate("rotate_v", &turn, nullptr, &ok, 8, &ok, &ok, &uneven);
+  rotate("rotate_layer", &turn, nullptr, nullptr, 0, nullptr, nullptr, nullptr, 2);
+  report("rotate_tables", fc_rotate_store_chunk(p16, 0, nullptr, 8, lens, news, nullptr, &turn, nullptr, 0, nullptr, &ok, &ok, 2, nullptr));
+  report("rotate_pool", fc_rotate_store_chunk(nullptr, 0, table, 8, lens, news, nullptr, &turn, nullptr, 0, nullptr, &ok, &ok, 2, nullptr));
+
+  // bounds
+  void* bounds = somewhere<void>();
+  auto bound = [&](const char* what, fc_pool* p, void* b, const int32_t* n, int layer = 0, int mb = 8, const int32_t* t = nullptr) {
+    report(what, fc_block_bounds(p, layer, t ? t : table, mb, lens, n, b, 2, nullptr));
+  };
+  printf("lens %d %d\n", lens[0], lens[1]);  // 101, 41
+  bound("bounds", p16, bounds, lens);
+  bound("bounds_new", p4, bounds, news);
+  bound("bounds8", p8, bounds, news, 1);
+  bound("bounds_null", p16, nullptr, news);
+  bound("bounds_askew", p16, static_cast<char*>(bounds) + 8, news);
+  bound("bounds_layer", p16, bounds, news, -1);
+  bound("bounds_short_table", p16, bounds, news, 0, 6);
+  bound("bounds_news", p16, bounds, nullptr);
+  bound("bounds_nothing", p16, nullptr, zeros);
+  int32_t more[2] = {102, 0};
+  bound("bounds_more", p16, bounds, more);
+
+  // selected blocks
+  auto sparse = [&](const char* what, int n_select, const fc_rows* q, const fc_rows* o, int n_q = 8, void* b = nullptr, int32_t* sel = nullptr,
+                    fc_pool* p = nullptr, const int32_t* n = nullptr) {
+    report(what, fc_sparse_attention(p ? p : p16, 0, table, 8, lens, n ? n : news, b ? b : bounds, n_select, q, n_q, o, sel, 2, 0.f, nullptr));
+  };
+  const int32_t one[2] = {1, 1};
+  sparse("sparse", 3, &ok, &ok, 8, nullptr, table, nullptr, one);
+  for (const ChunkReq& r : g_attended) printf("reads %d %d %d %d\n", r.table_row, r.seq_len, r.n_new, r.row_off);
+  sparse("sparse4", 2048, &ok, &ok, 4, nullptr, nullptr, p4);
+  sparse("sparse8", 1, &ok, &ok, 4, nullptr, nullptr, p8);
+  sparse("sparse_none", 0, &ok, &ok);
+  sparse("sparse_many", 2049, &ok, &ok);
+  sparse("sparse_q", 3, nullptr, &ok);
+  sparse("sparse_out", 3, &ok, nullptr);
+  sparse("sparse_overlap", 3, &ok, &same);
+  sparse("sparse_heads", 3, &ok, &ok, 6);
+  sparse("sparse_askew", 3, &ok, &ok, 8, static_cast<char*>(bounds) + 2);
+  sparse("sparse_selected", 3, &ok, &ok, 8, nullptr, reinterpret_cast<int32_t*>(somewhere<char>() + 2));
+  report("sparse_bounds", fc_sparse_attention(p16, 0, table, 8, lens, news, nullptr, 3, &ok, 8, &ok, nullptr, 2, 0.f, nullptr));
+  sparse("sparse_nothing", 0, nullptr, nullptr, 0, nullptr, nullptr, nullptr, zeros);
+  int32_t long_lens[1] = {30000}, first[1] = {1};
+  report("sparse_long", fc_sparse_attention(p16, 0, table, 2048, long_lens, first, bounds, 64, &ok, 4, &ok, nullptr, 1, 0.f, nullptr));
+  for (const ChunkReq& r : g_attended) printf("reads %d %d %d %d\n", r.table_row, r.seq_len, r.n_new, r.row_off);
+
+  // captured: nothing is allocated
+  const int n = 150;
+  std::vector<int32_t> l(n, 200), ones(n, 1);
+  fc_pool* fresh = pool_of(FC_DTYPE_F16, 4, 128, ~(size_t)0);
+  auto many = [&](const char* what, int n_req, bool captured) {
+    g_capturing = captured;
+    report(what, fc_sparse_attention(fresh, 0, table, 16, l.data(), ones.data(), bounds, 3, &ok, 4, &ok, nullptr, n_req, 0.f, nullptr));
+    g_capturing = false;
+  };
+  many("captured_first", 100, true);
+  many("eager", 100, false);
+  const char* used = fresh->sparse.data;
+  many("captured", 100, true);
+  printf("kept %d\n", (int)(fresh->sparse.captured && fresh->sparse.data == used));
+  many("captured_many", n, true);  // (descriptors that no call left room for)
+  l.assign(4000, 200);
+  ones.assign(4000, 1);
+  report("eager_more", fc_sparse_attention(fresh, 0, table, 16, l.data(), ones.data(), bounds, 3, &ok, 4, &ok, nullptr, 4000, 0.f, nullptr));
+  printf("retired %d\n", (int)(fresh->retired.size() == 1 && fresh->retired[0] == used && !fresh->sparse.captured));
+  for (fc_pool* p : {p4, p8, p16, other, fresh}) fc_pool_destroy(p);
+  return 0;
+}

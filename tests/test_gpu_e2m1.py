@@ -1,0 +1,277 @@
+"""The 4-bit pool: copies, stores and appends byte by byte, attention over it in 64 bits."""
+
+import numpy as np
+import pytest
+
+from attention_util import blocks_for
+from cache_util import Cache, decode_check, encode, rows_of
+from oracle import cache_oracle as co
+
+pytestmark = pytest.mark.gpu
+
+
+def _hard_rows(rng, n, dim):
+    """Rows over fp16's whole range: every group of another magnitude, ties between codes, the
+    ends of the range, zeros of both signs, groups that are not finite."""
+    x = rng.standard_normal((n, dim)) * np.exp2(rng.uniform(-26, 15, (n, dim // 32))).repeat(32, 1)
+    x = np.clip(x, -65504, 65504).astype(np.float16)
+    ties = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 6], np.float16)
+    x[0] = 0
+    x[1, :4] = [65504, -57344, 49152, 49184]
+    x[2] = np.tile(np.concatenate([ties, -ties]), dim // 16)
+    x[3] = x[2] * np.float16(2.0 ** -21)                       # ties among the smallest
+    x[4, 0], x[4, 1] = 6.004, 6                                # just over a border
+    x[5] = np.arange(dim).astype(np.float16) * np.float16(2.0 ** -24)
+    x[6, 3], x[6, 40] = np.inf, 1                              # the first group only
+    x[7, 33], x[7, 34] = np.nan, -np.inf                       # the second only
+    x[8] = -0.0
+    x[9] = 12288 * (np.arange(dim) % 5 + 1)
+    return x
+
+
+def _put(want, c_layer, block, slot, rows, heads, dim):
+    """Rows [2][head][d] of one token into the pool's bytes."""
+    codes, exps = encode(rows, "e2m1")
+    for which, h in np.ndindex(2, heads):
+        row = (which * heads + h) * 16 + slot
+        want[c_layer, block, row * (dim // 2):(row + 1) * (dim // 2)] = codes[which, h]
+        at = 16 * heads * dim + row * (dim // 32)
+        want[c_layer, block, at:at + dim // 32] = exps[which, h]
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_quantise_batch_byte_by_byte(dim):
+    """Ragged lengths, a request switched off, an empty one; slots behind the last token and other
+    blocks keep what they had."""
+    import torch
+    from paper_2503_08461_amd import fastcache as fc
+    rng = np.random.default_rng(dim)
+    lens, enable = [33, 0, 16, 5, 48], np.array([1, 1, 1, 0, 1], np.int32)
+    heads, layers, nb4 = 3, 2, 12
+
+    def kv(c):
+        rows = np.concatenate([_hard_rows(rng, 64, dim) for _ in range(c.kv.size // dim // 64 + 1)])
+        return rows[rng.permutation(c.kv.size // dim)].reshape(c.kv.shape)
+
+    c = Cache(lens, [0] * 5, heads, 1, dim, fmt="f16", layers=layers, kv=kv)
+    kv4 = torch.full((layers, nb4, 17 * heads * dim), 0xA5, dtype=torch.uint8, device=c.dev)
+    pool4 = fc.fc_pool_create(kv4, nb4, layers, heads, dim, dtype=fc.FC_DTYPE_E2M1)
+    try:
+        table4 = torch.full((5, 4), -1, dtype=torch.int32, device=c.dev)
+        lens4 = np.zeros(5, np.int32)
+        fc.fc_extend_batch(pool4, table4, lens4, (c.lens * enable).astype(np.int32))
+        fc.fc_quantise_batch(pool4, table4, c.pool, c.table_dev, c.lens, enable)
+        want = np.full(tuple(kv4.shape), 0xA5, np.uint8)
+        t4 = table4.cpu().numpy()
+        for r, n in enumerate(lens):
+            for t in range(n if enable[r] else 0):
+                for layer in range(layers):
+                    _put(want, layer, t4[r, t // 16], t % 16, c.kv[layer, c.table[r, t // 16], :, :, t % 16], heads, dim)
+        assert (kv4.cpu().numpy() == want).all()
+    finally:
+        c.close()
+        fc.fc_pool_destroy(pool4)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("strided", [True, False])
+def test_store_chunk_byte_by_byte(dim, strided):
+    import torch
+    from paper_2503_08461_amd import fastcache as fc
+    rng = np.random.default_rng(dim + strided)
+    c = Cache([33, 16, 7, 40], [33, 1, 0, 17], 3, 2, dim, strided=strided)
+    try:
+        k, v = (_hard_rows(rng, 51 * 3, dim).reshape(51, 3, dim) for _ in range(2))
+        c.k_dev.copy_(torch.from_numpy(k))
+        c.v_dev.copy_(torch.from_numpy(v))
+        want = c.kv_dev.cpu().numpy()
+        fc.fc_store_chunk(c.pool, 1, c.table_dev, c.lens, c.news, c.k_dev, c.v_dev)
+        row = 0
+        for r, n in enumerate(c.news.tolist()):
+            for t in range(int(c.lens[r]) - n, int(c.lens[r])):
+                _put(want, 1, c.table[r, t // 16], t % 16, np.stack([k[row], v[row]]), 3, dim)
+                row += 1
+        assert (c.kv_dev.cpu().numpy() == want).all()
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_append_byte_by_byte(dim):
+    """Three steps over block boundaries, a request switched off."""
+    import torch
+    from paper_2503_08461_amd import fastcache as fc
+    rng = np.random.default_rng(9)
+    c = Cache([15, 16, 0, 30], [0] * 4, 3, 1, dim, spare=8)
+    try:
+        fc.fc_pool_import_state(c.pool, np.array(sorted(set(range(c.n_blocks)) - set(c.table[c.table >= 0].tolist())) +
+                                                 [0] * int((c.table >= 0).sum()), np.int32), 8)
+        want = c.kv_dev.cpu().numpy()
+        enable = np.array([1, 1, 1, 0], np.int32)
+        for step in range(3):
+            new = _hard_rows(rng, 4 * c.layers * 2 * 3, dim).reshape(4, c.layers, 2, 3, dim)
+            before = c.lens.copy()
+            fc.fc_append_batch(c.pool, c.table_dev, c.lens, torch.from_numpy(new).to(c.dev), enable)
+            assert (c.lens == before + enable).all()
+            table = c.table_dev.cpu().numpy()
+            for r in range(3):
+                for layer in range(c.layers):
+                    _put(want, layer, table[r, before[r] // 16], before[r] % 16, new[r, layer], 3, dim)
+        assert (c.kv_dev.cpu().numpy() == want).all()
+    finally:
+        c.close()
+
+
+def _decode(c, seed=4, scale=0.0):
+    import torch
+    q = np.random.default_rng(seed).standard_normal((len(c.lens), c.layers, c.heads, c.dim)).astype(np.float16)
+    got = c.fc.fc_decode_attention(c.pool, c.table_dev, c.lens, torch.from_numpy(q).to(c.dev), scale=scale).cpu().numpy()
+    decode_check(c, q, got, scale or None)
+
+
+# (one workgroup of four or of eight wavefronts a head; odd numbers of blocks; heads cut into segments)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("lens", [[1], [17], [1, 0, 15, 16, 17, 33, 65, 300], [511, 40], [1100, 2, 1121], [3000, 900]], ids=str)
+def test_decode_attention(lens, dim):
+    c = Cache(lens, [0] * len(lens), 2, 1, dim, seed=dim)
+    try:
+        _decode(c)
+        _decode(c, seed=5, scale=0.7)
+    finally:
+        c.close()
+
+
+def test_decode_of_more_requests_than_arguments_hold():
+    c = Cache([1 + 7 * i % 50 for i in range(151)], [0] * 151, 1, 1, 64, layers=1)
+    try:
+        _decode(c)
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_decode_of_climbing_logits(dim):
+    """Every key's logit is above the one before by less, and by more, than the maximum may fall behind."""
+    import torch
+    c = Cache([200, 70], [0, 0], 1, 1, dim, layers=1)
+    try:
+        c.kv[:, :, 0] = 0
+        step = np.array([0.5, 6.0], np.float16)
+        for r, n in enumerate(c.lens.tolist()):
+            for t in range(n):  # (powers of two are exact in 4 bits, and so are sums of two of them over two groups)
+                c.kv[0, c.table[r, t // 16], 0, 0, t % 16, 0] = 2.0 ** (t % 11)
+                c.kv[0, c.table[r, t // 16], 0, 0, t % 16, 32] = 6 * (t // 40)
+        c.upload()
+        for s in step:
+            q = np.full((2, 1, 1, dim), s, np.float16)
+            got = c.fc.fc_decode_attention(c.pool, c.table_dev, c.lens, torch.from_numpy(q).to(c.dev), scale=1.0).cpu().numpy()
+            decode_check(c, q, got, 1.0)
+    finally:
+        c.close()
+
+
+def test_not_a_number_reaches_the_output_where_it_is_seen():
+    """Of a K row in fp32 sums, of a V channel's group; behind the last token it reaches nothing."""
+    import torch
+    c = Cache([300, 300, 300], [1, 1, 1], 1, 2, 128, layers=1)
+    try:
+        for r, which, slot in [(1, 0, 5), (2, 1, 6)]:
+            c.kv_dev[0, int(c.table[r, 3]), 16 * 128 + (which * 16 + slot) * 4 + 1] = 255     # the second group's exponent
+        for r in range(3):                                                                  # slots 12 .. 15 of the last block
+            c.kv_dev[0, int(c.table[r, 18]), 16 * 128 + 12 * 4:16 * 128 + 64] = 255
+            c.kv_dev[0, int(c.table[r, 18]), 16 * 128 + 64 + 12 * 4:] = 255
+        q = torch.ones((3, 1, 1, 128), dtype=torch.float16, device=c.dev)
+        got = c.fc.fc_decode_attention(c.pool, c.table_dev, c.lens, q)[:, 0, 0]
+        out = c.fc.fc_chunk_attention(c.pool, 0, c.table_dev, c.lens, c.news, c.q_dev)
+        for x in (got, out[:, 0], out[:, 1]):
+            assert not torch.isnan(x[0]).any() and torch.isnan(x[1]).all()
+            assert torch.isnan(x[2]).nonzero().flatten().tolist() == list(range(32, 64))
+    finally:
+        c.close()
+
+
+# few rows (one to 32), many (to 128 and beyond), both in one call, groups that do not divide a tile
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("lens,news,heads,group", [
+    ([1], [1], 1, 1), ([300, 16, 17, 5, 0], [1, 1, 3, 5, 0], 2, 4), ([70, 129, 31], [33, 40, 31], 3, 1),
+    ([500, 40], [150, 1], 2, 5), ([64, 2000], [64, 3], 1, 8), ([90], [2], 1, 64)], ids=str)
+def test_chunk_attention(lens, news, heads, group, dim):
+    import torch
+    c = Cache(lens, news, heads, group, dim, seed=dim)
+    try:
+        window = 4
+        lse = torch.full((len(lens), c.layers, heads * group, window), 7.0, device=c.dev)
+        for layer in range(c.layers):
+            c.fc.fc_store_chunk(c.pool, layer, c.table_dev, c.lens, c.news, c.k_dev, c.v_dev)
+            out = c.fc.fc_chunk_attention(c.pool, layer, c.table_dev, c.lens, c.news, c.q_dev, lse_out=lse, window=window)
+            c.check(layer, out, lse, window)
+        lse = lse.cpu().numpy()
+        for r, n in enumerate(news):
+            assert (lse[r, :, :, :max(0, window - n)] == 7).all()
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_long_caches_are_cut(new):
+    """Segments of few and of many rows, with a last one that ends inside a tile."""
+    c = Cache([9000 + new, 2003], [new, new], 1, 1, 128, layers=1)
+    try:
+        c.fc.fc_store_chunk(c.pool, 0, c.table_dev, c.lens, c.news, c.k_dev, c.v_dev)
+        c.check(0, c.fc.fc_chunk_attention(c.pool, 0, c.table_dev, c.lens, c.news, c.q_dev))
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("new,group", [(3, 1), (40, 1), (3, 20)])
+def test_masked_places_that_are_not_numbers(new, group):
+    """K and V of the new tokens, which earlier rows do not see, and of the slots behind the last one."""
+    import torch
+    c = Cache([60 + new], [new], 1, group, 64, layers=1)
+    try:
+        c.k_dev[-1], c.v_dev[-1] = float("nan"), float("inf")
+        c.fc.fc_store_chunk(c.pool, 0, c.table_dev, c.lens, c.news, c.k_dev, c.v_dev)
+        out = c.fc.fc_chunk_attention(c.pool, 0, c.table_dev, c.lens, c.news, c.q_dev).cpu().numpy()
+        assert np.isnan(out[-1]).all() and np.isfinite(out[:-1]).all()
+        c.lens, c.news = c.lens - 1, c.news - 1
+        k, v = c.cached(c.pool_rows(0), 0)
+        from attention_util import check
+        for h in range(group):
+            check(c.q[:-1, h], k[0], v[0], 60, out[:-1, h])
+    finally:
+        c.close()
+
+
+def test_far_blocks():
+    """A pool whose codes lie behind 2^32 bytes."""
+    import torch
+    from paper_2503_08461_amd import fastcache as fc
+    heads, dim = 40, 128
+    n_blocks = (1 << 32) // (17 * heads * dim) + 40
+    dev = torch.device("cuda:0")
+    kv = torch.zeros((1, n_blocks, 17 * heads * dim), dtype=torch.uint8, device=dev)
+    pool = fc.fc_pool_create(kv, n_blocks, 1, heads, dim, dtype=fc.FC_DTYPE_E2M1)
+    try:
+        table = torch.arange(n_blocks - 3, n_blocks, dtype=torch.int32, device=dev)[None]
+        lens = np.array([40], np.int32)
+        x = torch.randn((40, heads, dim), generator=torch.Generator(dev).manual_seed(1), device=dev).half()
+        fc.fc_store_chunk(pool, 0, table, lens, lens, x, x)
+        got = kv[0, -3:].cpu().numpy()
+        want = np.stack(np.split(np.concatenate([x.cpu().numpy(), np.zeros((8, heads, dim), np.float16)]), 3))
+        rows = rows_of(got, "e2m1", heads, dim)
+        for b in range(3):
+            for h in (0, heads - 1):
+                for s in range(16 if b < 2 else 8):
+                    codes, exps = co.quantise_row(want[b, s, h])
+                    assert (rows[b, 0, h, s] == co.values(co.pack(codes), exps)).all()
+        assert int((kv[0, :-3] != 0).sum()) == 0
+        q = torch.randn((1, 1, heads, dim), generator=torch.Generator(dev).manual_seed(2), device=dev).half()
+        near = fc.fc_decode_attention(pool, table, lens, q)
+        kv[0, :3] = kv[0, -3:]
+        assert (fc.fc_decode_attention(pool, table - (n_blocks - 3), lens, q) == near).all()
+        news = np.array([1], np.int32)
+        out = fc.fc_chunk_attention(pool, 0, table, lens, news, q[:, 0])
+        assert (fc.fc_chunk_attention(pool, 0, table - (n_blocks - 3), lens, news, q[:, 0]) == out).all()
+        assert (near[0] - out.float()).abs().max() < 2e-2
+    finally:
+        fc.fc_pool_destroy(pool)
