@@ -126,7 +126,7 @@ __device__ __forceinline__ void lds_barrier() {
 // 32-key subtiles of fp16 rows in LDS, from row `at` of tiles k and v.
 template <int D>
 struct F16Keys {
-  static constexpr bool kPairedSlabs = false;  // (of the queries that its slabs meet: take_queries)
+  static constexpr int kSlabs = 1;  // of K that a lane reads at a time (take_queries)
   const half8 *k, *v;
   int at;
   // A operands: of a slab of K (lane: key, eight channels by half), ...
@@ -190,7 +190,8 @@ struct Rows32 {
 #pragma unroll
     for (int i = 0; i < KK; ++i) q[i] = load_half8(from((i * 64 + lane) / (D / 8)) + (lane % (D / 8)) * 8);
   }
-  template <bool kPairedSlabs>
+  // (kSlabs: slabs of K that a lane reads next to each other; the queries' channels follow)
+  template <int kSlabs>
   __device__ __forceinline__ void take_queries(half8* room) {
     const int lane = threadIdx.x & 63, half = lane >> 5;
 #pragma unroll
@@ -198,7 +199,7 @@ struct Rows32 {
     wave_lds_barrier();
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
-      q[kk] = room[k_chunk<D>(lane & 31, kPairedSlabs ? 2 * (2 * (kk / 2) + half) + kk % 2 : 2 * kk + half)];
+      q[kk] = room[k_chunk<D>(lane & 31, kSlabs * (2 * (kk / kSlabs) + half) + kk % kSlabs)];
     wave_lds_barrier();
   }
   // The lane's row times f, as fp16 rows in LDS (32 of the wavefront's own), then row by row to
@@ -614,7 +615,7 @@ __device__ __forceinline__ int2v read_byte_columns(const uint8_t* __restrict at)
 constexpr int kExponentBytes = 256;  // of a block, in LDS (what one load of a word a lane fills)
 template <int D>
 struct E4m3Keys {
-  static constexpr bool kPairedSlabs = true;  // a 16-byte read of K is its lane's part of two slabs
+  static constexpr int kSlabs = 2;  // a 16-byte read of K is its lane's part of two slabs
   const uint8_t *k, *v;
   float k_scale;         // of the lane's key
   half2v v_scale[2][4];  // of the lane's eight keys of a slab of V
@@ -683,6 +684,110 @@ struct E4m3Keys {
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = ((x >> (8 * e)) & 0x7fu) == 0x7fu ? __builtin_nanf("") : 0.f;
     return y;
+  }
+};
+
+// 4 bits: codes straight to LDS as well, fp16 numbers as they are read.  A block there: 16 rows of K, 16
+// of V, D / 2 bytes each, 16-byte chunks (a group of 32 channels) permuted within the row for K's reads
+// (32 rows at one chunk) and V's transposing ones (rows 0-3, 8-11 and so on of a tile, 8 bytes each).
+// Through registers, with fp16 rows written to LDS and read from there, the LDS is busy for 1280 of the 1600
+// cycles that a SIMD has for a tile at the memory's rate, so for 500.
+template <int D>
+__device__ __forceinline__ int chunk4(int r, int c) {
+  return D == 128 ? c ^ (((r >> 2) & 3) ^ ((r >> 4) & 1)) : c ^ ((r >> 3) & 1);
+}
+template <int D>
+struct Loader4 {
+  static constexpr int kRow = D / 2, kHalf = 16 * kRow, kBlock = 2 * kHalf;  // bytes: a row, K's of a block, a block
+  static constexpr int kExpWords = D / 8;                                   // of a block's K, and of V
+  static constexpr int kLoads = D == 128 ? 3 : 2;                           // wavefront loads of a block
+  int at[2];  // the lane's chunk in a tile's first and second block (at 64 channels lanes from 32 on have V's)
+  int e_at;
+  __device__ __forceinline__ Loader4(int n_heads, int head) {
+    const int lane = threadIdx.x & 63;
+    const int l = D == 128 ? lane : lane & 31;
+    const int r = l / (kRow / 16), c = l % (kRow / 16);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      at[j] = r * kRow + chunk4<D>(16 * j + r, c) * 16 + (D == 64 && lane >= 32 ? n_heads * kHalf : 0);
+    e_at = lane < kExpWords       ? (head * kExpWords + lane) * 4
+           : lane < 2 * kExpWords ? ((n_heads + head) * kExpWords + lane - kExpWords) * 4
+                                  : 1 << 30;
+  }
+  // block j of a tile, or nothing; the exponents' room is kExponentBytes
+  __device__ __forceinline__ void request(const uint8_t* block, int n_heads, int head, int j, bool wanted, uint8_t* to, uint8_t* to_e) const {
+    const uint8_t* k = block + (size_t)head * kHalf;
+    const int v_off = n_heads * kHalf;
+    load_to_lds<true>(buffer_of(k, wanted ? kHalf + (D == 64 ? v_off : 0) : 0), at[j], reinterpret_cast<half8*>(to));
+    if constexpr (D == 128) load_to_lds<true>(buffer_of(k + v_off, wanted ? kHalf : 0), at[j], reinterpret_cast<half8*>(to + kHalf));
+    load_word_to_lds(buffer_of(block + 2 * (size_t)v_off, wanted ? 2 * n_heads * kExpWords * 4 : 0), e_at, to_e);
+  }
+};
+typedef __attribute__((address_space(3))) int2v* LdsNibbles;
+// (lane l: of the sixteen rows that the sixteen lanes around it point to, 8 bytes each, the code in place l % 16)
+__device__ __forceinline__ int2v read_code_columns(const uint8_t* __restrict at) {
+  return __builtin_amdgcn_ds_read_tr4_b64_v2i32((LdsNibbles)at);
+}
+template <int D>
+struct E2m1Keys {
+  static constexpr int kSlabs = 4;  // a 16-byte read of K is its lane's part of four slabs
+  static constexpr int DT = D / 32, G = D / kE2m1Group;
+  typedef Loader4<D> L;
+  const uint8_t* codes;      // two blocks
+  const uint8_t* exponents;  // of each
+  _Float16* scales;          // V's powers of two [group][half of the wavefront][16 keys], the wavefront's own
+  uint4v k_part[G / 2];
+  float k_scale[G / 2];
+  int2v v_part[DT];
+  bool not_finite_seen;
+  __device__ __forceinline__ static const uint8_t* row(const uint8_t* codes, int r) { return codes + (r >> 4) * L::kBlock + (r & 15) * L::kRow; }
+  // where a key's scale of V lies in its half's sixteen: in the order of the products' keys
+  __device__ __forceinline__ static int place(int dt, int key) {
+    return (dt * 2 + ((key >> 2) & 1)) * 16 + (key >> 4) * 8 + ((key >> 3) & 1) * 4 + (key & 3);
+  }
+  __device__ __forceinline__ void set_k() {
+    const int lane = threadIdx.x & 63, r = lane & 31, half = lane >> 5;
+    const uint8_t* e = exponents + (r >> 4) * kExponentBytes + (r & 15) * G + half;
+#pragma unroll
+    for (int j = 0; j < G / 2; ++j) {
+      k_part[j] = *reinterpret_cast<const uint4v*>(row(codes, r) + chunk4<D>(r, 2 * j + half) * 16);
+      k_scale[j] = e4m3_scale(e[2 * j]);
+    }
+  }
+  __device__ __forceinline__ half8 k_slab(int, int kk) const { return e2m1_values(k_part[kk / 4][kk % 4], k_scale[kk / 4]); }
+  // Keys behind `last` are seen by no row (and their slots may hold anything): times zero.
+  template <bool kMasked>
+  __device__ __forceinline__ void set_v(int last) {
+    const int lane = threadIdx.x & 63, key = lane & 31;
+    constexpr int kPer = DT / 2;  // scales that a lane makes
+    const uint8_t* e = exponents + (key >> 4) * kExponentBytes + L::kExpWords * 4 + (key & 15) * G + (lane >> 5) * kPer;
+    not_finite_seen = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const uint32_t x = e[i];
+      const bool seen = !kMasked || key <= last;
+      // (the code of 1, scaled: 255 << 23 makes it not a number)
+      const _Float16 f = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(0x22u, e4m3_scale(x), 0)[0];
+      scales[place((lane >> 5) * kPer + i, key)] = seen ? f : (_Float16)0.f;
+      if (kMasked && seen && x == kE2m1NotFinite) not_finite_seen = true;
+    }
+    wave_lds_barrier();
+    // row (lane % 16) of the transposing reads: keys in the order of place()
+    const int i = lane & 15;
+    const int r = (i >> 3) * 16 + ((i >> 2) & 1) * 8 + (lane >> 5) * 4 + (i & 3);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      v_part[dt] = read_code_columns(row(codes, r) + L::kHalf + chunk4<D>(r, dt) * 16 + ((lane >> 4) & 1) * 8);
+  }
+  __device__ __forceinline__ half8 v_slab(int, int kk, int dt) const {
+    const half8 scale = *reinterpret_cast<const half8*>(scales + (dt * 2 + ((threadIdx.x & 63) >> 5)) * 16 + kk * 8);
+    return e2m1_values(v_part[dt][kk], 1.f) * scale;
+  }
+  template <int kSub>
+  __device__ __forceinline__ bool dirty() const { return __any(not_finite_seen); }
+  __device__ __forceinline__ floatx4 not_finite(int key, int channel) const {
+    const float x = abs_bits(scales[place(channel / 32, key)]) >= 0x7c00u ? __builtin_nanf("") : 0.f;
+    return floatx4{x, x, x, x};
   }
 };
 
@@ -805,7 +910,7 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
     request(0);
     if constexpr (kCodes) put8(0);
     // (the second tile's room is free until the first barrier)
-    rows.template take_queries<F16Keys<D>::kPairedSlabs>(sm + 2 * kTile + wave * 32 * D / 8);
+    rows.template take_queries<F16Keys<D>::kSlabs>(sm + 2 * kTile + wave * 32 * D / 8);
   }
   int t = 0;
   for (; t + 1 < n_full; t += 2) {
@@ -867,6 +972,11 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
 // Bytes of one row of K or V in the LDS of such a wavefront.
 template <int D, int SRC>
 constexpr int kFlatRowBytes = SRC == ATTN_E4M3 ? D : 2 * D;
+
+// Tiles of a 4-bit pool that such a wavefront has room for, and their bytes with the exponents and V's scales.
+constexpr int kStages4 = 3;
+constexpr int stage4_bytes(int head_dim) { return 32 * head_dim + 2 * kExponentBytes; }
+constexpr int wave4_bytes(int head_dim) { return kStages4 * stage4_bytes(head_dim) + 2 * head_dim; }
 
 // LDS reads before this point have been answered: what they read may be overwritten by loads.
 __device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
@@ -944,7 +1054,7 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
         request_v(i);
         lds_reads_done();
         if (i == 0) {  // through the second tile's room
-          rows.template take_queries<E4m3Keys<D>::kPairedSlabs>(sm_k + 2 * kTile);
+          rows.template take_queries<E4m3Keys<D>::kSlabs>(sm_k + 2 * kTile);
           lds_reads_done();
         }
       }
@@ -973,28 +1083,44 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
     for (; i < full; ++i) step(i, std::false_type());
     for (; i < mine; ++i) step(i, std::true_type());
   } else if constexpr (SRC == ATTN_E2M1) {
-    // The next tile's codes in registers while one is worked on as fp16 rows in LDS.
-    const F16Keys<D> keys{sm_k, sm_k + kTile, 0};
-    Block4<D> next[2];
+    // Two tiles on their way while a third is worked on.
+    typedef Loader4<D> L;
+    const L loader(p.n_heads, head);
+    uint8_t* mine4 = reinterpret_cast<uint8_t*>(sm) + wave * wave4_bytes(D);
+    auto stage = [&](int i) { return mine4 + (i % kStages4) * stage4_bytes(D); };
     auto request = [&](int i) {
-      look_up(i);
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        next[j].request(static_cast<const uint8_t*>(p.kv) + (size_t)ids[j] * e2m1_block_bytes(p.n_heads, D), p.n_heads, head);
-      requests_first();
+        loader.request(static_cast<const uint8_t*>(p.kv) + (size_t)ids[j] * e2m1_block_bytes(p.n_heads, D), p.n_heads, head, j, i < mine,
+                       stage(i) + j * L::kBlock, stage(i) + 2 * L::kBlock + j * kExponentBytes);
     };
-    auto step = [&](int i, auto masked_) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) next[j].put(sm_k, sm_k + kTile, 16 * j);
-      wave_lds_barrier();
-      request(i + 1);  // (behind the last one: the last block again)
-      rows.template attend<1, decltype(masked_)::value>(keys, key_of(i), last_key, p.scale_log2e, [] {}, [] {});
-      wave_lds_barrier();
-    };
+    E2m1Keys<D> keys;
+    keys.scales = reinterpret_cast<_Float16*>(mine4 + kStages4 * stage4_bytes(D));
     if (mine > 0) {
-      request(0);
-      rows.template take_queries<F16Keys<D>::kPairedSlabs>(sm_k);
+      static_assert((kStages4 - 1) * stage4_bytes(D) >= 32 * D * 2, "the queries' room");
+#pragma unroll
+      for (int i = 0; i < kStages4; ++i) {
+        look_up(i);
+        request(i);
+        if (i == 0) {  // through the other tiles' room
+          rows.template take_queries<E2m1Keys<D>::kSlabs>(reinterpret_cast<half8*>(stage(1)));
+          lds_reads_done();
+        }
+      }
     }
+    auto step = [&](int i, auto masked_) {
+      constexpr bool kMasked = decltype(masked_)::value;
+      const int key0 = key_of(i);
+      look_up(i + kStages4);
+      wait_loads<(kStages4 - 1) * 2 * L::kLoads>();
+      keys.codes = stage(i);
+      keys.exponents = stage(i) + 2 * L::kBlock;
+      keys.set_k();
+      rows.template attend<1, kMasked>(
+          keys, key0, last_key, p.scale_log2e, [] {}, [&] { keys.template set_v<kMasked>(w.key_end - 1 - key0); });
+      lds_reads_done();
+      request(i + kStages4);
+    };
     int i = 0;
     for (; i < full; ++i) step(i, std::false_type());
     for (; i < mine; ++i) step(i, std::true_type());
@@ -1025,7 +1151,7 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
       look_up(0);
       request_k(0);
       lds_reads_done();  // (K's loads stay ahead of V's, as the waits count on)
-      rows.template take_queries<F16Keys<D>::kPairedSlabs>(sm_k + kTile);  // through V's room
+      rows.template take_queries<F16Keys<D>::kSlabs>(sm_k + kTile);  // through V's room
       lds_reads_done();
       request_v(0);
     }
@@ -1166,7 +1292,9 @@ __global__ __launch_bounds__(256) void attention_merge_kernel(AttnParams p, Attn
 
 // two tiles of many rows, or four states of few; as much as the keys of few, but for the exponents
 constexpr int lds_bytes(int head_dim, int source) {
-  return 2 * 2 * 64 * head_dim * 2 + (source == ATTN_E4M3 ? 4 * 2 * 2 * kExponentBytes : 0);
+  const int tiles = 2 * 2 * 64 * head_dim * 2;
+  if (source == ATTN_E2M1) return std::max(tiles, 4 * wave4_bytes(head_dim));
+  return tiles + (source == ATTN_E4M3 ? 4 * 2 * 2 * kExponentBytes : 0);
 }
 static_assert(2 * 2 * 64 * 2 == 4 * 32 * 4 && 4 * 2 * 32 * 2 == 4 * 32 * 4, "per channel");
 
