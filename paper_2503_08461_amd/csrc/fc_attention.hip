@@ -692,11 +692,13 @@ struct E4m3Keys {
 // (32 rows at one chunk) and V's transposing ones (rows 0-3, 8-11 and so on of a tile, 8 bytes each).
 // Through registers, with fp16 rows written to LDS and read from there, the LDS is busy for 1280 of the 1600
 // cycles that a SIMD has for a tile at the memory's rate, so for 500.
-template <int D>
+// (kFew: for Keys16 below, whose transposing reads take rows 0-7 and 16-23, or the others, at a time)
+template <int D, bool kFew>
 __device__ __forceinline__ int chunk4(int r, int c) {
+  if constexpr (kFew) return D == 128 ? c ^ (((r >> 2) & 1) | ((r >> 4) & 1) << 1) : c ^ ((r >> 4) & 1);
   return D == 128 ? c ^ (((r >> 2) & 3) ^ ((r >> 4) & 1)) : c ^ ((r >> 3) & 1);
 }
-template <int D>
+template <int D, bool kFew>
 struct Loader4 {
   static constexpr int kRow = D / 2, kHalf = 16 * kRow, kBlock = 2 * kHalf;  // bytes: a row, K's of a block, a block
   static constexpr int kExpWords = D / 8;                                   // of a block's K, and of V
@@ -709,7 +711,7 @@ struct Loader4 {
     const int r = l / (kRow / 16), c = l % (kRow / 16);
 #pragma unroll
     for (int j = 0; j < 2; ++j)
-      at[j] = r * kRow + chunk4<D>(16 * j + r, c) * 16 + (D == 64 && lane >= 32 ? n_heads * kHalf : 0);
+      at[j] = r * kRow + chunk4<D, kFew>(16 * j + r, c) * 16 + (D == 64 && lane >= 32 ? n_heads * kHalf : 0);
     e_at = lane < kExpWords       ? (head * kExpWords + lane) * 4
            : lane < 2 * kExpWords ? ((n_heads + head) * kExpWords + lane - kExpWords) * 4
                                   : 1 << 30;
@@ -732,7 +734,7 @@ template <int D>
 struct E2m1Keys {
   static constexpr int kSlabs = 4;  // a 16-byte read of K is its lane's part of four slabs
   static constexpr int DT = D / 32, G = D / kE2m1Group;
-  typedef Loader4<D> L;
+  typedef Loader4<D, false> L;
   const uint8_t* codes;      // two blocks
   const uint8_t* exponents;  // of each
   _Float16* scales;          // V's powers of two [group][half of the wavefront][16 keys], the wavefront's own
@@ -750,7 +752,7 @@ struct E2m1Keys {
     const uint8_t* e = exponents + (r >> 4) * kExponentBytes + (r & 15) * G + half;
 #pragma unroll
     for (int j = 0; j < G / 2; ++j) {
-      k_part[j] = *reinterpret_cast<const uint4v*>(row(codes, r) + chunk4<D>(r, 2 * j + half) * 16);
+      k_part[j] = *reinterpret_cast<const uint4v*>(row(codes, r) + chunk4<D, false>(r, 2 * j + half) * 16);
       k_scale[j] = e4m3_scale(e[2 * j]);
     }
   }
@@ -777,7 +779,7 @@ struct E2m1Keys {
     const int r = (i >> 3) * 16 + ((i >> 2) & 1) * 8 + (lane >> 5) * 4 + (i & 3);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
-      v_part[dt] = read_code_columns(row(codes, r) + L::kHalf + chunk4<D>(r, dt) * 16 + ((lane >> 4) & 1) * 8);
+      v_part[dt] = read_code_columns(row(codes, r) + L::kHalf + chunk4<D, false>(r, dt) * 16 + ((lane >> 4) & 1) * 8);
   }
   __device__ __forceinline__ half8 v_slab(int, int kk, int dt) const {
     const half8 scale = *reinterpret_cast<const half8*>(scales + (dt * 2 + ((threadIdx.x & 63) >> 5)) * 16 + kk * 8);
@@ -1084,7 +1086,7 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
     for (; i < mine; ++i) step(i, std::true_type());
   } else if constexpr (SRC == ATTN_E2M1) {
     // Two tiles on their way while a third is worked on.
-    typedef Loader4<D> L;
+    typedef Loader4<D, false> L;
     const L loader(p.n_heads, head);
     uint8_t* mine4 = reinterpret_cast<uint8_t*>(sm) + wave * wave4_bytes(D);
     auto stage = [&](int i) { return mine4 + (i % kStages4) * stage4_bytes(D); };
@@ -1230,6 +1232,281 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
   }
 }
 
+// ---------------------------------------------------------------------------
+// Up to 16 rows of a head over 4 bits (single tokens of grouped heads): as the few rows above, on
+// v_mfma_f32_16x16x32_f16, a lane a row again, four lanes to each.  With the keys in so few bytes the
+// instructions are what a wavefront waits for: of 32 rows' softmax and products most are of rows that
+// there are not, and 222 registers leave a SIMD two wavefronts.  Here it has four.
+//   S^T: a lane reads a group of 32 channels of a key (16 at 64 channels); the queries' channels follow.
+//   O^T: a transposing read has eight keys of a lane's column for two tiles of 16 channels, one group.
+// ---------------------------------------------------------------------------
+constexpr int kFewRows = 16;
+constexpr int kFewStages = 2;
+constexpr int few_wave_bytes(int head_dim) { return kFewStages * stage4_bytes(head_dim) + 2 * head_dim; }
+
+__device__ __forceinline__ float quarter_max(float v) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  return other_half_max(v);
+}
+
+template <int D>
+struct Keys16 {
+  static constexpr int KS = D / 32, DT = D / 32, G = D / kE2m1Group;  // slabs of a key that a lane has; groups
+  typedef Loader4<D, true> L;
+  const uint8_t* codes;      // two blocks
+  const uint8_t* exponents;  // of each
+  _Float16* scales;          // V's powers of two [group][quarter of the wavefront][8 keys], the wavefront's own
+  uint32_t k_part[2][KS];
+  float k_scale[2];
+  int2v v_part[DT];
+  bool not_finite_seen;
+  __device__ __forceinline__ static const uint8_t* row(const uint8_t* codes, int r) { return codes + (r >> 4) * L::kBlock + (r & 15) * L::kRow; }
+  // where a key's scale of V lies: in the order of the products' keys
+  __device__ __forceinline__ static int place(int dt, int key) { return (dt * 4 + ((key >> 2) & 3)) * 8 + (key >> 4) * 4 + (key & 3); }
+  __device__ __forceinline__ void set_k() {
+    const int lane = threadIdx.x & 63, quarter = lane >> 4;
+    const int group = D == 128 ? quarter : quarter >> 1;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int r = 16 * t + (lane & 15);
+      const uint8_t* from = row(codes, r) + chunk4<D, true>(r, group) * 16;
+      if constexpr (D == 128) {
+        const uint4v c = *reinterpret_cast<const uint4v*>(from);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k_part[t][i] = c[i];
+      } else {
+        const uint2v c = *reinterpret_cast<const uint2v*>(from + (quarter & 1) * 8);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) k_part[t][i] = c[i];
+      }
+      k_scale[t] = e4m3_scale(exponents[t * kExponentBytes + (lane & 15) * G + group]);
+    }
+  }
+  // Keys behind `last` are seen by no row (and their slots may hold anything): times zero.
+  template <bool kMasked>
+  __device__ __forceinline__ void set_v(int last) {
+    const int lane = threadIdx.x & 63, key = lane & 31;
+    constexpr int kPer = DT / 2;  // scales that a lane makes
+    const uint8_t* e = exponents + (key >> 4) * kExponentBytes + L::kExpWords * 4 + (key & 15) * G + (lane >> 5) * kPer;
+    not_finite_seen = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const uint32_t x = e[i];
+      const bool seen = !kMasked || key <= last;
+      // (the code of 1, scaled: 255 << 23 makes it not a number)
+      const _Float16 f = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(0x22u, e4m3_scale(x), 0)[0];
+      scales[place((lane >> 5) * kPer + i, key)] = seen ? f : (_Float16)0.f;
+      if (kMasked && seen && x == kE2m1NotFinite) not_finite_seen = true;
+    }
+    wave_lds_barrier();
+    // rows of the transposing reads: eight keys, at 16 channels and at the next 16
+    const int i = lane & 7, r = (i >> 2) * 16 + (lane >> 4) * 4 + (i & 3);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      v_part[dt] = read_code_columns(row(codes, r) + L::kHalf + chunk4<D, true>(r, dt) * 16 + ((lane >> 3) & 1) * 8);
+  }
+  __device__ __forceinline__ half8 v_scales(int dt) const {
+    return *reinterpret_cast<const half8*>(scales + (dt * 4 + ((threadIdx.x & 63) >> 4)) * 8);
+  }
+};
+
+template <int D, bool kSplit, typename Reqs>
+__global__ __launch_bounds__(256, 4) void attention_few4_kernel(AttnParams p, Reqs reqs) {
+  extern __shared__ __align__(16) half8 sm[];
+  constexpr int kKeys = 32, KS = D / 32, CT = D / 16;
+  typedef Loader4<D, true> L;
+  const int unit = blockIdx.x / p.n_heads;
+  const int head = blockIdx.x - unit * p.n_heads;
+  const AttnLaunchView& l = p.launch[ATTN_FLAT];
+  const Place w = place_of<kFlatRows, kSplit>(p, reqs, l, unit);  // (no more rows than a tile: one a request)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, quarter = lane >> 4;
+  const int first_key = w.rq.seq_len - w.rq.n_new;
+  const LaneRow me = lane_row(p, lane & 15, w.n_rows);
+  const int last_key = min(first_key + me.token, w.key_end - 1);
+  const int first_seen = min(first_key, w.key_end - 1);  // all rows see keys up to this one
+  const int n_tiles = w.key_end > w.key_begin ? (w.key_end - w.key_begin + kKeys - 1) / kKeys : 0;
+  const int mine = own_tiles(n_tiles, wave, 4);
+  // tiles that every row sees whole come first
+  const int full = min(mine, own_tiles(max(first_seen + 1 - w.key_begin, 0) / kKeys, wave, 4));
+  const GroupRows from(p.q, w.rq, p, head), to(p.out, w.rq, p, head);
+
+  half8 q[KS];
+#pragma unroll
+  for (int i = 0; i < KS; ++i) {
+    const int at = i * 64 + lane;
+    q[i] = load_half8(from.at(lane_row(p, at / (D / 8), w.n_rows)) + (at % (D / 8)) * 8);
+  }
+  floatx4 o[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) o[c] = floatx4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, z = 0.f;
+
+  const int32_t* table = table_of(p, w.rq, head);
+  const L loader(p.n_heads, head);
+  uint8_t* own = reinterpret_cast<uint8_t*>(sm) + wave * few_wave_bytes(D);
+  auto stage = [&](int i) { return own + (i % kFewStages) * stage4_bytes(D); };
+  int ids[2] = {0, 0};
+  auto look_up = [&](int i) {
+    const int b = (w.key_begin >> 4) + 2 * (wave + 4 * i);
+    ids[0] = block_id(p, table, b, w.nb);
+    ids[1] = block_id(p, table, b + 1, w.nb);
+  };
+  // (tiles behind the last one are requested as nothing: every wait counts the same loads)
+  auto request = [&](int i) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      loader.request(static_cast<const uint8_t*>(p.kv) + (size_t)ids[j] * e2m1_block_bytes(p.n_heads, D), p.n_heads, head, j, i < mine,
+                     stage(i) + j * L::kBlock, stage(i) + 2 * L::kBlock + j * kExponentBytes);
+  };
+  Keys16<D> keys;
+  keys.scales = reinterpret_cast<_Float16*>(own + kFewStages * stage4_bytes(D));
+  if (mine > 0) {
+    look_up(0);
+    request(0);
+    look_up(1);
+    // the queries through the other tile's room
+    static_assert(stage4_bytes(D) >= kFewRows * D * 2, "room");
+    half8* room = reinterpret_cast<half8*>(stage(1));
+#pragma unroll
+    for (int i = 0; i < KS; ++i) room[k_chunk<D>((i * 64 + lane) / (D / 8), lane % (D / 8))] = q[i];
+    wave_lds_barrier();
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) q[kk] = room[k_chunk<D>(lane & 15, KS * quarter + kk)];
+    lds_reads_done();
+    request(1);
+  }
+  auto step = [&](int i, auto masked_) {
+    constexpr bool kMasked = decltype(masked_)::value;
+    const int key0 = w.key_begin + (wave + 4 * i) * kKeys;
+    look_up(i + kFewStages);
+    wait_loads<(kFewStages - 1) * 2 * L::kLoads>();
+    keys.codes = stage(i);
+    keys.exponents = stage(i) + 2 * L::kBlock;
+    keys.set_k();
+    keys.template set_v<kMasked>(w.key_end - 1 - key0);
+    floatx4 s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(e2m1_values(keys.k_part[t][kk], keys.k_scale[t]), q[kk], s[t], 0, 0, 0);
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if constexpr (kMasked) {
+          if (key0 + t * 16 + quarter * 4 + r > last_key) s[t][r] = -INFINITY;
+        }
+        top = fmaxf(top, s[t][r]);
+      }
+    // m follows the maximum when that is more than kSlack ahead, as in Rows32
+    const float mn = fmaxf(m, quarter_max(top) * p.scale_log2e);
+    if (__any(mn > m + kSlack)) {
+      const float a = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      z *= a;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) o[c] *= a;
+      m = mn;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+    half8 pb;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[t][r], p.scale_log2e, -base));
+        z += x;
+        pb[t * 4 + r] = (_Float16)x;
+      }
+    // Where some row does not see some key, 0 * NaN must not reach it: as in Rows32
+    bool dirty = false;
+    if constexpr (kMasked) {
+      dirty = __any(key0 + kKeys - 1 > last_key) && __any(keys.not_finite_seen);
+      if (dirty) {
+#pragma unroll 1
+        for (int key = 0; key < kKeys; ++key) {
+          if (key0 + key > last_key) continue;
+#pragma unroll
+          for (int c = 0; c < CT; ++c)
+            if (abs_bits(keys.scales[Keys16<D>::place(c / 2, key)]) >= 0x7c00u) o[c] += __builtin_nanf("");
+        }
+      }
+    }
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) {
+      const half8 scale = keys.v_scales(dt);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        half8 v = e2m1_values(keys.v_part[dt][h], 1.f) * scale;
+        if constexpr (kMasked) {
+          if (dirty) v = finite_only(v);
+        }
+        o[2 * dt + h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pb, o[2 * dt + h], 0, 0, 0);
+      }
+    }
+    lds_reads_done();
+    request(i + kFewStages);
+  };
+  int i = 0;
+  for (; i < full; ++i) step(i, std::false_type());
+  for (; i < mine; ++i) step(i, std::true_type());
+  wait_loads<0>();
+  z = quarter_sum(z);
+
+  // ---- joining the four states, as above ---------------------------------------------------
+  __shared__ float sm_m[4][kFewRows], sm_z[4][kFewRows];
+  if (quarter == 0) {
+    sm_m[wave][lane] = m;
+    sm_z[wave][lane] = z;
+  }
+  __syncthreads();  // (and every wavefront is done with its keys)
+  float mm = -INFINITY, zz = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) mm = fmaxf(mm, sm_m[k][lane & 15]);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float zk = sm_z[k][lane & 15];
+    zz += zk == 0.f ? 0.f : zk * __builtin_amdgcn_exp2f(sm_m[k][lane & 15] - mm);
+  }
+  const float log2_sum = zz == 0.f ? -INFINITY : mm + __builtin_amdgcn_logf(zz);
+  const float f = z == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - mm) / zz;
+  constexpr int kQuads = D / 4;
+  floatx4* sm_o = reinterpret_cast<floatx4*>(sm);
+  static_assert(4 * kFewRows * kQuads * 16 <= 4 * few_wave_bytes(D), "room");
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+    sm_o[(wave * kFewRows + (lane & 15)) * kQuads + ((c * 4 + quarter) ^ (lane & 15))] = o[c] * f;
+  if (wave == 0 && quarter == 0 && me.real) {
+    const int q_head = head * p.group + me.in_group;
+    if (kSplit && w.n_seg > 1)
+      state_of<D>(p, l, w.rq, me.token, q_head, w.seg)[D] = log2_sum;
+    else
+      write_lse(p, w.rq, me.token, q_head, log2_sum);
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < kFewRows * kQuads; k += 256) {
+    const int r = k / kQuads, c = k % kQuads;
+    const LaneRow it = lane_row(p, r, w.n_rows);
+    if (!it.real) break;
+    floatx4 x = sm_o[r * kQuads + (c ^ r)];
+#pragma unroll
+    for (int n = 1; n < 4; ++n) x += sm_o[(n * kFewRows + r) * kQuads + (c ^ r)];
+    if (kSplit && w.n_seg > 1) {
+      *reinterpret_cast<floatx4*>(state_of<D>(p, l, w.rq, it.token, head * p.group + it.in_group, w.seg) + c * 4) = x;
+    } else {
+      half4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = (_Float16)f16_result(x[e]);
+      *reinterpret_cast<half4*>(to.at(it) + c * 4) = y;
+    }
+  }
+}
+
 // The units with many rows come first: they are the heavy ones.
 template <int D, int SRC, bool kSplit, typename Reqs>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, Reqs reqs) {
@@ -1301,6 +1578,12 @@ static_assert(2 * 2 * 64 * 2 == 4 * 32 * 4 && 4 * 2 * 32 * 2 == 4 * 32 * 4, "per
 template <int D, int SRC, bool kSplit, typename Reqs>
 void launch_kernel(const AttnParams& p, const Reqs& reqs, hipStream_t s) {
   const unsigned grid = (unsigned)(p.launch[0].n_units + p.launch[1].n_units) * p.n_heads;
+  if constexpr (SRC == ATTN_E2M1) {
+    if (p.launch[ATTN_TALL].n_units == 0 && p.launch[ATTN_FLAT].most_rows <= kFewRows) {
+      attention_few4_kernel<D, kSplit, Reqs><<<grid, 256, 4 * few_wave_bytes(D), s>>>(p, reqs);
+      return;
+    }
+  }
   attention_kernel<D, SRC, kSplit, Reqs><<<grid, 256, lds_bytes(D, SRC), s>>>(p, reqs);
 }
 

@@ -33,27 +33,31 @@ int sparse_attention(fc_pool* p, int layer, const int32_t* dev_block_tables, int
   if ((rc = check_q_heads(p, n_q_heads)) || (rc = check_aligned(dev_bounds, 16, "dev_bounds"))) return rc;
   if (reinterpret_cast<uintptr_t>(dev_selected) & 3) return fail(FC_EINVAL, "dev_selected must be 4-byte aligned");
   SparsePlan plan;
-  if (plan_sparse(geometry(p), p->n_cu, n_select, chunk, &plan) != PLAN_OK) return fail(plan.code, "%s", plan.message);
+  if (plan_sparse(geometry(p), p->n_cu, n_q_heads / p->n_heads, n_select, chunk, &plan) != PLAN_OK) return fail(plan.code, "%s", plan.message);
   if ((rc = check_rows(q, "q", chunk.n_rows, n_q_heads, p->head_dim, false)) ||
       (rc = check_rows(out, "out", chunk.n_rows, n_q_heads, p->head_dim, true)))
     return rc;
   AttnLaunch launches[ATTN_KINDS];
-  if (plan_attention(geometry(p), p->n_cu, n_q_heads / p->n_heads, true, p->max_states, &plan.attention, launches) != PLAN_OK)
+  if (plan_attention(geometry(p), p->n_cu, n_q_heads / p->n_heads, true, p->max_states, &plan.attention, launches,
+                     p->dtype == FC_DTYPE_E2M1) != PLAN_OK)
     return fail(plan.attention.code, "%s", plan.attention.message);
 
   // (what may grow grows before the descriptors are on their way)
-  const int64_t heads = chunk.n_rows * p->n_heads;
-  const size_t key_bytes = plan.part_blocks ? (size_t)heads * plan.key_stride * sizeof(uint64_t) : 0;
-  if ((rc = scratch_for(p, &p->sparse, key_bytes + (size_t)heads * n_select * sizeof(int32_t), stream))) return rc;
+  const size_t heads = (size_t)chunk.n_rows * p->n_heads;
+  const size_t score_bytes = plan.part_blocks ? heads * plan.longest * sizeof(float) : 0;
+  const size_t most_bytes = (size_t)plan.n_units * p->n_heads * sizeof(uint32_t);
+  if ((rc = scratch_for(p, &p->sparse, score_bytes + most_bytes + heads * n_select * sizeof(int32_t), stream))) return rc;
   std::vector<ChunkReq> reqs(plan.tokens);
   const std::vector<ChunkReq> attended = attention_reqs(launches);
-  ChunkReqs token_reqs, attention_inline;
+  ChunkReqs token_reqs, scored_reqs, attention_inline;
   const ChunkReq* on_device = nullptr;
   if (reqs.size() <= ChunkReqs::kInline) {
     std::copy(reqs.begin(), reqs.end(), token_reqs.req);
+    std::copy(plan.scored.begin(), plan.scored.end(), scored_reqs.req);
     std::copy(attended.begin(), attended.end(), attention_inline.req);
   } else {
     reqs.insert(reqs.end(), attended.begin(), attended.end());
+    reqs.insert(reqs.end(), plan.scored.begin(), plan.scored.end());
     const void* at = nullptr;
     if ((rc = meta_to_device(p, reqs.data(), reqs.size() * sizeof(ChunkReq), &at, stream))) return rc;
     on_device = static_cast<const ChunkReq*>(at);
@@ -67,18 +71,22 @@ int sparse_attention(fc_pool* p, int layer, const int32_t* dev_block_tables, int
   sp.head_dim = p->head_dim;
   sp.block_tables = dev_block_tables;
   sp.max_blocks = max_blocks;
-  sp.reqs = on_device;
+  sp.tokens = on_device;
   sp.n_tokens = (int)chunk.n_rows;
   sp.q = view(q);
   sp.n_select = n_select;
-  sp.part_blocks = plan.part_blocks;
-  sp.n_units = (int)plan.n_units;
-  sp.keys = reinterpret_cast<uint64_t*>(p->sparse.data);
-  sp.key_stride = plan.key_stride;
-  sp.lds_keys = plan.part_blocks ? 0 : plan.key_stride;
-  sp.ids = reinterpret_cast<int32_t*>(p->sparse.data + key_bytes);
+  sp.scores = reinterpret_cast<float*>(p->sparse.data);
+  sp.most = reinterpret_cast<uint32_t*>(p->sparse.data + score_bytes);
+  sp.ids = reinterpret_cast<int32_t*>(p->sparse.data + score_bytes + most_bytes);
   sp.selected = dev_selected;
-  FC_HIP(launch_select_blocks(sp, token_reqs, stream));
+  sp.lds_keys = plan.longest;
+  sp.part_blocks = plan.part_blocks;
+  sp.tile_tokens = plan.tile_tokens;
+  sp.reqs = on_device ? on_device + plan.tokens.size() + attended.size() : nullptr;
+  sp.n_req = (int)plan.scored.size();
+  sp.n_units = (int)plan.n_units;
+  sp.score_stride = plan.longest;
+  FC_HIP(launch_select_blocks(sp, token_reqs, scored_reqs, stream));
 
   AttnParams ap = {};
   ap.kv = layer_blocks(p, layer);

@@ -105,6 +105,7 @@ inline void set_launches(const fc_pool* p, const AttnLaunch launches[ATTN_KINDS]
     a.n_units = (int)l.n_units;
     a.seg_blocks = std::max(l.seg_blocks, 1);
     a.n_seg = l.n_seg;
+    for (const ChunkReq& q : l.reqs) a.most_rows = (int)std::max<int64_t>(a.most_rows, (int64_t)q.n_new * ap->group);
     first_req += a.n_req;
     if (l.n_seg > 1) {
       a.state_rows = (int)l.state_rows;

@@ -78,7 +78,7 @@ int plan_store_units(ChunkPlan* plan) {
 }
 
 int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, int64_t max_states,
-                   ChunkPlan* plan, AttnLaunch launches[kAttnKinds]) {
+                   ChunkPlan* plan, AttnLaunch launches[kAttnKinds], bool four_bits) {
   for (int s = 0; s < kAttnKinds; ++s) launches[s] = AttnLaunch();
   // Few rows of a head are those of one tile that shares the keys.  What 33-127 rows cost as many
   // rows / as two to four tiles of few, each of which reads the keys again (the attention, us):
@@ -127,7 +127,8 @@ int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, in
     const int64_t room = states_left / (l.state_rows * n_q_heads);  // segments of a row
     if (room >= 2) {
       const int64_t wanted = s == 0 ? (slots + units - 1) / units : 1;
-      const int64_t seg = std::max<int64_t>({s == 0 ? (longest + wanted - 1) / wanted : total / slots, kPlanMinSegment,
+      const int64_t least = four_bits && s == 1 ? std::max(16, (longest + 63) / 64) : kPlanMinSegment;
+      const int64_t seg = std::max<int64_t>({s == 0 ? (longest + wanted - 1) / wanted : total / (four_bits ? 2 * slots : slots), least,
                                              (longest + room - 1) / room});
       if (2 * seg <= longest) {
         l.seg_blocks = (int)seg;
@@ -169,38 +170,52 @@ int plan_bounds(ChunkPlan* plan) {
   return PLAN_OK;
 }
 
-int plan_sparse(const PoolView& pool, int n_cu, int n_select, const ChunkPlan& chunk, SparsePlan* plan) {
+int plan_sparse(const PoolView& pool, int n_cu, int group, int n_select, const ChunkPlan& chunk, SparsePlan* plan) {
   *plan = SparsePlan();
   if (n_select < 1 || n_select > kPlanMaxSeqLen / kPlanBlockSize)
     return fail(plan, PLAN_EINVAL, "n_select %d outside 1..%d", n_select, kPlanMaxSeqLen / kPlanBlockSize);
   if (chunk.n_rows * pool.n_heads > kPlanMaxWorkgroups) return fail(plan, PLAN_EINVAL, "batch too large for one launch");
-  int longest = 0;
-  int64_t scored = 0;  // blocks, of one head
-  for (const ChunkReq& q : chunk.reqs)
+  bool single = true;
+  // (with one block, the token's own, nothing is scored)
+  auto scores = [&](int nb) { return nb > n_select && n_select > 1; };
+  for (const ChunkReq& q : chunk.reqs) {
+    single = single && q.n_new == 1;
     for (int i = 0; i < q.n_new; ++i) {
       const int seen = q.seq_len - q.n_new + i + 1, nb = blocks_for(seen), row = q.row_off + i;
-      plan->tokens.push_back({q.table_row, seen, 1, row, 0, 0});
+      plan->tokens.push_back({q.table_row, seen, 0, row, 0, 0});
       // (whole blocks, but for the token's own, the last one)
       const int read = (std::min(nb, n_select) - 1) * kPlanBlockSize + (seen - 1) % kPlanBlockSize + 1;
       plan->attention.reqs.push_back({row, read, 1, row, 0, 0});
-      if (nb > n_select) {
-        longest = std::max(longest, nb);
-        scored += nb - 1;
-      }
+      if (scores(nb)) plan->longest = std::max(plan->longest, nb - 1);
     }
+  }
   plan->attention.n_rows = chunk.n_rows;
-  plan->key_stride = std::max(longest - 1, 1);
-  // Few heads leave CUs free, and one draws only so much: their scores are made by as many
-  // workgroups as fill the card, in a launch of its own.
-  const int64_t heads = chunk.n_rows * pool.n_heads;
-  if (longest > 64 && heads < 2 * (int64_t)std::max(n_cu, 1)) {
-    const int64_t wanted = 4 * (int64_t)std::max(n_cu, 1);
-    plan->part_blocks = (int)std::max<int64_t>(32, (scored * pool.n_heads + wanted - 1) / wanted);
-    for (ChunkReq& t : plan->tokens) {
-      t.unit_start = (int32_t)plan->n_units;
-      const int nb = blocks_for(t.seq_len);
-      if (nb > n_select) plan->n_units += (nb - 1 + plan->part_blocks - 1) / plan->part_blocks;
+  // One launch for scores and selection where its workgroups fill the card or have little to read (384 heads of
+  // 80-440 blocks: 64.7 us a step, with two 67.9); else the scores are made by as many as fill it, and for the
+  // tokens of a request together.  (Up to half of the
+  // rows: what else is kept of the queries and blocks would not fit the LDS beside more.)
+  const int cu = std::max(n_cu, 1);
+  if (single && group <= kScoreRows / 2 && (chunk.n_rows * pool.n_heads >= cu || plan->longest <= 64)) return PLAN_OK;
+  plan->tile_tokens = std::max(1, kScoreRows / group);
+  int64_t total = 0;  // blocks of all workgroups
+  auto tiles = [&](const ChunkReq& q) { return ((int64_t)q.n_new + plan->tile_tokens - 1) / plan->tile_tokens; };
+  for (const ChunkReq& q : chunk.reqs) {
+    const int nb = blocks_for(q.seq_len);
+    if (!scores(nb)) continue;
+    plan->scored.push_back(q);
+    plan->scored.back().state_off = nb - 1;
+    total += tiles(q) * (nb - 1) * pool.n_heads;
+  }
+  plan->part_blocks = (int)std::max<int64_t>(64, (total + 2 * cu - 1) / (2 * cu) + 15) & ~15;
+  for (ChunkReq& q : plan->scored) {
+    const int parts = (q.state_off + plan->part_blocks - 1) / plan->part_blocks;
+    q.unit_start = (int32_t)plan->n_units;
+    for (int i = 0; i < q.n_new; ++i) {
+      ChunkReq& t = plan->tokens[q.row_off + i];
+      t.unit_start = (int32_t)plan->n_units + i / plan->tile_tokens * parts;
+      t.n_new = parts;
     }
+    plan->n_units += tiles(q) * parts;
     if (plan->n_units * pool.n_heads > kPlanMaxWorkgroups) return fail(plan, PLAN_EINVAL, "batch too large for one launch");
   }
   return PLAN_OK;

@@ -49,7 +49,7 @@ struct AttnLaunch {
 // group: query heads per head of K and V; max_states: states that fit the pool's memory, 0 for
 // none.  FC_EINVAL (plan->code) where the launch would be too large.
 int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, int64_t max_states,
-                   ChunkPlan* plan, AttnLaunch launches[kAttnKinds]);
+                   ChunkPlan* plan, AttnLaunch launches[kAttnKinds], bool four_bits = false);
 
 // fc_rotate_store_chunk: plan->reqs get the position of their first new token (state_off), by
 // default that of the cache.  FC_EINVAL (plan->code) for one outside the table.
@@ -63,13 +63,16 @@ int plan_bounds(ChunkPlan* plan);
 struct SparsePlan {
   int code = PLAN_OK;
   char message[256] = "";
-  std::vector<ChunkReq> tokens;  // one a new token, row_off its packed row, unit_start its first part
-  ChunkPlan attention;           // the same as requests of their own, of the blocks that they read
+  std::vector<ChunkReq> tokens;  // one a new token, row_off its packed row; unit_start and n_new: its scores' parts
+  std::vector<ChunkReq> scored;  // requests whose scores are made in a launch of their own, state_off blocks each
+  ChunkPlan attention;           // the tokens as requests of their own, of the blocks that they read
   int part_blocks = 0;           // 0: a workgroup scores and selects, else blocks a workgroup that scores
-  int64_t n_units = 0;           // parts of all tokens
-  int key_stride = 0;            // scores kept of a token's head
+  int tile_tokens = 1;           // ... and tokens of a request at a time
+  int64_t n_units = 0;           // ... parts of all
+  int longest = 1;               // most blocks that a token scores
 };
-int plan_sparse(const PoolView& pool, int n_cu, int n_select, const ChunkPlan& chunk, SparsePlan* plan);
+static constexpr int kScoreRows = 64;  // rows (tokens x query heads of a group) of a workgroup that scores
+int plan_sparse(const PoolView& pool, int n_cu, int group, int n_select, const ChunkPlan& chunk, SparsePlan* plan);
 
 // fc_quantise_batch: a unit is a block of a request.
 int plan_quantise(int n_req, int dst_max_blocks, int src_max_blocks, const int32_t* seq_lens,

@@ -134,24 +134,30 @@ struct BoundsParams {
   _Float16* bounds;      // the layer's [block][head][2][d]
 };
 
-// Blocks with the best scores, of every token and head (fc_sparse.hip).  The requests: one a
-// token, table_row its request's, seq_len the tokens it sees, row_off its packed row.
+// Blocks with the best scores, of every token and head (fc_sparse.hip).
 struct SelectParams {
   const _Float16* bounds;  // the layer's
   int32_t n_blocks, n_heads, group, head_dim;
   const int32_t* block_tables;
   int32_t max_blocks;
-  const ChunkReq* reqs;    // NULL: in the ChunkReqs argument; a token's unit_start: its first part
+  // One a token: table_row its request's, seq_len the tokens it sees, row_off its packed row;
+  // with part_blocks, unit_start and n_new where its scores' parts are.  NULL: in the argument.
+  const ChunkReq* tokens;
   int32_t n_tokens;
   RowsView q;
   int32_t n_select;
-  int32_t part_blocks;     // scores in a launch of their own: blocks a workgroup, else 0
-  int32_t n_units;         // ... and parts of all tokens
-  uint64_t* keys;          // ... and their scores' order, [token][head][key_stride]
-  int32_t key_stride;
-  int32_t lds_keys;        // no launch of their own: keys of the longest cache
   int32_t* ids;            // [token][head][n_select] blocks of the pool, ascending in the request's table
   int32_t* selected;       // nullable: the same as entries of the table, -1 behind the last
+  int32_t lds_keys;        // blocks that any token scores, at most
+  // Scores in a launch of their own (part_blocks 0: not): parts of part_blocks blocks, tile_tokens
+  // tokens of a request at a time.  One a request that scores: n_new tokens from row_off on,
+  // state_off blocks, unit_start.
+  int32_t part_blocks, tile_tokens;
+  const ChunkReq* reqs;    // NULL: in the argument
+  int32_t n_req, n_units;
+  float* scores;           // [token][head][score_stride]
+  int32_t score_stride;
+  uint32_t* most;          // [unit][head] largest magnitude of a bound, as fp16 bits
 };
 
 struct QuantiseParams {
@@ -174,6 +180,7 @@ struct AttnLaunchView {
   int32_t n_units;            // row tiles x segments
   int32_t seg_blocks, n_seg;  // blocks per segment of a head, segments of the longest one
   int32_t state_rows;         // rows (tokens) that have states
+  int32_t most_rows;          // most rows (tokens x query heads of a group) of a request
   float* states;              // [row][head][n_seg][DecodeParams::state_words]
 };
 struct AttnParams {
@@ -335,7 +342,7 @@ hipError_t launch_quantise(const QuantiseParams& p, const ChunkReqs& inline_reqs
 hipError_t launch_rotate_store(const RotateParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
 // bounds of blocks, and the blocks that queries select by them (fc_sparse.hip)
 hipError_t launch_bounds(const BoundsParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
-hipError_t launch_select_blocks(const SelectParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
+hipError_t launch_select_blocks(const SelectParams& p, const ChunkReqs& inline_tokens, const ChunkReqs& inline_reqs, hipStream_t s);
 // attention of chunks (fc_attention.hip)
 hipError_t attention_one_time_setup();
 hipError_t launch_attention(const AttnParams& p, const ChunkReqs& inline_reqs, hipStream_t s);

@@ -29,9 +29,9 @@ hipError_t launch_rotate_store(const RotateParams& p, const ChunkReqs& reqs, hip
 hipError_t launch_bounds(const BoundsParams& p, const ChunkReqs&, hipStream_t) {
   return launched(("bounds" + std::to_string(p.format) + ":" + std::to_string(p.n_units)).c_str());
 }
-hipError_t launch_select_blocks(const SelectParams& p, const ChunkReqs& reqs, hipStream_t) {
-  std::string s = "select" + std::string(p.reqs ? "" : "_inline") + ":" + std::to_string(p.n_tokens) + ":" + std::to_string(p.part_blocks ? 1 : 0) +
-                  ":" + std::to_string(p.lds_keys);
+hipError_t launch_select_blocks(const SelectParams& p, const ChunkReqs&, const ChunkReqs&, hipStream_t) {
+  std::string s = "select" + std::string(p.tokens ? "" : "_inline") + ":" + std::to_string(p.n_tokens) + ":" + std::to_string(p.n_req) + "x" +
+                  std::to_string(p.n_units) + ":" + std::to_string(p.lds_keys);
   return launched(s.c_str());
 }
 }  // namespace fc
