@@ -307,6 +307,27 @@ __device__ __forceinline__ void values_of(uint4v codes, float scale, float (&f)[
   for (int w = 0; w < 4; ++w) e2m1_floats(codes[w], scale, f + 8 * w);
 }
 
+// stream_tiles with three tiles on their way: of 4 bits a tile is 2 KB (heads cut into segments, 16 caches of
+// 130-16384 tokens, 32 heads: 118.5 -> 110.6 us; whole heads gain nothing by it).
+template <typename Tile, typename Load, typename Use>
+__device__ __forceinline__ void stream_tiles_deep(int n, Load load, Use use) {
+  if (n <= 0) return;
+  Tile t[4];
+  auto request = [&](int i, Tile& tile) {  // (behind the last one: the last one again)
+    load(min(i, n - 1), tile);
+    requests_first();
+  };
+#pragma unroll
+  for (int j = 0; j < 3; ++j) request(j, t[j]);
+  for (int i = 0; i < n; i += 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      request(i + j + 3, t[(j + 3) % 4]);
+      if (i + j < n) use(i + j, t[j]);
+    }
+  }
+}
+
 template <int D, int kFormat, int W, bool kCut, typename Reqs>
 __global__ __launch_bounds__(64 * W) void decode_attention_codes_kernel(DecodeParams p, Reqs reqs) {
   constexpr bool k4 = kFormat == ROWS_E2M1;
@@ -380,8 +401,15 @@ __global__ __launch_bounds__(64 * W) void decode_attention_codes_kernel(DecodePa
       float f[CPL];
       values_of(x.k[i], e4m3_scale(x.ke[i]), f);
       float s = 0.f;
+      if constexpr (k4) {  // (four sums: one waits for itself 32 times)
+        float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int e = 0; e < CPL; ++e) s += qf[e] * f[e];
+        for (int e = 0; e < CPL; ++e) part[e % 4] += qf[e] * f[e];
+        s = (part[0] + part[1]) + (part[2] + part[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) s += qf[e] * f[e];
+      }
       s = short_row_sum<LPR>(s);
       if constexpr (!k4) s *= e4m3_scale(x.ke[i]);
       const int tok = (b0 + t * BPT) * 16 + i * RPI + grp;
@@ -416,12 +444,16 @@ __global__ __launch_bounds__(64 * W) void decode_attention_codes_kernel(DecodePa
       }
     }
   };
-  stream_tiles<Rows>(
-      own_tiles((b1 - b0 + BPT - 1) / BPT, wave, W), [&](int i, Rows& x) { fetch(wave + W * i, x); },
-      [&](int i, const Rows& x) { attend(wave + W * i, x); });
+  auto request = [&](int i, Rows& x) { fetch(wave + W * i, x); };
+  auto use = [&](int i, const Rows& x) { attend(wave + W * i, x); };
+  const int tiles = own_tiles((b1 - b0 + BPT - 1) / BPT, wave, W);
+  if constexpr (k4 && kCut)
+    stream_tiles_deep<Rows>(tiles, request, use);
+  else
+    stream_tiles<Rows>(tiles, request, use);
 
   // merge the states: of a wavefront's rows by lane exchanges, then of the wavefronts
-  auto join = [&](auto step) {
+  auto join = [&](auto step, auto first) {  // (first: channels from this one on are given away before)
     constexpr int kStep = decltype(step)::value;
     float m0, m1, z0, z1;
     two_lanes<kStep>(m, m0, m1);
@@ -430,27 +462,50 @@ __global__ __launch_bounds__(64 * W) void decode_attention_codes_kernel(DecodePa
     // (a sum of zero: no token; not a number stays not a number)
     const float f0 = z0 == 0.f ? 0.f : __builtin_amdgcn_exp2f(m0 - m), f1 = z1 == 0.f ? 0.f : __builtin_amdgcn_exp2f(m1 - m);
     z = z0 * f0 + z1 * f1;
+    constexpr int kLeft = decltype(first)::value;
+    if constexpr (k4 && kStep >= 16) {
+      // each half of the lanes goes on with half of the channels: one exchange brings either its own and the other's
 #pragma unroll
-    for (int e = 0; e < CPL; ++e) {
-      float x0, x1;
-      two_lanes<kStep>(acc[e], x0, x1);
-      acc[e] = x0 * f0 + x1 * f1;
+      for (int e = 0; e < kLeft / 2; ++e) {
+        const auto x = kStep == 32
+                           ? __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[e]), __float_as_uint(acc[e + kLeft / 2]), false, false)
+                           : __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[e]), __float_as_uint(acc[e + kLeft / 2]), false, false);
+        acc[e] = __uint_as_float(x[0]) * f0 + __uint_as_float(x[1]) * f1;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kLeft; ++e) {
+        float x0, x1;
+        two_lanes<kStep>(acc[e], x0, x1);
+        acc[e] = x0 * f0 + x1 * f1;
+      }
     }
   };
-  if constexpr (LPR <= 2) join(std::integral_constant<int, 2>());
-  if constexpr (LPR <= 4) join(std::integral_constant<int, 4>());
-  join(std::integral_constant<int, 8>());
-  join(std::integral_constant<int, 16>());
-  join(std::integral_constant<int, 32>());
+  constexpr int kEnd = k4 ? CPL / 4 : CPL;  // channels that a lane ends with
+  typedef std::integral_constant<int, CPL> All;
+  typedef std::integral_constant<int, kEnd> End;
+  if constexpr (k4) {
+    join(std::integral_constant<int, 32>(), All());
+    join(std::integral_constant<int, 16>(), std::integral_constant<int, CPL / 2>());
+    if constexpr (LPR <= 2) join(std::integral_constant<int, 2>(), End());
+    join(std::integral_constant<int, 4>(), End());
+    join(std::integral_constant<int, 8>(), End());
+  } else {
+    if constexpr (LPR == 4) join(std::integral_constant<int, 4>(), All());
+    join(std::integral_constant<int, 8>(), All());
+    join(std::integral_constant<int, 16>(), All());
+    join(std::integral_constant<int, 32>(), All());
+  }
   __shared__ float sm_m[W], sm_z[W];
   __shared__ float sm_acc[W][D];
   if (lane == 0) {
     sm_m[wave] = m;
     sm_z[wave] = z;
   }
-  if (grp == 0) {
+  if (k4 ? (lane & 15) < LPR : grp == 0) {
+    const int at = piece * CPL + (k4 ? (lane >> 5) * (CPL / 2) + ((lane >> 4) & 1) * (CPL / 4) : 0);
 #pragma unroll
-    for (int e = 0; e < CPL; ++e) sm_acc[wave][piece * CPL + e] = acc[e];
+    for (int e = 0; e < kEnd; ++e) sm_acc[wave][at + e] = acc[e];
   }
   __syncthreads();
   float mm = -INFINITY, zz = 0.f, o = 0.f;

@@ -64,29 +64,48 @@ __global__ __launch_bounds__(256) void rotate_store_kernel(RotateParams p, Reqs 
       w.sin[i] = kInterleaved ? (i % 2 ? s[i / 2] : -s[i / 2]) : second ? s[i] : -s[i];
     }
   }
-  const int n_kv = 2 * st.n_heads;
-  for (int i = threadIdx.x / PPR; i < n_kv + p.n_q_heads; i += 256 / PPR) {
-    // K's rows, V's, then the queries'
+  const int n_kv = 2 * st.n_heads, n_rows = n_kv + p.n_q_heads;
+  // rows: K's, V's, then the queries'; the next one is requested before this one is worked on
+  struct Row {
+    half8 x, y;
+  };
+  auto request = [&](int i, Row& r) {
     const bool q = i >= n_kv, v = !q && i >= st.n_heads;
     const RowsView& from = q ? p.q : v ? st.v : st.k;
     const int head = q ? i - n_kv : v ? i - st.n_heads : i;
-    const _Float16* x_at = from.data + (int64_t)row * from.token_stride + (int64_t)head * from.head_stride + piece * 8;
-    half8 x = load_half8(x_at);
+    const _Float16* at_row = from.data + (int64_t)row * from.token_stride + (int64_t)head * from.head_stride + piece * 8;
+    r.x = load_half8(at_row);
+    if constexpr (!kInterleaved) r.y = load_half8(at_row + (turned && !v ? partner : 0));
+    requests_first();
+  };
+  auto work = [&](int i, const Row& r) {
+    const bool q = i >= n_kv, v = !q && i >= st.n_heads;
+    half8 x = r.x;
     if (turned && !v) {
-      const half8 y = kInterleaved ? x : load_half8(x_at + partner);
-      half8 z;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const double own = (double)(float)x[e], other = (double)(float)y[kInterleaved ? e ^ 1 : e];
-        z[e] = rounded(__builtin_fma(own, w.cos[e], other * w.sin[e]));
+        const double own = (double)(float)r.x[e], other = (double)(float)(kInterleaved ? r.x[e ^ 1] : r.y[e]);
+        x[e] = rounded(__builtin_fma(own, w.cos[e], other * w.sin[e]));
       }
-      x = z;
     }
     if (q)
       // (q itself, perhaps: the wavefront that has the row has read all of it)
-      store_half8(p.q_out.data + (int64_t)row * p.q_out.token_stride + (int64_t)head * p.q_out.head_stride + piece * 8, x);
+      store_half8(p.q_out.data + (int64_t)row * p.q_out.token_stride + (int64_t)(i - n_kv) * p.q_out.head_stride + piece * 8, x);
     else
       write_piece<D, kFormat>(st.kv, blk, st.n_heads, i, slot, piece, x);
+  };
+  constexpr int kStep = 256 / PPR;
+  int i = threadIdx.x / PPR;
+  if (i >= n_rows) return;
+  Row a, b;
+  request(i, a);
+  while (true) {  // (behind the last row: the last one again, and nothing is made of it)
+    request(min(i + kStep, n_rows - 1), b);
+    work(i, a);
+    if ((i += kStep) >= n_rows) break;
+    request(min(i + kStep, n_rows - 1), a);
+    work(i, b);
+    if ((i += kStep) >= n_rows) break;
   }
 }
 

@@ -25,48 +25,55 @@ void with_reqs_of(const ChunkReq* on_device, const ChunkReqs& inline_reqs, F f) 
 }
 
 // ---------------------------------------------------------------------------
-// bounds: workgroup = block of a request; D / 8 neighbouring lanes a head, eight channels each, walk
-// the block's rows.  Memory bounds it: K is read once.
+// bounds: workgroup = block of a request; a lane has 16 bytes of a head's rows, 8, 16 or 32 channels, and walks the
+// block's 16 rows.  Memory bounds it: K is read once.
 // ---------------------------------------------------------------------------
-template <int D, int kFormat>
-__device__ __forceinline__ half8 key_channels(const void* layer, int blk, int n_heads, int head, int slot, int piece) {
-  const size_t row = (size_t)head * 16 + slot;
-  if constexpr (kFormat == ROWS_E4M3) {
-    const uint8_t* block = static_cast<const uint8_t*>(layer) + (size_t)blk * e4m3_block_bytes(n_heads, D);
-    const uint2v c = *reinterpret_cast<const uint2v*>(block + row * D + piece * 8);
-    return e4m3_values(c[0], c[1], e4m3_scale(block[(size_t)2 * n_heads * 16 * D + row]));
-  } else if constexpr (kFormat == ROWS_E2M1) {
-    const uint8_t* block = static_cast<const uint8_t*>(layer) + (size_t)blk * e2m1_block_bytes(n_heads, D);
-    const uint32_t c = *reinterpret_cast<const uint32_t*>(block + row * (D / 2) + piece * 4);
-    return e2m1_values(c, e4m3_scale(block[e2m1_code_bytes(n_heads, D) + row * (D / 32) + piece / 4]));
-  } else {
-    return load_half8(static_cast<const _Float16*>(layer) + (size_t)blk * 2 * n_heads * 16 * D + row * D + piece * 8);
-  }
-}
-
 template <int D, int kFormat, typename Reqs>
 __global__ __launch_bounds__(256) void bounds_kernel(BoundsParams p, Reqs reqs) {
-  constexpr int PPR = D / 8;
+  constexpr int C = kFormat == ROWS_F16 ? 8 : kFormat == ROWS_E4M3 ? 16 : 32;  // channels of a lane
+  constexpr int LPR = D / C;
   const ChunkReq rq = reqs.req[request_of(0, p.n_req, blockIdx.x, [&](int i) { return reqs.req[i].unit_start; })];
   const int b = rq.row_off + (int)blockIdx.x - rq.unit_start;
   const int blk = clamp_block(p.block_tables[(size_t)rq.table_row * p.max_blocks + b], p.n_blocks);
   const int tokens = min(16, rq.seq_len - b * 16);
-  const int piece = threadIdx.x % PPR;
-  for (int head = threadIdx.x / PPR; head < p.n_heads; head += 256 / PPR) {
-    half8 x[16];
+  const int piece = threadIdx.x % LPR;
+  const size_t bytes = kFormat == ROWS_E4M3   ? e4m3_block_bytes(p.n_heads, D)
+                       : kFormat == ROWS_E2M1 ? e2m1_block_bytes(p.n_heads, D)
+                                              : (size_t)2 * p.n_heads * 16 * D * sizeof(_Float16);
+  const uint8_t* block = static_cast<const uint8_t*>(p.kv) + (size_t)blk * bytes;
+  for (int head = threadIdx.x / LPR; head < p.n_heads; head += 256 / LPR) {
+    const uint8_t* rows = block + (size_t)head * 16 * LPR * 16 + piece * 16;
+    uint4v x[16];
+    uint32_t e[16];
 #pragma unroll
-    for (int s = 0; s < 16; ++s)  // (behind the last token: the last one)
-      x[s] = key_channels<D, kFormat>(p.kv, blk, p.n_heads, head, min(s, tokens - 1), piece);
-    half8 lo = x[0], hi = x[0];
-#pragma unroll
-    for (int s = 1; s < 16; ++s) {
-      // (not a number, where one is)
-      lo = __builtin_elementwise_minimum(lo, x[s]);
-      hi = __builtin_elementwise_maximum(hi, x[s]);
+    for (int s = 0; s < 16; ++s) {  // (behind the last token: the last one)
+      const int row = min(s, tokens - 1);
+      x[s] = __builtin_nontemporal_load(reinterpret_cast<const uint4v*>(rows + row * LPR * 16));
+      if constexpr (kFormat == ROWS_E4M3) e[s] = block[(size_t)2 * p.n_heads * 16 * D + head * 16 + row];
+      if constexpr (kFormat == ROWS_E2M1) e[s] = block[e2m1_code_bytes(p.n_heads, D) + (head * 16 + row) * LPR + piece];
     }
-    _Float16* to = p.bounds + ((size_t)blk * p.n_heads + head) * 2 * D + piece * 8;
-    store_half8(to, lo);
-    store_half8(to + D, hi);
+    half8 lo[C / 8], hi[C / 8];
+#pragma unroll
+    for (int s = 0; s < 16; ++s)
+#pragma unroll
+      for (int i = 0; i < C / 8; ++i) {
+        half8 y;
+        if constexpr (kFormat == ROWS_E4M3)
+          y = e4m3_values(x[s][2 * i], x[s][2 * i + 1], e4m3_scale(e[s]));
+        else if constexpr (kFormat == ROWS_E2M1)
+          y = e2m1_values(x[s][i], e4m3_scale(e[s]));
+        else
+          y = __builtin_bit_cast(half8, x[s]);
+        // (not a number, where one is)
+        lo[i] = s == 0 ? y : __builtin_elementwise_minimum(lo[i], y);
+        hi[i] = s == 0 ? y : __builtin_elementwise_maximum(hi[i], y);
+      }
+    _Float16* to = p.bounds + ((size_t)blk * p.n_heads + head) * 2 * D + piece * C;
+#pragma unroll
+    for (int i = 0; i < C / 8; ++i) {
+      store_half8(to + 8 * i, lo[i]);
+      store_half8(to + D + 8 * i, hi[i]);
+    }
   }
 }
 
@@ -91,6 +98,10 @@ __device__ __forceinline__ uint64_t score_order(double s) {
   return bits >> 63 ? ~bits : bits | (1ull << 63);
 }
 
+// Workgroups that select have this many wavefronts (with four, the scores of 1809 blocks, eight a thread, took 8.5 us to
+// select from, where 1.6 are for what is read first).
+constexpr int kSelectWaves = 8, kSelectThreads = 64 * kSelectWaves;
+
 template <int CTRL>
 __device__ __forceinline__ double from_lane_f64(double v) {
   const uint64_t b = __builtin_bit_cast(uint64_t, v);
@@ -103,17 +114,19 @@ __device__ __forceinline__ const _Float16* query_of(const SelectParams& p, int r
 }
 
 // The first product's operands in LDS, in the order of the lanes: of 16 rows (token * group + query head of the
-// group, zeros behind the last one) the parts below and above zero, 2 D numbers each, 32 at a time.
-template <int D>
-__device__ __forceinline__ void queries_to_lds(const SelectParams& p, int first_row, int n_tokens, int head, half8* sm_a) {
+// group, zeros behind the last one) the parts below and above zero, 2 D numbers each, 32 at a time.  sm_q: NULL, or
+// the rows themselves.
+template <int D, int kThreadsHere>
+__device__ __forceinline__ void queries_to_lds(const SelectParams& p, int first_row, int n_tokens, int head, half8* sm_a, _Float16* sm_q) {
   constexpr int KK = 2 * D / 32, PPR = D / 8;
   const int rows = n_tokens * p.group, tiles = (rows + 15) >> 4;
-  for (int i = threadIdx.x; i < tiles * 16 * PPR; i += kThreads) {
+  for (int i = threadIdx.x; i < tiles * 16 * PPR; i += kThreadsHere) {
     const int r = i / PPR, c = i % PPR;
     half8 x = {};
     if (r < rows) {
       const int t = r / p.group;
       x = load_half8(query_of(p, first_row + t, head * p.group + r - t * p.group) + c * 8);
+      if (sm_q) store_half8(sm_q + r * D + c * 8, x);
     }
     half8 below, above;
 #pragma unroll
@@ -130,8 +143,8 @@ __device__ __forceinline__ void queries_to_lds(const SelectParams& p, int first_
 
 // Scores of blocks [b0, b1) for some tokens.  A wavefront has 16 blocks at a time, a block a column.  The first ones
 // are requested when this is made: a block's number and its bounds are two latencies, one after the other.
-template <int D>
-struct BlockScores {
+template <int D, int W>
+struct BlockScores {  // W: wavefronts of the workgroup
   static constexpr int KK = 2 * D / 32;
   struct Bounds {
     half8 x[KK];
@@ -143,13 +156,13 @@ struct BlockScores {
   __device__ __forceinline__ BlockScores(const SelectParams& p_, const int32_t* table_, int head_, int b0_, int b1_)
       : p(p_), table(table_), head(head_), b0(b0_), b1(b1_) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    n = max(own_tiles((b1 - b0 + 15) / 16, wave, kWaves), 0);
+    n = max(own_tiles((b1 - b0 + 15) / 16, wave, W), 0);
     id = table[block(0)];
     const int second = table[block(1)];
     request(a);
     id = second;
   }
-  __device__ __forceinline__ int first(int i) const { return b0 + ((int)(threadIdx.x >> 6) + kWaves * i) * 16; }
+  __device__ __forceinline__ int first(int i) const { return b0 + ((int)(threadIdx.x >> 6) + W * i) * 16; }
   __device__ __forceinline__ int block(int i) const { return min(first(i) + (int)(threadIdx.x & 15), b1 - 1); }
   __device__ __forceinline__ void request(Bounds& t) const {
     const _Float16* from = p.bounds + ((size_t)clamp_block(id, p.n_blocks) * p.n_heads + head) * 2 * D + ((threadIdx.x & 63) >> 4) * 8;
@@ -212,7 +225,7 @@ __device__ __forceinline__ void score_exactly(const SelectParams& p, const _Floa
                                               uint64_t* keys) {
   constexpr int PPR = D / 8;
   const int piece = threadIdx.x % PPR;
-  for (int i = threadIdx.x / PPR; i < n; i += kThreads / PPR) {
+  for (int i = threadIdx.x / PPR; i < n; i += kSelectThreads / PPR) {
     const _Float16* from = p.bounds + ((size_t)clamp_block(blocks[i], p.n_blocks) * p.n_heads + head) * 2 * D + piece * 8;
     const half8 lo = load_half8(from), hi = load_half8(from + D);
     uint64_t best = 0;
@@ -232,32 +245,36 @@ __device__ __forceinline__ void score_exactly(const SelectParams& p, const _Floa
   }
 }
 
-constexpr int kMaxKeys = kPlanMaxSeqLen / kPlanBlockSize, kPerThread = kMaxKeys / kThreads;
+constexpr int kMaxKeys = kPlanMaxSeqLen / kPlanBlockSize, kPerThread = kMaxKeys / kSelectThreads;
 
-// For every element i = j * kThreads + thread (j < mine): how many before it have the first flag and how many the second,
-// in the low and high half of before[j]; returns how many there are of each.  counts: kPerThread * kWaves numbers in
+// set bits of the lanes below this one
+__device__ __forceinline__ uint32_t below_lane(uint64_t set) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(set >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)set, 0));
+}
+
+// For every element i = j * kSelectThreads + thread (j < mine): how many before it have the first flag and how many the second,
+// in the low and high half of before[j]; returns how many there are of each.  counts: kPerThread * kSelectWaves numbers in
 // LDS, free when all threads are here.
 template <typename One, typename Two>
 __device__ __forceinline__ uint32_t places_of(int mine, One one, Two two, uint32_t* counts, uint32_t* before) {
-  static_assert(kPerThread * kWaves <= 64 && kMaxKeys < 1 << 16, "a count a lane, two in a word");
+  static_assert(kPerThread * kSelectWaves <= 64 && kMaxKeys < 1 << 16, "a count a lane, two in a word");
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
   for (int j = 0; j < kPerThread; ++j) {
     const uint64_t a = j < mine ? __ballot(one(j)) : 0, b = j < mine ? __ballot(two(j)) : 0;
-    const uint64_t below = (1ull << lane) - 1;
-    before[j] = __popcll(a & below) | __popcll(b & below) << 16;
-    if (j < mine && lane == 0) counts[j * kWaves + wave] = __popcll(a) | __popcll(b) << 16;
+    before[j] = below_lane(a) | below_lane(b) << 16;
+    if (j < mine && lane == 0) counts[j * kSelectWaves + wave] = __popcll(a) | __popcll(b) << 16;
   }
   __syncthreads();
-  const uint32_t own = lane < mine * kWaves ? counts[lane] : 0;
+  const uint32_t own = lane < mine * kSelectWaves ? counts[lane] : 0;
   const uint32_t sum = (uint32_t)wave_scan_add((int)own);
 #pragma unroll
-  for (int j = 0; j < kPerThread; ++j) before[j] += (uint32_t)__builtin_amdgcn_readlane((int)(sum - own), j * kWaves + wave);
+  for (int j = 0; j < kPerThread; ++j) before[j] += (uint32_t)__builtin_amdgcn_readlane((int)(sum - own), j * kSelectWaves + wave);
   return (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
 }
 
-// The k-th largest of n > k > 0 keys, key[j] of thread t being that of element j * kThreads + t (0: none; Key: 32 or
+// The k-th largest of n > k > 0 keys, key[j] of thread t being that of element j * kSelectThreads + t (0: none; Key: 32 or
 // 64 bits, no key is 0): a threshold that exactly k keys reach, or the k-th one itself where more do.  Two bits at a
 // time from the first one in which keys differ, with three counts of all keys a step.  reached: how many keys reach it.
 template <typename Key>
@@ -268,12 +285,12 @@ struct FoundKey {
 template <typename Key>
 __device__ __forceinline__ FoundKey<Key> kth_largest(const Key (&key)[kPerThread], int n, int k) {
   typedef int int4v __attribute__((ext_vector_type(4)));
-  __shared__ int4v sm_count[2][kWaves];
-  __shared__ Key sm_most[kWaves], sm_least[kWaves];
+  __shared__ int4v sm_count[2][kSelectWaves];
+  __shared__ Key sm_most[kSelectWaves], sm_least[kSelectWaves];
   constexpr int kBits = 8 * sizeof(Key);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int mine = (n + kThreads - 1) / kThreads;  // uniform
+  const int mine = (n + kSelectThreads - 1) / kSelectThreads;  // uniform
   Key most = 0, least = ~(Key)0;
 #pragma unroll
   for (int j = 0; j < kPerThread; ++j) {
@@ -297,7 +314,7 @@ __device__ __forceinline__ FoundKey<Key> kth_largest(const Key (&key)[kPerThread
   }
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < kSelectWaves; ++w) {
     most = sm_most[w] > most ? sm_most[w] : most;
     least = sm_least[w] < least ? sm_least[w] : least;
   }
@@ -318,7 +335,7 @@ __device__ __forceinline__ FoundKey<Key> kth_largest(const Key (&key)[kPerThread
     __syncthreads();
     int4v sum = {0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum += sm_count[step & 1][w];
+    for (int w = 0; w < kSelectWaves; ++w) sum += sm_count[step & 1][w];
     const int d = sum[3] >= k ? 3 : sum[2] >= k ? 2 : sum[1] >= k ? 1 : 0;
     f.threshold |= (Key)d << shift;
     if (d > 0) f.reached = d == 3 ? sum[3] : d == 2 ? sum[2] : sum[1];
@@ -333,10 +350,11 @@ struct Between {
 };
 constexpr size_t between_bytes(int n) { return (size_t)((n + 1) / 2 * 2) * (sizeof(int32_t) + sizeof(uint64_t)); }
 
-// What a thread knows of blocks j * kThreads + thread of a table (-infinity, 0 behind the last one).
+// What a thread knows of blocks j * kSelectThreads + thread of a table (-infinity, 0 behind the last one).
 struct Scored {
   float score[kPerThread];
   int32_t id[kPerThread];
+  int32_t last_id;  // of the token's own block, which is not scored
 };
 
 constexpr int kBuckets = 1024;  // of scores, as wide as each other
@@ -349,20 +367,20 @@ constexpr int kBuckets = 1024;  // of scores, as wide as each other
 template <int D, typename Out>
 __device__ __forceinline__ void select_best(const SelectParams& p, const _Float16* sm_q, int head, const Scored& b, int n, int k, float most,
                                             Between between, Out out) {
-  static_assert(kBuckets % kThreads == 0, "whole");
-  constexpr int kOwn = kBuckets / kThreads;
-  __shared__ uint32_t sm_place[kPerThread * kWaves];
+  static_assert(kBuckets % kSelectThreads == 0, "whole");
+  constexpr int kOwn = kBuckets / kSelectThreads;
+  __shared__ uint32_t sm_place[kPerThread * kSelectWaves];
   __shared__ uint32_t sm_bucket[kBuckets];
-  __shared__ float sm_sum[kWaves], sm_top[kWaves], sm_low[kWaves];
-  __shared__ int sm_above[kWaves], sm_found;
+  __shared__ float sm_sum[kSelectWaves], sm_top[kSelectWaves], sm_low[kSelectWaves];
+  __shared__ int sm_above[kSelectWaves], sm_found;
   __shared__ uint64_t sm_kept;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int mine = (n + kThreads - 1) / kThreads;
+  const int mine = (n + kSelectThreads - 1) / kSelectThreads;
   float top = -INFINITY, low = INFINITY;
 #pragma unroll
   for (int j = 0; j < kPerThread; ++j) {
-    if (j * kThreads + (int)threadIdx.x >= n) continue;
+    if (j * kSelectThreads + (int)threadIdx.x >= n) continue;
     top = fmaxf(top, b.score[j]);
     low = fminf(low, b.score[j]);
   }
@@ -371,7 +389,7 @@ __device__ __forceinline__ void select_best(const SelectParams& p, const _Float1
     top = fmaxf(top, __shfl_xor(top, d));
     low = fminf(low, __shfl_xor(low, d));
   }
-  for (int i = 0; i < kOwn; ++i) sm_bucket[i * kThreads + threadIdx.x] = 0;
+  for (int i = 0; i < kOwn; ++i) sm_bucket[i * kSelectThreads + threadIdx.x] = 0;
   if (lane == 0) {
     sm_top[wave] = top;
     sm_low[wave] = low;
@@ -379,7 +397,7 @@ __device__ __forceinline__ void select_best(const SelectParams& p, const _Float1
   __syncthreads();
   // the largest sum of |q|
   float sum = 0.f;
-  for (int h = wave; h < p.group; h += kWaves) {
+  for (int h = wave; h < p.group; h += kSelectWaves) {
     float s = 0.f;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) s += fabsf((float)sm_q[h * D + lane * (D / 64) + c]);
@@ -388,7 +406,7 @@ __device__ __forceinline__ void select_best(const SelectParams& p, const _Float1
   }
   if (lane == 0) sm_sum[wave] = sum;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < kSelectWaves; ++w) {
     top = fmaxf(top, sm_top[w]);
     low = fminf(low, sm_low[w]);
   }
@@ -397,7 +415,7 @@ __device__ __forceinline__ void select_best(const SelectParams& p, const _Float1
   auto bucket_of = [&](float s) { return min((int)fmaxf((top - s) * scale, 0.f), kBuckets - 1); };
 #pragma unroll
   for (int j = 0; j < kPerThread; ++j)
-    if (j * kThreads + (int)threadIdx.x < n) atomicAdd(&sm_bucket[bucket_of(b.score[j])], 1u);
+    if (j * kSelectThreads + (int)threadIdx.x < n) atomicAdd(&sm_bucket[bucket_of(b.score[j])], 1u);
   __syncthreads();
   int own[kOwn], mine_sum = 0;
 #pragma unroll
@@ -410,7 +428,7 @@ __device__ __forceinline__ void select_best(const SelectParams& p, const _Float1
   __syncthreads();
   int above = scan - mine_sum;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < kSelectWaves; ++w) {
     above += w < wave ? sm_above[w] : 0;
     sum = sm_sum[w] > sum || sm_sum[w] != sm_sum[w] ? sm_sum[w] : sum;
   }
@@ -428,7 +446,7 @@ __device__ __forceinline__ void select_best(const SelectParams& p, const _Float1
   const float width = scale > 0.f ? (top - low) * (1.f / kBuckets) : top - low;
   const float sure_from = top - (found - 0.01f) * width + margin, least = top - (found + 1.01f) * width - margin;
   const bool all = !(margin < INFINITY) || !(width < INFINITY);
-  auto within = [&](int j) { return j * kThreads + (int)threadIdx.x < n; };
+  auto within = [&](int j) { return j * kSelectThreads + (int)threadIdx.x < n; };
   auto is_sure = [&](int j) { return within(j) && !all && b.score[j] > sure_from; };
   auto is_between = [&](int j) { return within(j) && (all || (b.score[j] >= least && b.score[j] <= sure_from)); };
   uint32_t before[kPerThread];
@@ -469,10 +487,10 @@ __device__ __forceinline__ void select_best(const SelectParams& p, const _Float1
     return;
   }
   uint64_t exact[kPerThread];
-  const int parts = (n_between + kThreads - 1) / kThreads;
+  const int parts = (n_between + kSelectThreads - 1) / kSelectThreads;
 #pragma unroll
   for (int j = 0; j < kPerThread; ++j) {
-    const int i = j * kThreads + (int)threadIdx.x;
+    const int i = j * kSelectThreads + (int)threadIdx.x;
     exact[j] = i < n_between ? between.keys[i] : 0;
   }
   const FoundKey<uint64_t> f = kth_largest<uint64_t>(exact, n_between, wanted);
@@ -482,7 +500,7 @@ __device__ __forceinline__ void select_best(const SelectParams& p, const _Float1
                                      sm_place, place) & 0xffff;
 #pragma unroll
   for (int j = 0; j < kPerThread; ++j) {
-    const int i = j * kThreads + (int)threadIdx.x;
+    const int i = j * kSelectThreads + (int)threadIdx.x;
     if (i < n_between) between.blocks[i] = exact[j] > f.threshold || (exact[j] == f.threshold && (place[j] >> 16) < (uint32_t)wanted - n_above);
   }
   __syncthreads();
@@ -506,7 +524,7 @@ struct Selection {
     if (selected) selected[place] = block;
   }
   __device__ __forceinline__ void put_all(const SelectParams& p, const int32_t* table, int nb) const {
-    for (int b = threadIdx.x; b < p.n_select; b += kThreads) {
+    for (int b = threadIdx.x; b < p.n_select; b += kSelectThreads) {
       if (b < nb)
         put(b, b, table[b]);
       else if (selected)
@@ -515,25 +533,26 @@ struct Selection {
   }
 };
 template <int D>
-__device__ __forceinline__ void write_selection(const SelectParams& p, const int32_t* table, const _Float16* sm_q, int nb, int head, int64_t at,
+__device__ __forceinline__ void write_selection(const SelectParams& p, const _Float16* sm_q, int nb, int head, int64_t at,
                                                 const Scored& b, float most, Between between) {
   const Selection to(p, at);
   select_best<D>(p, sm_q, head, b, nb - 1, p.n_select - 1, most, between,
-                 [&](int place, int j) { to.put(place, j * kThreads + (int)threadIdx.x, b.id[j]); });
-  if (threadIdx.x == 0) to.put(p.n_select - 1, nb - 1, table[nb - 1]);
+                 [&](int place, int j) { to.put(place, j * kSelectThreads + (int)threadIdx.x, b.id[j]); });
+  if (threadIdx.x == 0) to.put(p.n_select - 1, nb - 1, b.last_id);
 }
 
 // Where the thread's blocks lie; the queries to LDS.
 __device__ __forceinline__ void request_blocks(const int32_t* table, int n, Scored& b) {
 #pragma unroll
   for (int j = 0; j < kPerThread; ++j) {
-    const int i = j * kThreads + (int)threadIdx.x;
+    const int i = j * kSelectThreads + (int)threadIdx.x;
     b.id[j] = i < n ? table[i] : 0;
   }
+  b.last_id = table[n];
 }
 template <int D>
 __device__ __forceinline__ void request_queries(const SelectParams& p, int row, int head, _Float16* sm_q) {
-  for (int i = threadIdx.x; i < p.group * (D / 8); i += kThreads) {
+  for (int i = threadIdx.x; i < p.group * (D / 8); i += kSelectThreads) {
     const int h = i / (D / 8), c = i % (D / 8);
     store_half8(sm_q + h * D + c * 8, load_half8(query_of(p, row, head * p.group + h) + c * 8));
   }
@@ -544,9 +563,9 @@ __device__ __forceinline__ float magnitude(uint32_t bits) { return (float)__buil
 
 // Scores and selection by one workgroup, of the one new token of a request.
 template <int D, typename Reqs>
-__global__ __launch_bounds__(kThreads) void select_blocks_kernel(SelectParams p, Reqs reqs) {
+__global__ __launch_bounds__(kSelectThreads) void select_blocks_kernel(SelectParams p, Reqs reqs) {
   extern __shared__ __align__(16) char sm[];
-  __shared__ uint32_t sm_most[kWaves];
+  __shared__ uint32_t sm_most[kSelectWaves];
   const int token = blockIdx.x / p.n_heads;
   const int head = blockIdx.x - token * p.n_heads;
   const ChunkReq rq = reqs.req[token];
@@ -570,22 +589,21 @@ __global__ __launch_bounds__(kThreads) void select_blocks_kernel(SelectParams p,
   float* room = reinterpret_cast<float*>(rest + rows * 2 * D * 2) + (threadIdx.x >> 6) * rows * 16;
   Scored b;
   request_blocks(table, nb - 1, b);
-  request_queries<D>(p, rq.row_off, head, sm_q);
-  BlockScores<D> blocks(p, table, head, 0, nb - 1);
-  queries_to_lds<D>(p, rq.row_off, 1, head, sm_a);
+  BlockScores<D, kSelectWaves> blocks(p, table, head, 0, nb - 1);
+  queries_to_lds<D, kSelectThreads>(p, rq.row_off, 1, head, sm_a, sm_q);
   uint32_t most = blocks.run(1, sm_a, room, [&](int, int i, float s) { scores[i] = s; });
   most = wave_max(most);
   if ((threadIdx.x & 63) == 0) sm_most[threadIdx.x >> 6] = most;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) most = max(most, sm_most[w]);
+  for (int w = 0; w < kSelectWaves; ++w) most = max(most, sm_most[w]);
 #pragma unroll
   for (int j = 0; j < kPerThread; ++j) {
-    const int i = j * kThreads + (int)threadIdx.x;
+    const int i = j * kSelectThreads + (int)threadIdx.x;
     b.score[j] = i < nb - 1 ? scores[i] : -INFINITY;
   }
   uint64_t* keys = reinterpret_cast<uint64_t*>(rest);
-  write_selection<D>(p, table, sm_q, nb, head, at, b, magnitude(most), Between{reinterpret_cast<int32_t*>(keys + p.lds_keys), keys});
+  write_selection<D>(p, sm_q, nb, head, at, b, magnitude(most), Between{reinterpret_cast<int32_t*>(keys + p.lds_keys), keys});
 }
 
 // Scores alone: workgroup = (part of the blocks, some tokens of a request, head).  The requests: n_new tokens,
@@ -604,8 +622,8 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(SelectParams p, 
   const int rows = (n_tokens * p.group + 15) & ~15;
   half8* sm_a = reinterpret_cast<half8*>(sm);
   float* room = reinterpret_cast<float*>(sm + rows * 2 * D * 2) + (threadIdx.x >> 6) * rows * 16;
-  BlockScores<D> blocks(p, table, head, part * p.part_blocks, min((part + 1) * p.part_blocks, rq.state_off));
-  queries_to_lds<D>(p, rq.row_off + first, n_tokens, head, sm_a);
+  BlockScores<D, kWaves> blocks(p, table, head, part * p.part_blocks, min((part + 1) * p.part_blocks, rq.state_off));
+  queries_to_lds<D, kThreads>(p, rq.row_off + first, n_tokens, head, sm_a, nullptr);
   float* scores = p.scores + ((int64_t)(rq.row_off + first) * p.n_heads + head) * p.score_stride;
   uint32_t most = blocks.run(n_tokens, sm_a, room,
                              [&](int token, int b, float s) { scores[(int64_t)token * p.n_heads * p.score_stride + b] = s; });
@@ -621,7 +639,7 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(SelectParams p, 
 
 // The selection alone: workgroup = (token, head).  The tokens: unit_start the first part's unit, n_new their number.
 template <int D, typename Reqs>
-__global__ __launch_bounds__(kThreads) void select_scored_kernel(SelectParams p, Reqs reqs) {
+__global__ __launch_bounds__(kSelectThreads) void select_scored_kernel(SelectParams p, Reqs reqs) {
   extern __shared__ __align__(16) char sm[];
   const int token = blockIdx.x / p.n_heads;
   const int head = blockIdx.x - token * p.n_heads;
@@ -642,13 +660,13 @@ __global__ __launch_bounds__(kThreads) void select_scored_kernel(SelectParams p,
   // (all of it requested before any of it is waited for)
   Scored b;
 #pragma unroll
-  for (int j = 0; j < kPerThread; ++j) b.score[j] = p.scores[at * p.score_stride + min(j * kThreads + (int)threadIdx.x, nb - 2)];
+  for (int j = 0; j < kPerThread; ++j) b.score[j] = p.scores[at * p.score_stride + min(j * kSelectThreads + (int)threadIdx.x, nb - 2)];
   request_blocks(table, nb - 1, b);
   uint32_t most = 0;
   for (int i = threadIdx.x & 63; i < rq.n_new; i += 64) most = max(most, p.most[(int64_t)(rq.unit_start + i) * p.n_heads + head]);
   request_queries<D>(p, rq.row_off, head, sm_q);
   most = wave_max(most);
-  write_selection<D>(p, table, sm_q, nb, head, at, b, magnitude(most), Between{reinterpret_cast<int32_t*>(keys + p.lds_keys), keys});
+  write_selection<D>(p, sm_q, nb, head, at, b, magnitude(most), Between{reinterpret_cast<int32_t*>(keys + p.lds_keys), keys});
 }
 
 }  // namespace
@@ -673,25 +691,25 @@ hipError_t launch_select_blocks(const SelectParams& p, const ChunkReqs& inline_t
     return hipErrorInvalidValue;
   const unsigned heads = (unsigned)p.n_tokens * p.n_heads;
   const size_t between = between_bytes(p.lds_keys), queries = (size_t)p.group * p.head_dim * sizeof(_Float16);
-  auto operands = [&](int rows) { return (size_t)((rows + 15) & ~15) * (2 * p.head_dim * 2 + kWaves * 16 * sizeof(float)); };
+  auto operands = [&](int rows, int waves) { return (size_t)((rows + 15) & ~15) * (2 * p.head_dim * 2 + waves * 16 * sizeof(float)); };
   auto launch = [&](auto dim) {
     constexpr int D = decltype(dim)::value;
     if (p.part_blocks == 0) {
-      const size_t lds = queries + ((p.lds_keys * sizeof(float) + 15) & ~(size_t)15) + std::max(between, operands(p.group));
+      const size_t lds = queries + ((p.lds_keys * sizeof(float) + 15) & ~(size_t)15) + std::max(between, operands(p.group, kSelectWaves));
       with_reqs_of(p.tokens, inline_tokens, [&](const auto& reqs) {
         using Reqs = std::decay_t<decltype(reqs)>;
-        select_blocks_kernel<D, Reqs><<<heads, kThreads, lds, s>>>(p, reqs);
+        select_blocks_kernel<D, Reqs><<<heads, kSelectThreads, lds, s>>>(p, reqs);
       });
       return;
     }
     if (p.n_units > 0)
       with_reqs_of(p.reqs, inline_reqs, [&](const auto& reqs) {
         using Reqs = std::decay_t<decltype(reqs)>;
-        block_scores_kernel<D, Reqs><<<(unsigned)p.n_units * p.n_heads, kThreads, operands(p.tile_tokens * p.group), s>>>(p, reqs);
+        block_scores_kernel<D, Reqs><<<(unsigned)p.n_units * p.n_heads, kThreads, operands(p.tile_tokens * p.group, kWaves), s>>>(p, reqs);
       });
     with_reqs_of(p.tokens, inline_tokens, [&](const auto& reqs) {
       using Reqs = std::decay_t<decltype(reqs)>;
-      select_scored_kernel<D, Reqs><<<heads, kThreads, queries + between, s>>>(p, reqs);
+      select_scored_kernel<D, Reqs><<<heads, kSelectThreads, queries + between, s>>>(p, reqs);
     });
   };
   if (p.head_dim == 128)
