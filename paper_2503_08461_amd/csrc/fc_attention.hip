@@ -1240,7 +1240,7 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
 //   S^T: a lane reads a group of 32 channels of a key (16 at 64 channels); the queries' channels follow.
 //   O^T: a transposing read has eight keys of a lane's column for two tiles of 16 channels, one group.
 // ---------------------------------------------------------------------------
-constexpr int kFewRows = 16;
+constexpr int kFewRows = kFewRows4;
 constexpr int kFewStages = 2;
 constexpr int few_wave_bytes(int head_dim) { return kFewStages * stage4_bytes(head_dim) + 2 * head_dim; }
 
@@ -1386,6 +1386,9 @@ __global__ __launch_bounds__(256, 4) void attention_few4_kernel(AttnParams p, Re
     keys.exponents = stage(i) + 2 * L::kBlock;
     keys.set_k();
     keys.template set_v<kMasked>(w.key_end - 1 - key0);
+    // (the tile is in registers: two more are on their way while it is worked on)
+    lds_reads_done();
+    request(i + kFewStages);
     floatx4 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -1449,8 +1452,6 @@ __global__ __launch_bounds__(256, 4) void attention_few4_kernel(AttnParams p, Re
         o[2 * dt + h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pb, o[2 * dt + h], 0, 0, 0);
       }
     }
-    lds_reads_done();
-    request(i + kFewStages);
   };
   int i = 0;
   for (; i < full; ++i) step(i, std::false_type());

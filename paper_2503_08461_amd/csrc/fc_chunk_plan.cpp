@@ -103,7 +103,9 @@ int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, in
     const int longest = blocks_for(l.reqs.front().seq_len);
     l.seg_blocks = std::max(longest, 1);
     int64_t total = 0, units = 0;  // blocks that workgroups walk, workgroups, all heads
+    int64_t most_rows = 0;
     for (const ChunkReq& q : l.reqs) {
+      most_rows = std::max(most_rows, (int64_t)q.n_new * group);
       units += tiles(q) * pool.n_heads;
       total += tiles(q) * blocks_for(q.seq_len) * pool.n_heads;
       l.state_rows += q.n_new;
@@ -127,9 +129,19 @@ int plan_attention(const PoolView& pool, int n_cu, int group, bool may_split, in
     const int64_t room = states_left / (l.state_rows * n_q_heads);  // segments of a row
     if (room >= 2) {
       const int64_t wanted = s == 0 ? (slots + units - 1) / units : 1;
-      const int64_t least = four_bits && s == 1 ? std::max(16, (longest + 63) / 64) : kPlanMinSegment;
-      const int64_t seg = std::max<int64_t>({s == 0 ? (longest + wanted - 1) / wanted : total / (four_bits ? 2 * slots : slots), least,
-                                             (longest + room - 1) / room});
+      const bool few = four_bits && s == 1 && launches[0].reqs.empty() && most_rows <= kFewRows4;
+      const int64_t share = few ? total / (2 * slots) : total / slots;
+      const int64_t least = few ? std::max(16, (longest + 63) / 64) : kPlanMinSegment;
+      int64_t seg = std::max<int64_t>({s == 0 ? (longest + wanted - 1) / wanted : share, least, (longest + room - 1) / room});
+      if (few) {
+        // (a few more than fit at once would run after all others)
+        auto segments = [&] {
+          int64_t n = 0;
+          for (const ChunkReq& q : l.reqs) n += decode_segments(blocks_for(q.seq_len), (int)seg);
+          return n * pool.n_heads;
+        };
+        for (int64_t n = segments(); n > 2 * slots && n < 3 * slots && 2 * seg <= longest; n = segments()) seg += seg / 32 + 1;
+      }
       if (2 * seg <= longest) {
         l.seg_blocks = (int)seg;
         l.n_seg = decode_segments(longest, l.seg_blocks);

@@ -36,6 +36,7 @@ int plan_store_units(ChunkPlan* plan);
 static constexpr int kAttnKinds = 2;
 static constexpr int kTallRows = 128;  // rows (new tokens x query heads of a group) of a workgroup
 static constexpr int kFlatRows = 32;
+static constexpr int kFewRows4 = 16;  // of 4 bits: up to here, if no request has more, in a kernel of its own
 static constexpr int kPlanMinSegment = 32;  // blocks
 // Most states of a call's split rows, what the pool's buffer holds if the card has the room (42 MB
 // at 128 channels; else kMaxDecodeSegments, or none).
