@@ -113,33 +113,46 @@ __device__ __forceinline__ const _Float16* query_of(const SelectParams& p, int r
   return p.q.data + (int64_t)row * p.q.token_stride + (int64_t)q_head * p.q.head_stride;
 }
 
-// The first product's operands in LDS, in the order of the lanes: of 16 rows (token * group + query head of the
-// group, zeros behind the last one) the parts below and above zero, 2 D numbers each, 32 at a time.  sm_q: NULL, or
-// the rows themselves.
-template <int D, int kThreadsHere>
-__device__ __forceinline__ void queries_to_lds(const SelectParams& p, int first_row, int n_tokens, int head, half8* sm_a, _Float16* sm_q) {
-  constexpr int KK = 2 * D / 32, PPR = D / 8;
-  const int rows = n_tokens * p.group, tiles = (rows + 15) >> 4;
-  for (int i = threadIdx.x; i < tiles * 16 * PPR; i += kThreadsHere) {
-    const int r = i / PPR, c = i % PPR;
-    half8 x = {};
-    if (r < rows) {
-      const int t = r / p.group;
-      x = load_half8(query_of(p, first_row + t, head * p.group + r - t * p.group) + c * 8);
-      if (sm_q) store_half8(sm_q + r * D + c * 8, x);
-    }
-    half8 below, above;
+// The first product's operands: of up to kRows rows (token * group + query head of the group, zeros behind the last
+// one, in tiles of 16) the parts below and above zero, 2 D numbers each, in LDS in the order of the lanes, 32 at a time.
+// Requested when this is made, before the bounds: loads are answered in order.
+template <int D, int kRows, int kThreadsHere>
+struct ScoredQueries {
+  static constexpr int KK = 2 * D / 32, PPR = D / 8, kEach = (kRows * PPR + kThreadsHere - 1) / kThreadsHere;
+  half8 x[kEach];
+  int rows;
+  __device__ __forceinline__ ScoredQueries(const SelectParams& p, int first_row, int n_tokens, int head) : rows(n_tokens * p.group) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      below[e] = x[e] < (_Float16)0.f ? x[e] : (_Float16)0.f;
-      above[e] = x[e] > (_Float16)0.f ? x[e] : (_Float16)0.f;
+    for (int k = 0; k < kEach; ++k) {
+      const int i = k * kThreadsHere + (int)threadIdx.x, r = i / PPR, c = i % PPR;
+      x[k] = half8{};
+      if (r < rows) {
+        const int t = r / p.group;
+        x[k] = load_half8(query_of(p, first_row + t, head * p.group + r - t * p.group) + c * 8);
+      }
     }
-    half8* to = sm_a + (size_t)(r >> 4) * KK * 64 + (r & 15);
-    to[(c / 4) * 64 + (c % 4) * 16] = below;
-    to[((c + PPR) / 4) * 64 + ((c + PPR) % 4) * 16] = above;
+    requests_first();
   }
-  __syncthreads();
-}
+  // sm_q: NULL, or for the rows themselves
+  __device__ __forceinline__ void put(half8* sm_a, _Float16* sm_q) const {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int i = k * kThreadsHere + (int)threadIdx.x, r = i / PPR, c = i % PPR;
+      if (r >= ((rows + 15) & ~15)) continue;
+      if (sm_q && r < rows) store_half8(sm_q + r * D + c * 8, x[k]);
+      half8 below, above;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        below[e] = x[k][e] < (_Float16)0.f ? x[k][e] : (_Float16)0.f;
+        above[e] = x[k][e] > (_Float16)0.f ? x[k][e] : (_Float16)0.f;
+      }
+      half8* to = sm_a + (size_t)(r >> 4) * KK * 64 + (r & 15);
+      to[(c / 4) * 64 + (c % 4) * 16] = below;
+      to[((c + PPR) / 4) * 64 + ((c + PPR) % 4) * 16] = above;
+    }
+    __syncthreads();
+  }
+};
 
 // Scores of blocks [b0, b1) for some tokens.  A wavefront has 16 blocks at a time, a block a column.  The first ones
 // are requested when this is made: a block's number and its bounds are two latencies, one after the other.
@@ -587,10 +600,11 @@ __global__ __launch_bounds__(kSelectThreads) void select_blocks_kernel(SelectPar
   const int rows = (p.group + 15) & ~15;
   half8* sm_a = reinterpret_cast<half8*>(rest);
   float* room = reinterpret_cast<float*>(rest + rows * 2 * D * 2) + (threadIdx.x >> 6) * rows * 16;
+  const ScoredQueries<D, kScoreRows / 2, kSelectThreads> queries(p, rq.row_off, 1, head);
+  BlockScores<D, kSelectWaves> blocks(p, table, head, 0, nb - 1);
   Scored b;
   request_blocks(table, nb - 1, b);
-  BlockScores<D, kSelectWaves> blocks(p, table, head, 0, nb - 1);
-  queries_to_lds<D, kSelectThreads>(p, rq.row_off, 1, head, sm_a, sm_q);
+  queries.put(sm_a, sm_q);
   uint32_t most = blocks.run(1, sm_a, room, [&](int, int i, float s) { scores[i] = s; });
   most = wave_max(most);
   if ((threadIdx.x & 63) == 0) sm_most[threadIdx.x >> 6] = most;
@@ -622,8 +636,9 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(SelectParams p, 
   const int rows = (n_tokens * p.group + 15) & ~15;
   half8* sm_a = reinterpret_cast<half8*>(sm);
   float* room = reinterpret_cast<float*>(sm + rows * 2 * D * 2) + (threadIdx.x >> 6) * rows * 16;
+  const ScoredQueries<D, kScoreRows, kThreads> queries(p, rq.row_off + first, n_tokens, head);
   BlockScores<D, kWaves> blocks(p, table, head, part * p.part_blocks, min((part + 1) * p.part_blocks, rq.state_off));
-  queries_to_lds<D, kThreads>(p, rq.row_off + first, n_tokens, head, sm_a, nullptr);
+  queries.put(sm_a, nullptr);
   float* scores = p.scores + ((int64_t)(rq.row_off + first) * p.n_heads + head) * p.score_stride;
   uint32_t most = blocks.run(n_tokens, sm_a, room,
                              [&](int token, int b, float s) { scores[(int64_t)token * p.n_heads * p.score_stride + b] = s; });
