@@ -681,18 +681,21 @@ int fc_rotate_store_chunk(fc_pool* pool, int layer, const int32_t* dev_block_tab
  *     table.  The score of a block is the largest over the query heads that
  *     share the head of  sum_c max(q_c * smallest_c, q_c * largest_c),  which no logit of the
  *     block exceeds (scale aside).  It is summed in 64 bits; a score that is not a
- *     number counts as larger than all others.
+ *     number counts as larger than all others (of two products of which one is not a number
+ *     the other one counts).
  * All of them where they are no more than n_select.  Over what it reads the
  * attention is that of fc_chunk_attention, whose arguments these are.
  *   dev_bounds    as fc_block_bounds left it (the token's own block is read whatever its entry)
  *   n_select      1 .. FC_MAX_SEQ_LEN / 16
  *   dev_selected  NULL, or dev, int32 [T][n_heads][n_select] (4-byte aligned): the table entries
  *                 that were read, ascending, -1 behind the last one
- * The order of scores and the selection lie in scratch memory of the pool, which grows on demand.
+ *
+ * Scores and the selection lie in scratch memory of the pool, which grows on demand: at most 4 bytes
+ * for each of n_select and the longest cache's blocks, for every new token and head of K and V.
  *
  * Both are asynchronous on `stream` and not part of the kernel times.  FC_EINVAL as for
  * fc_store_chunk and fc_chunk_attention; n_select outside its range, NULL or misaligned
- * dev_bounds, 2^24 or more blocks (fc_block_bounds) or tokens times heads.
+ * dev_bounds, 2^24 or more blocks (fc_block_bounds), 2^23 or more tokens times heads of K and V.
  */
 int fc_block_bounds(fc_pool* pool, int layer, const int32_t* dev_block_tables,
                     int max_blocks_per_req, const int32_t* host_seq_lens,

@@ -186,7 +186,8 @@ int plan_sparse(const PoolView& pool, int n_cu, int group, int n_select, const C
   *plan = SparsePlan();
   if (n_select < 1 || n_select > kPlanMaxSeqLen / kPlanBlockSize)
     return fail(plan, PLAN_EINVAL, "n_select %d outside 1..%d", n_select, kPlanMaxSeqLen / kPlanBlockSize);
-  if (chunk.n_rows * pool.n_heads > kPlanMaxWorkgroups) return fail(plan, PLAN_EINVAL, "batch too large for one launch");
+  // (workgroups that select have 512 threads)
+  if (chunk.n_rows * pool.n_heads > kPlanMaxWorkgroups / 2) return fail(plan, PLAN_EINVAL, "batch too large for one launch");
   bool single = true;
   // (with one block, the token's own, nothing is scored)
   auto scores = [&](int nb) { return nb > n_select && n_select > 1; };
@@ -203,9 +204,9 @@ int plan_sparse(const PoolView& pool, int n_cu, int group, int n_select, const C
   }
   plan->attention.n_rows = chunk.n_rows;
   // One launch for scores and selection where its workgroups fill the card or have little to read (384 heads of
-  // 80-440 blocks: 64.7 us a step, with two 67.9); else the scores are made by as many as fill it, and for the
-  // tokens of a request together.  (Up to half of the
-  // rows: what else is kept of the queries and blocks would not fit the LDS beside more.)
+  // 80-440 blocks: 63.1 us a step, with two 66.2); else the scores are made by as many as fill it, and for the
+  // tokens of a request together.  (Up to half of the rows: what else is kept of the queries and blocks would not
+  // fit the LDS beside more.)
   const int cu = std::max(n_cu, 1);
   if (single && group <= kScoreRows / 2 && (chunk.n_rows * pool.n_heads >= cu || plan->longest <= 64)) return PLAN_OK;
   plan->tile_tokens = std::max(1, kScoreRows / group);

@@ -1,6 +1,7 @@
 // The entry points on rotated rows, bounds of blocks and selected blocks (csrc/fc_cache_api.hip) and a 4-bit
 // pool's calls on the CPU: the HIP runtime and the launchers of api_host_driver.cpp, and these.  Built and
-// checked by test_cache_api.py; every line says what was called, its code and what was launched.
+// checked by test_cache_api.py; every line says what was called, its code and what was launched.  With an argument:
+// calls at the limits of a launch.
 #define main api_host_main
 #include "api_host_driver.cpp"
 #undef main
@@ -36,7 +37,44 @@ hipError_t launch_select_blocks(const SelectParams& p, const ChunkReqs&, const C
 }
 }  // namespace fc
 
-int main() {
+// Calls just within and just beyond what one launch takes: fewer than 2^32 threads.
+static int limits() {
+  int32_t* table = somewhere<int32_t>();
+  const fc_rows same = {somewhere<void>(), 0, 0};
+  const fc_rotation turn = {somewhere<float>(), 32768, 128, 0};
+  for (int beyond : {0, 1}) {
+    const std::string s = beyond ? "_beyond" : "_within";
+    auto pool_of = [&](int heads, int dtype) {
+      fc_pool* p = nullptr;
+      fc_pool_create(&p, somewhere<void>(), ~(size_t)0, 64, 16, 1, heads, 128, dtype);
+      g_launched.clear();
+      return p;
+    };
+    for (int dtype : {FC_DTYPE_F16, FC_DTYPE_E2M1}) {
+      // workgroups of 256 threads, one a new token: 512 * 32768 = 2^24
+      fc_pool* p = pool_of(1, dtype);
+      std::vector<int32_t> lens(511 + beyond, 32768);
+      report(("rotate" + s).c_str(), fc_rotate_store_chunk(p, 0, table, 2048, lens.data(), lens.data(), nullptr, &turn, nullptr, 0, nullptr, &same,
+                                                           &same, (int)lens.size(), nullptr));
+      // ... one a block: 8192 * 2048
+      lens.assign(8191 + beyond, 32768);
+      report(("bounds" + s).c_str(), fc_block_bounds(p, 0, table, 2048, lens.data(), lens.data(), somewhere<void>(), (int)lens.size(), nullptr));
+      fc_pool_destroy(p);
+      // of 512 threads, one a new token and head: 1024 * 8192 = 2^23
+      p = pool_of(8192, dtype);
+      const int32_t news[1] = {1023 + beyond};
+      const fc_rows out = {somewhere<void>(), 8192 * 128, 128};
+      for (int n_select : {1, 2048})
+        report(("sparse" + s).c_str(), fc_sparse_attention(p, 0, table, 2048, news, news, somewhere<void>(), n_select, &same, 8192, &out, nullptr, 1,
+                                                           0.f, nullptr));
+      fc_pool_destroy(p);
+    }
+  }
+  return 0;
+}
+
+int main(int argc, char**) {
+  if (argc > 1) return limits();
   int32_t* table = somewhere<int32_t>();
   float* out32 = somewhere<float>();
   auto pool_of = [&](int dtype, int heads, int dim, size_t bytes) {

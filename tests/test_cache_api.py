@@ -14,7 +14,7 @@ pytestmark = pytest.mark.skipif(shutil.which(HIPCC) is None, reason="no hipcc")
 
 
 @pytest.fixture(scope="module")
-def calls(tmp_path_factory):
+def driver(tmp_path_factory):
     tmp = tmp_path_factory.mktemp("cache_api")
     exe, obj = str(tmp / "cache_api"), str(tmp / "api.o")
     csrc = os.path.join(ROOT, "paper_2503_08461_amd", "csrc")
@@ -22,9 +22,17 @@ def calls(tmp_path_factory):
                     os.path.join(ROOT, "tests", "cache_api_driver.cpp"), "-o", obj], check=True)
     subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", obj, os.path.join(csrc, "fc_plan.cpp"),
                     os.path.join(csrc, "fc_chunk_plan.cpp"), "-o", exe], check=True)
-    r = subprocess.run([exe], capture_output=True, text=True, timeout=60)
-    assert r.returncode == 0, (r.returncode, r.stdout, r.stderr)
-    return [ln.split() for ln in r.stdout.splitlines()]
+
+    def run(*args):
+        r = subprocess.run([exe, *args], capture_output=True, text=True, timeout=60)
+        assert r.returncode == 0, (r.returncode, r.stdout, r.stderr)
+        return [ln.split() for ln in r.stdout.splitlines()]
+    return run
+
+
+@pytest.fixture(scope="module")
+def calls(driver):
+    return driver()
 
 
 def test_what_is_refused(calls):
@@ -68,3 +76,10 @@ def test_what_is_launched(calls):
 def test_scratch_of_captured_calls(calls):
     flags = {c[0]: c[1] for c in calls if c[0] in ("kept", "retired")}
     assert flags == {"kept": "1", "retired": "1"}
+
+
+def test_calls_within_and_beyond_one_launch(driver):
+    lines = driver("limits")
+    assert len(lines) == 2 * 2 * 4
+    for name, code, *launched in lines:
+        assert code == ("-1" if name.endswith("_beyond") else "0") and bool(launched) == name.endswith("_within"), name
