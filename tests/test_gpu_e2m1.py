@@ -275,3 +275,34 @@ def test_far_blocks():
         assert (near[0] - out.float()).abs().max() < 2e-2
     finally:
         fc.fc_pool_destroy(pool)
+
+
+def test_ownership_checks_of_a_4_bit_pool():
+    """Blocks handed out, written, appended to and released with the checks on; a block released twice is refused."""
+    import torch
+    from paper_2503_08461_amd import fastcache as fc
+    heads, dim, n_blocks = 2, 64, 12
+    dev = torch.device("cuda:0")
+    kv = torch.zeros((1, n_blocks, 17 * heads * dim), dtype=torch.uint8, device=dev)
+    pool = fc.fc_pool_create(kv, n_blocks, 1, heads, dim, dtype=fc.FC_DTYPE_E2M1)
+    try:
+        fc.fc_set_debug_checks(pool, True)
+        table = torch.full((2, 4), -1, dtype=torch.int32, device=dev)
+        news = np.array([32, 20], np.int32)
+        lens = fc.fc_extend_batch(pool, table, np.zeros(2, np.int32), news)
+        lens = news if lens is None else lens
+        x = torch.randn((52, heads, dim), generator=torch.Generator(dev).manual_seed(2), device=dev).half()
+        fc.fc_store_chunk(pool, 0, table, lens, news, x, x)
+        assert fc.fc_pool_num_free(pool) == n_blocks - 4
+        lens = lens.copy()
+        fc.fc_append_batch(pool, table, lens, x[:4].reshape(2, 1, 2, heads, dim).contiguous())
+        assert lens.tolist() == [33, 21] and fc.fc_pool_num_free(pool) == n_blocks - 5
+        held = table[table >= 0].contiguous()
+        fc.fc_pool_free(pool, held[:2].contiguous())
+        with pytest.raises(fc.FastCacheError):
+            fc.fc_pool_free(pool, held[1:3].contiguous())
+        fc.fc_pool_free(pool, held[2:].contiguous())
+        assert fc.fc_pool_num_free(pool) == n_blocks
+        fc.fc_pool_export_state(pool)
+    finally:
+        fc.fc_pool_destroy(pool)

@@ -86,7 +86,8 @@ def _step(c, layer, n_select, bounds=None, want_selected=None, scale=0.0, **kw):
 @pytest.mark.parametrize("lens,news,heads,group,dim,n_select", [
     ([1], [1], 1, 1, 64, 1), ([1], [1], 1, 1, 128, 9), ([300, 16, 17, 33, 0], [1, 1, 1, 3, 0], 2, 4, 128, 3),
     ([300, 97], [5, 2], 3, 1, 64, 1), ([500, 700], [1, 18], 2, 5, 64, 7), ([400], [1], 1, 40, 128, 6),
-    ([260, 5, 64], [1, 1, 1], 40, 1, 64, 16)], ids=str)
+    ([260, 5, 64], [1, 1, 1], 40, 1, 64, 16),
+    ([290, 40], [4, 3], 2, 2, 64, 1), ([1200, 90, 333], [1, 1, 2], 1, 64, 64, 5)], ids=str)
 def test_selection_and_attention(fmt, lens, news, heads, group, dim, n_select):
     c = Cache(lens, news, heads, group, dim, fmt=fmt, seed=n_select, layers=2 if fmt == "f16" else 1)
     try:
