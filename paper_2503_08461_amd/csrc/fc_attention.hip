@@ -968,7 +968,9 @@ __device__ __forceinline__ void attend_tall(const AttnParams& p, const Reqs& req
 // and the merge (135 us, 124 at the card's 6.4 TB/s for reads); 32 heads of their own, 6.4 (491 us).
 // 8-bit: 32 heads 6.2 TB/s (259 us), 8 heads of four 4.8 with the merge (84 us of attention and merge,
 // 62 at 6.4), the conversion to fp16 beside the loads (16 vector instructions a product, fp16 rows
-// 6.6); 5 drafted tokens of 32 caches of 256-1408: 19 us and 6 for the merge, latency.
+// 6.6); 5 drafted tokens of 32 caches of 256-1408: 19 us and 6 for the merge, latency.  4-bit, 17 rows and more:
+// the same drafts, 8 heads of four, 30.5 us with the store and the merge; a chunk of 2048 behind 30 000 is bound by
+// the matrix cores' power as with the other formats (1.05 ms).
 // ---------------------------------------------------------------------------
 
 // Bytes of one row of K or V in the LDS of such a wavefront.
@@ -1236,7 +1238,11 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
 // Up to 16 rows of a head over 4 bits (single tokens of grouped heads): as the few rows above, on
 // v_mfma_f32_16x16x32_f16, a lane a row again, four lanes to each.  With the keys in so few bytes the
 // instructions are what a wavefront waits for: of 32 rows' softmax and products most are of rows that
-// there are not, and 222 registers leave a SIMD two wavefronts.  Here it has four.
+// there are not, and 222 registers leave a SIMD two wavefronts.  Here it has four.  Single tokens of 48 caches of
+// 1280-7040, 8 heads of four: the attention 57.6 -> 44 us, 220 MB, 5.0 TB/s with the launch and its ends; between
+// them 6.7 (first loads some 5 us, and workgroups that end unevenly: heads are cut into segments of half a share,
+// thirds and whole ones take 56-57 for 54 of the whole step).  Rows of 16 keys as f8f6f4 operands, queries in three
+// e4m3 parts, saved the conversions and gained nothing (45 us).
 //   S^T: a lane reads a group of 32 channels of a key (16 at 64 channels); the queries' channels follow.
 //   O^T: a transposing read has eight keys of a lane's column for two tiles of 16 channels, one group.
 // ---------------------------------------------------------------------------

@@ -89,7 +89,8 @@ hipError_t launch_store_chunk(const StoreParams& p, const ChunkReqs& inline_reqs
 // quantise: workgroup = block of a request in one layer: 32 * n_heads rows, read once, and as many
 // rows of half the bytes written, in whole lines but for the exponents (32 * n_heads bytes, a few of
 // a line at a time, which the L2 joins).  Memory bounds it: 64 caches of 256-1408 tokens, 32 heads
-// of 128 channels, 4 layers, 1060 us = 4.85 TB/s read and written, what a large copy reaches here.
+// of 128 channels, 4 layers, 1060 us = 4.85 TB/s read and written, what a large copy reaches here;
+// into 4 bits 882 us, 4.9 TB/s.
 // ---------------------------------------------------------------------------
 template <int D, int kFormat, typename Reqs>
 __global__ __launch_bounds__(256) void quantise_kernel(QuantiseParams p, Reqs reqs) {

