@@ -27,6 +27,7 @@
 
 #include "fc_chunk_plan.h"
 #include "fc_e2m1.h"
+#include "fc_select_blocks.h"
 
 namespace fc {
 
@@ -985,15 +986,15 @@ constexpr int wave4_bytes(int head_dim) { return kStages4 * stage4_bytes(head_di
 // LDS reads before this point have been answered: what they read may be overwritten by loads.
 __device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-template <int D, int SRC, bool kSplit, typename Reqs>
-__device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& reqs, half8* sm, int unit, int head) {
+// id_of(b): number of the request's block b in the pool.
+template <int D, int SRC, bool kSplit, typename IdOf>
+__device__ __forceinline__ void attend_flat(const AttnParams& p, const Place& w, half8* sm, int head, IdOf id_of) {
   constexpr int kKeys = 32;
   // (codes: two tiles a wavefront fit where one of fp16 rows does; one alone keeps 6 KB on the way
   // on average, and 2048 wavefronts draw 4.2 TB/s with it)
   constexpr int kStages = SRC == ATTN_E4M3 ? 2 : 1;
   constexpr int kTile = kKeys * kFlatRowBytes<D, SRC> / 16;  // sm: [wavefront][stage][K, V][kTile], exponents
   const AttnLaunchView& l = p.launch[ATTN_FLAT];
-  const Place w = place_of<kFlatRows, kSplit>(p, reqs, l, unit);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int first_key = w.rq.seq_len - w.rq.n_new;
@@ -1012,14 +1013,13 @@ __device__ __forceinline__ void attend_flat(const AttnParams& p, const Reqs& req
   const GroupRows from(p.q, w.rq, p, head), to(p.out, w.rq, p, head);
   rows.request_queries([&](int r) { return from.at(lane_row(p, row0 + r, w.n_rows)); });
 
-  const int32_t* table = SRC == ATTN_ROWS ? nullptr : table_of(p, w.rq, head);
   half8* sm_k = sm + wave * 2 * kStages * kTile;
   int ids[2] = {0, 0};
   auto block_of = [&](int i, int j) { return (w.key_begin >> 4) + 2 * (wave + 4 * i) + j; };
   auto look_up = [&](int i) {
     if constexpr (SRC != ATTN_ROWS) {
-      ids[0] = block_id(p, table, block_of(i, 0), w.nb);
-      ids[1] = block_id(p, table, block_of(i, 1), w.nb);
+      ids[0] = id_of(block_of(i, 0));
+      ids[1] = id_of(block_of(i, 1));
     }
   };
   auto key_of = [&](int i) { return w.key_begin + (wave + 4 * i) * kKeys; };
@@ -1317,15 +1317,11 @@ struct Keys16 {
   }
 };
 
-template <int D, bool kSplit, typename Reqs>
-__global__ __launch_bounds__(256, 4) void attention_few4_kernel(AttnParams p, Reqs reqs) {
-  extern __shared__ __align__(16) half8 sm[];
+template <int D, bool kSplit, typename IdOf>
+__device__ __forceinline__ void attend_few4(const AttnParams& p, const Place& w, half8* sm, int head, IdOf id_of) {
   constexpr int kKeys = 32, KS = D / 32, CT = D / 16;
   typedef Loader4<D, true> L;
-  const int unit = blockIdx.x / p.n_heads;
-  const int head = blockIdx.x - unit * p.n_heads;
   const AttnLaunchView& l = p.launch[ATTN_FLAT];
-  const Place w = place_of<kFlatRows, kSplit>(p, reqs, l, unit);  // (no more rows than a tile: one a request)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, quarter = lane >> 4;
   const int first_key = w.rq.seq_len - w.rq.n_new;
@@ -1349,15 +1345,14 @@ __global__ __launch_bounds__(256, 4) void attention_few4_kernel(AttnParams p, Re
   for (int c = 0; c < CT; ++c) o[c] = floatx4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, z = 0.f;
 
-  const int32_t* table = table_of(p, w.rq, head);
   const L loader(p.n_heads, head);
   uint8_t* own = reinterpret_cast<uint8_t*>(sm) + wave * few_wave_bytes(D);
   auto stage = [&](int i) { return own + (i % kFewStages) * stage4_bytes(D); };
   int ids[2] = {0, 0};
   auto look_up = [&](int i) {
     const int b = (w.key_begin >> 4) + 2 * (wave + 4 * i);
-    ids[0] = block_id(p, table, b, w.nb);
-    ids[1] = block_id(p, table, b + 1, w.nb);
+    ids[0] = id_of(b);
+    ids[1] = id_of(b + 1);
   };
   // (tiles behind the last one are requested as nothing: every wait counts the same loads)
   auto request = [&](int i) {
@@ -1514,6 +1509,16 @@ __global__ __launch_bounds__(256, 4) void attention_few4_kernel(AttnParams p, Re
   }
 }
 
+template <int D, bool kSplit, typename Reqs>
+__global__ __launch_bounds__(256, 4) void attention_few4_kernel(AttnParams p, Reqs reqs) {
+  extern __shared__ __align__(16) half8 sm[];
+  const int unit = blockIdx.x / p.n_heads;
+  const int head = blockIdx.x - unit * p.n_heads;
+  const Place w = place_of<kFlatRows, kSplit>(p, reqs, p.launch[ATTN_FLAT], unit);  // (no more rows than a tile: one a request)
+  const int32_t* table = table_of(p, w.rq, head);
+  attend_few4<D, kSplit>(p, w, sm, head, [&](int b) { return block_id(p, table, b, w.nb); });
+}
+
 // The units with many rows come first: they are the heavy ones.
 template <int D, int SRC, bool kSplit, typename Reqs>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, Reqs reqs) {
@@ -1522,8 +1527,40 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, Reqs re
   const int head = blockIdx.x - unit * p.n_heads;
   if (unit < p.launch[ATTN_TALL].n_units)
     attend_tall<D, SRC, kSplit>(p, reqs, sm, unit, head);
+  else {
+    const Place w = place_of<kFlatRows, kSplit>(p, reqs, p.launch[ATTN_FLAT], unit - p.launch[ATTN_TALL].n_units);
+    const int32_t* table = SRC == ATTN_ROWS ? nullptr : table_of(p, w.rq, head);
+    attend_flat<D, SRC, kSplit>(p, w, sm, head, [&](int b) { return block_id(p, table, b, w.nb); });
+  }
+}
+
+// A token's head over the blocks that it selects: scores, selection and attention of up to 32 rows by one workgroup.
+// The tokens' selections end unevenly, chains of latencies all of them; here a workgroup's streams while another one's
+// on its CU selects, and the blocks' numbers stay in LDS.  Single tokens of 48 caches of 1280-7040, 8 heads of four,
+// n_select 64, with the bounds before (us, apart / so): fp16 63.5 / 56.6, 8 bits 49 / 42.7, 4 bits 45.5 / 36.8; 256
+// blocks of 32 caches 97 / 84; in 4 bits 16 caches of 1000-4000, 32 heads, 43 / 34.
+constexpr int kSelectedWaves = 4;
+template <int D, int SRC, bool kFew4, typename Reqs>
+__global__ __launch_bounds__(64 * kSelectedWaves, kFew4 ? 4 : 2) void attention_selected_kernel(SelectParams sp, AttnParams p, Reqs tokens, int ids_at) {
+  extern __shared__ __align__(16) half8 sm[];
+  const int token = blockIdx.x / p.n_heads;
+  const int head = blockIdx.x - token * p.n_heads;
+  const ChunkReq rq = tokens.req[token];
+  int32_t* ids = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(sm) + ids_at);
+  select_for_token<D, kSelectedWaves>(sp, rq, head, Selection(sp, ids, (int64_t)token * p.n_heads + head), reinterpret_cast<char*>(sm));
+  __syncthreads();
+  Place w;
+  w.rq = {token, selected_keys(rq.seq_len, sp.n_select), 1, rq.row_off, 0, 0};
+  w.n_rows = p.group;
+  w.tile = w.seg = w.key_begin = 0;
+  w.n_seg = 1;
+  w.nb = (w.rq.seq_len + 15) >> 4;
+  w.key_end = w.rq.seq_len;
+  auto id_of = [&](int b) { return clamp_block(__builtin_amdgcn_readfirstlane(ids[min(b, w.nb - 1)]), p.n_blocks); };
+  if constexpr (kFew4)
+    attend_few4<D, false>(p, w, sm, head, id_of);
   else
-    attend_flat<D, SRC, kSplit>(p, reqs, sm, unit - p.launch[ATTN_TALL].n_units, head);
+    attend_flat<D, SRC, false>(p, w, sm, head, id_of);
 }
 
 // Rows whose keys were split: the result from the segments' states.  Workgroup = (token of
@@ -1620,11 +1657,19 @@ void launch_shape(const AttnParams& p, const Reqs& reqs, hipStream_t s) {
     launch_source<D, ATTN_E2M1>(p, reqs, s);
 }
 
+template <int D, int SRC, bool kFew4, typename Reqs>
+void launch_selected(const SelectParams& sp, const AttnParams& p, const Reqs& tokens, hipStream_t s) {
+  const size_t at = std::max<size_t>(kFew4 ? 4 * few_wave_bytes(D) : lds_bytes(D, SRC), (select_bytes(sp, kSelectedWaves) + 15) & ~(size_t)15);
+  attention_selected_kernel<D, SRC, kFew4, Reqs>
+      <<<(unsigned)sp.n_tokens * sp.n_heads, 64 * kSelectedWaves, at + sp.n_select * sizeof(int32_t), s>>>(sp, p, tokens, (int)at);
+}
+
 template <typename Reqs>
 hipError_t allow_lds_with() {  // (with the static words more than 64 KB)
   hipError_t e = hipSuccess;
   auto allow = [&](const void* kernel) {
-    if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(128, ATTN_E4M3));
+    if (e == hipSuccess)
+      e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes(128, ATTN_E4M3) + kMaxKeys * (int)sizeof(int32_t));
   };
   allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_ROWS, false, Reqs>));
   allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_F16, false, Reqs>));
@@ -1633,6 +1678,9 @@ hipError_t allow_lds_with() {  // (with the static words more than 64 KB)
   allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_E4M3, true, Reqs>));
   allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_E2M1, false, Reqs>));
   allow(reinterpret_cast<const void*>(&attention_kernel<128, ATTN_E2M1, true, Reqs>));
+  allow(reinterpret_cast<const void*>(&attention_selected_kernel<128, ATTN_F16, false, Reqs>));
+  allow(reinterpret_cast<const void*>(&attention_selected_kernel<128, ATTN_E4M3, false, Reqs>));
+  allow(reinterpret_cast<const void*>(&attention_selected_kernel<128, ATTN_E2M1, false, Reqs>));
   return e;
 }
 
@@ -1641,6 +1689,35 @@ hipError_t allow_lds_with() {  // (with the static words more than 64 KB)
 hipError_t attention_one_time_setup() {
   const hipError_t e = allow_lds_with<ChunkReqs>();
   return e == hipSuccess ? allow_lds_with<ChunkReqList>() : e;
+}
+
+hipError_t launch_selected_attention(const SelectParams& sp, const AttnParams& p, const ChunkReqs& inline_tokens, hipStream_t s) {
+  if (sp.n_tokens == 0) return hipSuccess;
+  if ((sp.head_dim != 64 && sp.head_dim != 128) || sp.part_blocks || sp.group > kFlatRows || sp.lds_keys < 1 || sp.lds_keys > kMaxKeys ||
+      sp.n_select < 1 || sp.n_select > kMaxKeys || p.source == ATTN_ROWS)
+    return hipErrorInvalidValue;
+  auto with = [&](auto dim, const auto& tokens) {
+    constexpr int D = decltype(dim)::value;
+    if (p.source == ATTN_F16)
+      launch_selected<D, ATTN_F16, false>(sp, p, tokens, s);
+    else if (p.source == ATTN_E4M3)
+      launch_selected<D, ATTN_E4M3, false>(sp, p, tokens, s);
+    else if (sp.group <= kFewRows)
+      launch_selected<D, ATTN_E2M1, true>(sp, p, tokens, s);
+    else
+      launch_selected<D, ATTN_E2M1, false>(sp, p, tokens, s);
+  };
+  auto with_tokens = [&](const auto& tokens) {
+    if (sp.head_dim == 128)
+      with(std::integral_constant<int, 128>(), tokens);
+    else
+      with(std::integral_constant<int, 64>(), tokens);
+  };
+  if (sp.tokens)
+    with_tokens(ChunkReqList{sp.tokens});
+  else
+    with_tokens(inline_tokens);
+  return hipGetLastError();
 }
 
 hipError_t launch_attention(const AttnParams& p, const ChunkReqs& inline_reqs, hipStream_t s) {

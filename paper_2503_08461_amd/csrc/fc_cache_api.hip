@@ -26,6 +26,66 @@ int check_aligned(const void* at, size_t to, const char* name) {
 
 size_t bounds_elems(const fc_pool* p) { return (size_t)p->n_blocks * p->n_heads * 2 * p->head_dim; }  // of a layer
 
+// What a selection and an attention of its blocks have in common.
+void set_selection(const fc_pool* p, int layer, const int32_t* dev_block_tables, int max_blocks, const void* dev_bounds, int n_select,
+                   const fc_rows* q, int n_q_heads, int32_t* dev_selected, const SparsePlan& plan, SelectParams* sp) {
+  sp->bounds = static_cast<const _Float16*>(dev_bounds) + (size_t)layer * bounds_elems(p);
+  sp->n_blocks = p->n_blocks;
+  sp->n_heads = p->n_heads;
+  sp->group = n_q_heads / p->n_heads;
+  sp->head_dim = p->head_dim;
+  sp->block_tables = dev_block_tables;
+  sp->max_blocks = max_blocks;
+  sp->n_tokens = (int)plan.tokens.size();
+  sp->q = view(q);
+  sp->n_select = n_select;
+  sp->selected = dev_selected;
+  sp->lds_keys = plan.longest;
+}
+
+// Scores, selection and attention, a launch each.
+int select_then_attend(fc_pool* p, SparsePlan* plan, int n_q_heads, SelectParams* sp, AttnParams* ap, hipStream_t stream) {
+  AttnLaunch launches[ATTN_KINDS];
+  if (plan_attention(geometry(p), p->n_cu, sp->group, true, p->max_states, &plan->attention, launches, p->dtype == FC_DTYPE_E2M1) != PLAN_OK)
+    return fail(plan->attention.code, "%s", plan->attention.message);
+  // (what may grow grows before the descriptors are on their way)
+  int rc;
+  const size_t heads = plan->tokens.size() * p->n_heads;
+  const size_t score_bytes = heads * plan->longest * sizeof(float), most_bytes = (size_t)plan->n_units * p->n_heads * sizeof(uint32_t);
+  if ((rc = scratch_for(p, &p->sparse, score_bytes + most_bytes + heads * sp->n_select * sizeof(int32_t), stream))) return rc;
+  std::vector<ChunkReq> reqs(plan->tokens);
+  const std::vector<ChunkReq> attended = attention_reqs(launches);
+  ChunkReqs token_reqs, scored_reqs, attention_inline;
+  if (reqs.size() <= ChunkReqs::kInline) {
+    std::copy(reqs.begin(), reqs.end(), token_reqs.req);
+    std::copy(plan->scored.begin(), plan->scored.end(), scored_reqs.req);
+    std::copy(attended.begin(), attended.end(), attention_inline.req);
+  } else {
+    reqs.insert(reqs.end(), attended.begin(), attended.end());
+    reqs.insert(reqs.end(), plan->scored.begin(), plan->scored.end());
+    const void* at = nullptr;
+    if ((rc = meta_to_device(p, reqs.data(), reqs.size() * sizeof(ChunkReq), &at, stream))) return rc;
+    sp->tokens = static_cast<const ChunkReq*>(at);
+    ap->reqs = sp->tokens + plan->tokens.size();
+    sp->reqs = ap->reqs + attended.size();
+  }
+  sp->scores = reinterpret_cast<float*>(p->sparse.data);
+  sp->most = reinterpret_cast<uint32_t*>(p->sparse.data + score_bytes);
+  sp->ids = reinterpret_cast<int32_t*>(p->sparse.data + score_bytes + most_bytes);
+  sp->part_blocks = plan->part_blocks;
+  sp->tile_tokens = plan->tile_tokens;
+  sp->n_req = (int)plan->scored.size();
+  sp->n_units = (int)plan->n_units;
+  sp->score_stride = plan->longest;
+  FC_HIP(launch_select_blocks(*sp, token_reqs, scored_reqs, stream));
+  ap->block_tables = sp->ids;
+  ap->max_blocks = sp->n_select;
+  ap->table_heads = p->n_heads;
+  set_launches(p, launches, n_q_heads, ap);
+  FC_HIP(launch_attention(*ap, attention_inline, stream));
+  return FC_OK;
+}
+
 int sparse_attention(fc_pool* p, int layer, const int32_t* dev_block_tables, int max_blocks, const ChunkPlan& chunk,
                      const void* dev_bounds, int n_select, const fc_rows* q, int n_q_heads, const fc_rows* out,
                      int32_t* dev_selected, float scale, hipStream_t stream) {
@@ -37,67 +97,16 @@ int sparse_attention(fc_pool* p, int layer, const int32_t* dev_block_tables, int
   if ((rc = check_rows(q, "q", chunk.n_rows, n_q_heads, p->head_dim, false)) ||
       (rc = check_rows(out, "out", chunk.n_rows, n_q_heads, p->head_dim, true)))
     return rc;
-  AttnLaunch launches[ATTN_KINDS];
-  if (plan_attention(geometry(p), p->n_cu, n_q_heads / p->n_heads, true, p->max_states, &plan.attention, launches,
-                     p->dtype == FC_DTYPE_E2M1) != PLAN_OK)
-    return fail(plan.attention.code, "%s", plan.attention.message);
-
-  // (what may grow grows before the descriptors are on their way)
-  const size_t heads = (size_t)chunk.n_rows * p->n_heads;
-  const size_t score_bytes = plan.part_blocks ? heads * plan.longest * sizeof(float) : 0;
-  const size_t most_bytes = (size_t)plan.n_units * p->n_heads * sizeof(uint32_t);
-  if ((rc = scratch_for(p, &p->sparse, score_bytes + most_bytes + heads * n_select * sizeof(int32_t), stream))) return rc;
-  std::vector<ChunkReq> reqs(plan.tokens);
-  const std::vector<ChunkReq> attended = attention_reqs(launches);
-  ChunkReqs token_reqs, scored_reqs, attention_inline;
-  const ChunkReq* on_device = nullptr;
-  if (reqs.size() <= ChunkReqs::kInline) {
-    std::copy(reqs.begin(), reqs.end(), token_reqs.req);
-    std::copy(plan.scored.begin(), plan.scored.end(), scored_reqs.req);
-    std::copy(attended.begin(), attended.end(), attention_inline.req);
-  } else {
-    reqs.insert(reqs.end(), attended.begin(), attended.end());
-    reqs.insert(reqs.end(), plan.scored.begin(), plan.scored.end());
-    const void* at = nullptr;
-    if ((rc = meta_to_device(p, reqs.data(), reqs.size() * sizeof(ChunkReq), &at, stream))) return rc;
-    on_device = static_cast<const ChunkReq*>(at);
-  }
-
   SelectParams sp = {};
-  sp.bounds = static_cast<const _Float16*>(dev_bounds) + (size_t)layer * bounds_elems(p);
-  sp.n_blocks = p->n_blocks;
-  sp.n_heads = p->n_heads;
-  sp.group = n_q_heads / p->n_heads;
-  sp.head_dim = p->head_dim;
-  sp.block_tables = dev_block_tables;
-  sp.max_blocks = max_blocks;
-  sp.tokens = on_device;
-  sp.n_tokens = (int)chunk.n_rows;
-  sp.q = view(q);
-  sp.n_select = n_select;
-  sp.scores = reinterpret_cast<float*>(p->sparse.data);
-  sp.most = reinterpret_cast<uint32_t*>(p->sparse.data + score_bytes);
-  sp.ids = reinterpret_cast<int32_t*>(p->sparse.data + score_bytes + most_bytes);
-  sp.selected = dev_selected;
-  sp.lds_keys = plan.longest;
-  sp.part_blocks = plan.part_blocks;
-  sp.tile_tokens = plan.tile_tokens;
-  sp.reqs = on_device ? on_device + plan.tokens.size() + attended.size() : nullptr;
-  sp.n_req = (int)plan.scored.size();
-  sp.n_units = (int)plan.n_units;
-  sp.score_stride = plan.longest;
-  FC_HIP(launch_select_blocks(sp, token_reqs, scored_reqs, stream));
-
+  set_selection(p, layer, dev_block_tables, max_blocks, dev_bounds, n_select, q, n_q_heads, dev_selected, plan, &sp);
   AttnParams ap = {};
   ap.kv = layer_blocks(p, layer);
   ap.source = p->dtype == FC_DTYPE_E4M3 ? ATTN_E4M3 : p->dtype == FC_DTYPE_E2M1 ? ATTN_E2M1 : ATTN_F16;
   set_queries(p, q, out, n_q_heads, scale, &ap);
-  ap.block_tables = sp.ids;
-  ap.max_blocks = n_select;
-  ap.table_heads = p->n_heads;
-  ap.reqs = on_device ? on_device + plan.tokens.size() : nullptr;
-  set_launches(p, launches, n_q_heads, &ap);
-  FC_HIP(launch_attention(ap, attention_inline, stream));
+  if (plan.part_blocks) return select_then_attend(p, &plan, n_q_heads, &sp, &ap, stream);
+  ChunkReqs token_reqs;
+  if ((rc = pass_reqs(p, plan.tokens, &token_reqs, &sp.tokens, stream))) return rc;
+  FC_HIP(launch_selected_attention(sp, ap, token_reqs, stream));
   return FC_OK;
 }
 

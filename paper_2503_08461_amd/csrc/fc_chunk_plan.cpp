@@ -196,19 +196,27 @@ int plan_sparse(const PoolView& pool, int n_cu, int group, int n_select, const C
     for (int i = 0; i < q.n_new; ++i) {
       const int seen = q.seq_len - q.n_new + i + 1, nb = blocks_for(seen), row = q.row_off + i;
       plan->tokens.push_back({q.table_row, seen, 0, row, 0, 0});
-      // (whole blocks, but for the token's own, the last one)
-      const int read = (std::min(nb, n_select) - 1) * kPlanBlockSize + (seen - 1) % kPlanBlockSize + 1;
-      plan->attention.reqs.push_back({row, read, 1, row, 0, 0});
       if (scores(nb)) plan->longest = std::max(plan->longest, nb - 1);
     }
   }
-  plan->attention.n_rows = chunk.n_rows;
-  // One launch for scores and selection where its workgroups fill the card or have little to read (384 heads of
-  // 80-440 blocks: 63.1 us a step, with two 66.2); else the scores are made by as many as fill it, and for the
-  // tokens of a request together.  (Up to half of the rows: what else is kept of the queries and blocks would not
-  // fit the LDS beside more.)
+  // One launch, a workgroup of four wavefronts for a token's head, where each has little to score, or where there are
+  // many, of single tokens; else the scores are made by as many workgroups as fill the card, and for the tokens of a
+  // request together.  us a step, fp16, n_select 64, one / apart, for so many single tokens times heads:
+  //   tokens cached     8            32           64           128          192
+  //   2000-2500         29.2 / 32.6  30.1 / 34.8  31.0 / 35.8  33.2 / 41.3  36.0 / 48.5
+  //   4000-5000         30.5 / 31.8  31.6 / 34.2  32.8 / 36.5  35.3 / 42.0  38.4 / 50.4
+  //   8000-10000        33.3 / 32.0  37.0 / 36.6  38.0 / 38.8  40.0 / 47.4  43.5 / 56.8
+  //   30000             52.0 / 32.4  53.6 / 37.9  54.8 / 41.6  59.0 / 60.9  65.8 / 85.1
+  // five tokens of 32 caches of 1000-1250, 8 heads: 91 / 93, of 16 of 4000-5000 77 / 72; 256 of two of 16000: 463 / 302.
+  // (Up to half of the rows: what else is kept of the queries and blocks would not fit the LDS beside more.)
   const int cu = std::max(n_cu, 1);
-  if (single && group <= kScoreRows / 2 && (chunk.n_rows * pool.n_heads >= cu || plan->longest <= 64)) return PLAN_OK;
+  if (group <= kScoreRows / 2 && (plan->longest <= 384 || (single && 2 * chunk.n_rows * pool.n_heads >= cu))) return PLAN_OK;
+  for (const ChunkReq& t : plan->tokens) {
+    // (whole blocks, but for the token's own, the last one)
+    const int read = (std::min(blocks_for(t.seq_len), n_select) - 1) * kPlanBlockSize + (t.seq_len - 1) % kPlanBlockSize + 1;
+    plan->attention.reqs.push_back({t.row_off, read, 1, t.row_off, 0, 0});
+  }
+  plan->attention.n_rows = chunk.n_rows;
   plan->tile_tokens = std::max(1, kScoreRows / group);
   int64_t total = 0;  // blocks of all workgroups
   auto tiles = [&](const ChunkReq& q) { return ((int64_t)q.n_new + plan->tile_tokens - 1) / plan->tile_tokens; };

@@ -66,8 +66,8 @@ struct SparsePlan {
   char message[256] = "";
   std::vector<ChunkReq> tokens;  // one a new token, row_off its packed row; unit_start and n_new: its scores' parts
   std::vector<ChunkReq> scored;  // requests whose scores are made in a launch of their own, state_off blocks each
-  ChunkPlan attention;           // the tokens as requests of their own, of the blocks that they read
-  int part_blocks = 0;           // 0: a workgroup scores and selects, else blocks a workgroup that scores
+  ChunkPlan attention;           // the tokens as requests of their own, of the blocks that they read (with part_blocks)
+  int part_blocks = 0;           // 0: a workgroup scores, selects and attends, else blocks a workgroup that scores
   int tile_tokens = 1;           // ... and tokens of a request at a time
   int64_t n_units = 0;           // ... parts of all
   int longest = 1;               // most blocks that a token scores

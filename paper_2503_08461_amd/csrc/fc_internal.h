@@ -149,8 +149,8 @@ struct SelectParams {
   int32_t* ids;            // [token][head][n_select] blocks of the pool, ascending in the request's table
   int32_t* selected;       // nullable: the same as entries of the table, -1 behind the last
   int32_t lds_keys;        // blocks that any token scores, at most
-  // Scores in a launch of their own (part_blocks 0: not): parts of part_blocks blocks, tile_tokens
-  // tokens of a request at a time.  One a request that scores: n_new tokens from row_off on,
+  // Scores in a launch of their own (part_blocks 0: not, and no ids): parts of part_blocks blocks,
+  // tile_tokens tokens of a request at a time.  One a request that scores: n_new tokens from row_off on,
   // state_off blocks, unit_start.
   int32_t part_blocks, tile_tokens;
   const ChunkReq* reqs;    // NULL: in the argument
@@ -203,7 +203,7 @@ static_assert(sizeof(AttnParams) + sizeof(AttnLaunchView) + sizeof(ChunkReqs) <=
                   sizeof(StoreParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
                   sizeof(RotateParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
                   sizeof(BoundsParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
-                  sizeof(SelectParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
+                  sizeof(SelectParams) + sizeof(AttnParams) + sizeof(ChunkReqs) + 8 <= kMaxArgumentBytes &&
                   sizeof(QuantiseParams) + sizeof(ChunkReqs) <= kMaxArgumentBytes &&
                   sizeof(ExtendParams) + sizeof(ExtendReqs) <= kMaxArgumentBytes,
               "kernels of chunks");
@@ -342,7 +342,10 @@ hipError_t launch_quantise(const QuantiseParams& p, const ChunkReqs& inline_reqs
 hipError_t launch_rotate_store(const RotateParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
 // bounds of blocks, and the blocks that queries select by them (fc_sparse.hip)
 hipError_t launch_bounds(const BoundsParams& p, const ChunkReqs& inline_reqs, hipStream_t s);
+// (with part_blocks)
 hipError_t launch_select_blocks(const SelectParams& p, const ChunkReqs& inline_tokens, const ChunkReqs& inline_reqs, hipStream_t s);
+// Selection and attention in one launch: no parts, up to 32 query heads of a head.
+hipError_t launch_selected_attention(const SelectParams& sp, const AttnParams& p, const ChunkReqs& inline_tokens, hipStream_t s);
 // attention of chunks (fc_attention.hip)
 hipError_t attention_one_time_setup();
 hipError_t launch_attention(const AttnParams& p, const ChunkReqs& inline_reqs, hipStream_t s);

@@ -1,6 +1,6 @@
-// Attention over selected blocks: the bounds of blocks, and which blocks a query selects by them.
-// (What is selected is attended to by the kernels of fc_attention.hip, through block tables of
-// its own for every token and head.)
+// Attention over selected blocks: the bounds of blocks, and, where the scores take a launch of their own, which
+// blocks a query selects by them (fc_select_blocks.h).  What is selected is attended to by the kernels of
+// fc_attention.hip, through block tables of its own for every token and head.
 //
 // bounds: lo_c = min k_c, hi_c = max k_c over the tokens of a block, one head.
 // score of a block for query heads q_1 .. q_g of a head of K:
@@ -9,8 +9,8 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "fc_chunk_plan.h"
 #include "fc_e2m1.h"
+#include "fc_select_blocks.h"
 
 namespace fc {
 
@@ -79,552 +79,11 @@ __global__ __launch_bounds__(256) void bounds_kernel(BoundsParams p, Reqs reqs) 
   }
 }
 
-// ---------------------------------------------------------------------------
-// selection.  A score is a sum in 64 bits: a product of two fp16 numbers is exact in fp32, and which of
-// two blocks is read should follow from the inputs, not from the order in which a sum was made.  All
-// scores are made by the matrix cores in fp32 first,
-//     S [query heads x blocks] = min(Q, 0) . LO^T + max(Q, 0) . HI^T,
-// which is the same sum, off by at most E = 2 D 2^-23 (largest sum of |q|) (largest |bound|): each of 2 D
-// additions by 2^-23 of what was added up so far, twice what a rounding loses.  With T the k-th largest of
-// them, scores over T + 2 E are among the k best and those below T - 2 E are not; the few between are made
-// anew in 64 bits.  (What is infinite or not a number makes E so, and all blocks are "between".)
-// In 64 bits throughout, five vector instructions for each product, 48 caches of 1280-7040 tokens, 8 heads of
-// 4, took 22 us for the scores alone, and 10 tokens over 28 000-30 000 27; with the matrix cores the former are scored
-// and selected from in 18-19.7, of which a workgroup spends 3.3 on its first loads, 3.6 on scores and 4.4 on the
-// selection (medians; latency and barriers), the latter scored in 7.5 and selected from in 7.9.
-// ---------------------------------------------------------------------------
-
-// The order of scores as that of unsigned numbers: larger ones are larger, not a number is the
-// largest, both zeros are one; 0 is none of them.
-__device__ __forceinline__ uint64_t score_order(double s) {
-  const uint64_t bits = __builtin_bit_cast(uint64_t, s + 0.0);
-  if (s != s) return ~0ull;
-  return bits >> 63 ? ~bits : bits | (1ull << 63);
-}
-
-// Workgroups that select have this many wavefronts (with four, the scores of 1809 blocks, eight a thread, took 8.5 us to
-// select from, where 1.6 are for what is read first).
+// Workgroups of the kernels that select have this many wavefronts (with four, the scores of 1809 blocks, eight a thread,
+// took 8.5 us to select from, where 1.6 are for what is read first).
 constexpr int kSelectWaves = 8, kSelectThreads = 64 * kSelectWaves;
 
-template <int CTRL>
-__device__ __forceinline__ double from_lane_f64(double v) {
-  const uint64_t b = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = from_lane_u32<CTRL>((uint32_t)b), hi = from_lane_u32<CTRL>((uint32_t)(b >> 32));
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-
-__device__ __forceinline__ const _Float16* query_of(const SelectParams& p, int row, int q_head) {
-  return p.q.data + (int64_t)row * p.q.token_stride + (int64_t)q_head * p.q.head_stride;
-}
-
-// The first product's operands: of up to kRows rows (token * group + query head of the group, zeros behind the last
-// one, in tiles of 16) the parts below and above zero, 2 D numbers each, in LDS in the order of the lanes, 32 at a time.
-// Requested when this is made, before the bounds: loads are answered in order.
-template <int D, int kRows, int kThreadsHere>
-struct ScoredQueries {
-  static constexpr int KK = 2 * D / 32, PPR = D / 8, kEach = (kRows * PPR + kThreadsHere - 1) / kThreadsHere;
-  half8 x[kEach];
-  int rows;
-  __device__ __forceinline__ ScoredQueries(const SelectParams& p, int first_row, int n_tokens, int head) : rows(n_tokens * p.group) {
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      const int i = k * kThreadsHere + (int)threadIdx.x, r = i / PPR, c = i % PPR;
-      x[k] = half8{};
-      if (r < rows) {
-        const int t = r / p.group;
-        x[k] = load_half8(query_of(p, first_row + t, head * p.group + r - t * p.group) + c * 8);
-      }
-    }
-    requests_first();
-  }
-  // sm_q: NULL, or for the rows themselves
-  __device__ __forceinline__ void put(half8* sm_a, _Float16* sm_q) const {
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      const int i = k * kThreadsHere + (int)threadIdx.x, r = i / PPR, c = i % PPR;
-      if (r >= ((rows + 15) & ~15)) continue;
-      if (sm_q && r < rows) store_half8(sm_q + r * D + c * 8, x[k]);
-      half8 below, above;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        below[e] = x[k][e] < (_Float16)0.f ? x[k][e] : (_Float16)0.f;
-        above[e] = x[k][e] > (_Float16)0.f ? x[k][e] : (_Float16)0.f;
-      }
-      half8* to = sm_a + (size_t)(r >> 4) * KK * 64 + (r & 15);
-      to[(c / 4) * 64 + (c % 4) * 16] = below;
-      to[((c + PPR) / 4) * 64 + ((c + PPR) % 4) * 16] = above;
-    }
-    __syncthreads();
-  }
-};
-
-// Scores of blocks [b0, b1) for some tokens.  A wavefront has 16 blocks at a time, a block a column.  The first ones
-// are requested when this is made: a block's number and its bounds are two latencies, one after the other.
-template <int D, int W>
-struct BlockScores {  // W: wavefronts of the workgroup
-  static constexpr int KK = 2 * D / 32;
-  struct Bounds {
-    half8 x[KK];
-  };
-  const SelectParams& p;
-  const int32_t* table;
-  int head, b0, b1, n, id;  // n: of the wavefront's sixteens; id: of the lane's block in the next one
-  Bounds a, b;
-  __device__ __forceinline__ BlockScores(const SelectParams& p_, const int32_t* table_, int head_, int b0_, int b1_)
-      : p(p_), table(table_), head(head_), b0(b0_), b1(b1_) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    n = max(own_tiles((b1 - b0 + 15) / 16, wave, W), 0);
-    id = table[block(0)];
-    const int second = table[block(1)];
-    request(a);
-    id = second;
-  }
-  __device__ __forceinline__ int first(int i) const { return b0 + ((int)(threadIdx.x >> 6) + W * i) * 16; }
-  __device__ __forceinline__ int block(int i) const { return min(first(i) + (int)(threadIdx.x & 15), b1 - 1); }
-  __device__ __forceinline__ void request(Bounds& t) const {
-    const _Float16* from = p.bounds + ((size_t)clamp_block(id, p.n_blocks) * p.n_heads + head) * 2 * D + ((threadIdx.x & 63) >> 4) * 8;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) t.x[kk] = load_half8(from + kk * 32);
-    requests_first();
-  }
-  // out(token, block, score); room: 16 numbers for every row, the wavefront's own.  Returns the largest
-  // magnitude of the bounds that the thread has seen, as fp16 bits.
-  template <typename Out>
-  __device__ __forceinline__ uint32_t run(int n_tokens, const half8* sm_a, float* room, Out out) {
-    const int lane = threadIdx.x & 63, col = lane & 15, part = lane >> 4;
-    const int tiles = (n_tokens * p.group + 15) >> 4;
-    uint32_t most = 0;
-    auto use = [&](int i, const Bounds& t) {
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        const uint4v w = __builtin_bit_cast(uint4v, t.x[kk]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) most = max(most, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
-      }
-      for (int tile = 0; tile < tiles; ++tile) {
-        floatx4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
-          s = __builtin_amdgcn_mfma_f32_16x16x32_f16(sm_a[(tile * KK + kk) * 64 + lane], t.x[kk], s, 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) room[(tile * 16 + part * 4 + r) * 16 + col] = s[r];
-      }
-      wave_lds_barrier();
-      // (a score that is not a number: E is none, too)
-      if (first(i) + col < b1)
-        for (int token = part; token < n_tokens; token += 4) {
-          float best = -INFINITY;
-          for (int h = 0; h < p.group; ++h) best = fmaxf(best, room[(token * p.group + h) * 16 + col]);
-          out(token, first(i) + col, best);
-        }
-      wave_lds_barrier();
-    };
-    // (behind the last sixteen: the last block again, of which nothing is made)
-    for (int i = 0; i < n; i += 2) {
-      int ahead = table[block(i + 2)];
-      request(b);
-      id = ahead;
-      use(i, a);
-      if (i + 1 == n) break;
-      ahead = table[block(i + 3)];
-      request(a);
-      id = ahead;
-      use(i + 1, b);
-    }
-    return most;
-  }
-};
-
-// The order of the scores in 64 bits of the n blocks listed, into keys[].  D / 8 neighbouring lanes a block;
-// sm_q: the queries [query head of the group][D].
-template <int D>
-__device__ __forceinline__ void score_exactly(const SelectParams& p, const _Float16* sm_q, int head, const int32_t* blocks, int n,
-                                              uint64_t* keys) {
-  constexpr int PPR = D / 8;
-  const int piece = threadIdx.x % PPR;
-  for (int i = threadIdx.x / PPR; i < n; i += kSelectThreads / PPR) {
-    const _Float16* from = p.bounds + ((size_t)clamp_block(blocks[i], p.n_blocks) * p.n_heads + head) * 2 * D + piece * 8;
-    const half8 lo = load_half8(from), hi = load_half8(from + D);
-    uint64_t best = 0;
-    for (int h = 0; h < p.group; ++h) {
-      const half8 q = load_half8(sm_q + h * D + piece * 8);
-      double s = 0.0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s += (double)fmaxf((float)q[e] * (float)lo[e], (float)q[e] * (float)hi[e]);
-      s += from_lane_f64<0xB1>(s);
-      s += from_lane_f64<0x4E>(s);
-      s += from_lane_f64<0x141>(s);
-      if constexpr (PPR == 16) s += from_lane_f64<0x140>(s);
-      const uint64_t key = score_order(s);
-      best = key > best ? key : best;
-    }
-    if (piece == 0) keys[i] = best;
-  }
-}
-
-constexpr int kMaxKeys = kPlanMaxSeqLen / kPlanBlockSize, kPerThread = kMaxKeys / kSelectThreads;
-
-// set bits of the lanes below this one
-__device__ __forceinline__ uint32_t below_lane(uint64_t set) {
-  return __builtin_amdgcn_mbcnt_hi((uint32_t)(set >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)set, 0));
-}
-
-// For every element i = j * kSelectThreads + thread (j < mine): how many before it have the first flag and how many the second,
-// in the low and high half of before[j]; returns how many there are of each.  counts: kPerThread * kSelectWaves numbers in
-// LDS, free when all threads are here.
-template <typename One, typename Two>
-__device__ __forceinline__ uint32_t places_of(int mine, One one, Two two, uint32_t* counts, uint32_t* before) {
-  static_assert(kPerThread * kSelectWaves <= 64 && kMaxKeys < 1 << 16, "a count a lane, two in a word");
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j) {
-    const uint64_t a = j < mine ? __ballot(one(j)) : 0, b = j < mine ? __ballot(two(j)) : 0;
-    before[j] = below_lane(a) | below_lane(b) << 16;
-    if (j < mine && lane == 0) counts[j * kSelectWaves + wave] = __popcll(a) | __popcll(b) << 16;
-  }
-  __syncthreads();
-  const uint32_t own = lane < mine * kSelectWaves ? counts[lane] : 0;
-  const uint32_t sum = (uint32_t)wave_scan_add((int)own);
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j) before[j] += (uint32_t)__builtin_amdgcn_readlane((int)(sum - own), j * kSelectWaves + wave);
-  return (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
-}
-
-// The k-th largest of n > k > 0 keys, key[j] of thread t being that of element j * kSelectThreads + t (0: none; Key: 32 or
-// 64 bits, no key is 0): a threshold that exactly k keys reach, or the k-th one itself where more do.  Two bits at a
-// time from the first one in which keys differ, with three counts of all keys a step.  reached: how many keys reach it.
-template <typename Key>
-struct FoundKey {
-  Key threshold;
-  int reached;
-};
-template <typename Key>
-__device__ __forceinline__ FoundKey<Key> kth_largest(const Key (&key)[kPerThread], int n, int k) {
-  typedef int int4v __attribute__((ext_vector_type(4)));
-  __shared__ int4v sm_count[2][kSelectWaves];
-  __shared__ Key sm_most[kSelectWaves], sm_least[kSelectWaves];
-  constexpr int kBits = 8 * sizeof(Key);
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int mine = (n + kSelectThreads - 1) / kSelectThreads;  // uniform
-  Key most = 0, least = ~(Key)0;
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j) {
-    most = key[j] > most ? key[j] : most;
-    least = key[j] != 0 && key[j] < least ? key[j] : least;
-  }
-  if constexpr (kBits == 32) {
-    most = wave_max(most);
-    least = wave_min(least);
-  } else {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-      const Key a = __shfl_xor((unsigned long long)most, d), b = __shfl_xor((unsigned long long)least, d);
-      most = a > most ? a : most;
-      least = b < least ? b : least;
-    }
-  }
-  if (lane == 0) {
-    sm_most[wave] = most;
-    sm_least[wave] = least;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kSelectWaves; ++w) {
-    most = sm_most[w] > most ? sm_most[w] : most;
-    least = sm_least[w] < least ? sm_least[w] : least;
-  }
-  // all keys have the bits above the pair of the first one in which the largest and the smallest differ
-  const Key differ = (most ^ least) | 1;
-  int shift = (kBits - 1 - (kBits == 64 ? __builtin_clzll((uint64_t)differ) : __builtin_clz((uint32_t)differ))) & ~1;
-  FoundKey<Key> f = {shift == kBits - 2 ? (Key)0 : most >> (shift + 2) << (shift + 2), n};
-  for (int step = 0; shift >= 0 && f.reached != k; shift -= 2, ++step) {
-    int count[4] = {};
-#pragma unroll
-    for (int d = 1; d < 4; ++d) {
-      const Key candidate = f.threshold | (Key)d << shift;
-#pragma unroll
-      for (int j = 0; j < kPerThread; ++j)
-        if (j < mine) count[d] += __popcll(__ballot(key[j] >= candidate));
-    }
-    if (lane == 0) sm_count[step & 1][wave] = int4v{0, count[1], count[2], count[3]};
-    __syncthreads();
-    int4v sum = {0, 0, 0, 0};
-#pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w) sum += sm_count[step & 1][w];
-    const int d = sum[3] >= k ? 3 : sum[2] >= k ? 2 : sum[1] >= k ? 1 : 0;
-    f.threshold |= (Key)d << shift;
-    if (d > 0) f.reached = d == 3 ? sum[3] : d == 2 ? sum[2] : sum[1];
-  }
-  return f;
-}
-
-// What a selection needs of LDS: blocks between, their keys, whether they are kept.
-struct Between {
-  int32_t* blocks;
-  uint64_t* keys;
-};
-constexpr size_t between_bytes(int n) { return (size_t)((n + 1) / 2 * 2) * (sizeof(int32_t) + sizeof(uint64_t)); }
-
-// What a thread knows of blocks j * kSelectThreads + thread of a table (-infinity, 0 behind the last one).
-struct Scored {
-  float score[kPerThread];
-  int32_t id[kPerThread];
-  int32_t last_id;  // of the token's own block, which is not scored
-};
-
-constexpr int kBuckets = 1024;  // of scores, as wide as each other
-
-// The k best of n > k > 0 blocks by their scores, out(place, j) in ascending order.  sm_q as above, made by threads
-// that need not have met since; most: the largest magnitude of a bound.
-// The k-th largest score T is looked for only as far as the bucket that holds it: what is in its reach, 2 E and the
-// bucket, is scored anew.  (With T itself, found bit by bit with a count of all keys and a barrier for each, 5.1 us for
-// 1809 blocks and 2.7 for 92; so 1.4.)
-template <int D, typename Out>
-__device__ __forceinline__ void select_best(const SelectParams& p, const _Float16* sm_q, int head, const Scored& b, int n, int k, float most,
-                                            Between between, Out out) {
-  static_assert(kBuckets % kSelectThreads == 0, "whole");
-  constexpr int kOwn = kBuckets / kSelectThreads;
-  __shared__ uint32_t sm_place[kPerThread * kSelectWaves];
-  __shared__ uint32_t sm_bucket[kBuckets];
-  __shared__ float sm_sum[kSelectWaves], sm_top[kSelectWaves], sm_low[kSelectWaves];
-  __shared__ int sm_above[kSelectWaves], sm_found;
-  __shared__ uint64_t sm_kept;
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int mine = (n + kSelectThreads - 1) / kSelectThreads;
-  float top = -INFINITY, low = INFINITY;
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j) {
-    if (j * kSelectThreads + (int)threadIdx.x >= n) continue;
-    top = fmaxf(top, b.score[j]);
-    low = fminf(low, b.score[j]);
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    top = fmaxf(top, __shfl_xor(top, d));
-    low = fminf(low, __shfl_xor(low, d));
-  }
-  for (int i = 0; i < kOwn; ++i) sm_bucket[i * kSelectThreads + threadIdx.x] = 0;
-  if (lane == 0) {
-    sm_top[wave] = top;
-    sm_low[wave] = low;
-  }
-  __syncthreads();
-  // the largest sum of |q|
-  float sum = 0.f;
-  for (int h = wave; h < p.group; h += kSelectWaves) {
-    float s = 0.f;
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) s += fabsf((float)sm_q[h * D + lane * (D / 64) + c]);
-    s = wave_sum(s);
-    sum = s > sum || s != s ? s : sum;
-  }
-  if (lane == 0) sm_sum[wave] = sum;
-#pragma unroll
-  for (int w = 0; w < kSelectWaves; ++w) {
-    top = fmaxf(top, sm_top[w]);
-    low = fminf(low, sm_low[w]);
-  }
-  // bucket 0: the best.  (Monotone in the score, whatever the rounding; all in one where the range is nothing, or none)
-  const float per = kBuckets / (top - low), scale = per < 3e38f ? per : 0.f;
-  auto bucket_of = [&](float s) { return min((int)fmaxf((top - s) * scale, 0.f), kBuckets - 1); };
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j)
-    if (j * kSelectThreads + (int)threadIdx.x < n) atomicAdd(&sm_bucket[bucket_of(b.score[j])], 1u);
-  __syncthreads();
-  int own[kOwn], mine_sum = 0;
-#pragma unroll
-  for (int i = 0; i < kOwn; ++i) {
-    own[i] = (int)sm_bucket[threadIdx.x * kOwn + i];
-    mine_sum += own[i];
-  }
-  const int scan = wave_scan_add(mine_sum);
-  if (lane == 63) sm_above[wave] = scan;
-  __syncthreads();
-  int above = scan - mine_sum;
-#pragma unroll
-  for (int w = 0; w < kSelectWaves; ++w) {
-    above += w < wave ? sm_above[w] : 0;
-    sum = sm_sum[w] > sum || sm_sum[w] != sm_sum[w] ? sm_sum[w] : sum;
-  }
-#pragma unroll
-  for (int i = 0; i < kOwn; ++i) {
-    if (above < k && above + own[i] >= k) sm_found = (int)threadIdx.x * kOwn + i;
-    above += own[i];
-  }
-  __syncthreads();
-  const int found = sm_found;
-  // Sure: over every score of that bucket by more than 2 E; out of reach: as far below.  (The bucket's ends, and a
-  // little more than 2 E: this arithmetic is rounded, by less than a thousandth of a bucket and 2^-22 of a score,
-  // of which 2 E is 2^-14 at least)
-  const float margin = 2.1f * (2 * D) * 0x1p-23f * sum * most;
-  const float width = scale > 0.f ? (top - low) * (1.f / kBuckets) : top - low;
-  const float sure_from = top - (found - 0.01f) * width + margin, least = top - (found + 1.01f) * width - margin;
-  const bool all = !(margin < INFINITY) || !(width < INFINITY);
-  auto within = [&](int j) { return j * kSelectThreads + (int)threadIdx.x < n; };
-  auto is_sure = [&](int j) { return within(j) && !all && b.score[j] > sure_from; };
-  auto is_between = [&](int j) { return within(j) && (all || (b.score[j] >= least && b.score[j] <= sure_from)); };
-  uint32_t before[kPerThread];
-  const uint32_t n_both = places_of(mine, is_sure, is_between, sm_place, before);
-  const int n_between = (int)(n_both >> 16), wanted = k - (int)(n_both & 0xffff);  // of those between
-  if (n_between == wanted) {
-#pragma unroll
-    for (int j = 0; j < kPerThread; ++j)
-      if (is_sure(j) || is_between(j)) out((before[j] & 0xffff) + (before[j] >> 16), j);
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j)
-    if (is_between(j)) between.blocks[before[j] >> 16] = b.id[j];
-  __syncthreads();
-  score_exactly<D>(p, sm_q, head, between.blocks, n_between, between.keys);
-  __syncthreads();
-  if (n_between <= 64) {
-    // (ties: the lower blocks, which come first)
-    if (wave == 0) {
-      const uint64_t own_key = lane < n_between ? between.keys[lane] : 0;
-      int rank = 0;
-      for (int i = 0; i < n_between; ++i) {
-        const uint64_t other = between.keys[i];
-        rank += other > own_key || (other == own_key && i < lane) ? 1 : 0;
-      }
-      const uint64_t kept = __ballot(lane < n_between && rank < wanted);
-      if (lane == 0) sm_kept = kept;
-    }
-    __syncthreads();
-    const uint64_t kept = sm_kept;
-#pragma unroll
-    for (int j = 0; j < kPerThread; ++j) {
-      const int i = (int)(before[j] >> 16);
-      const bool keep = is_between(j) && (kept >> i & 1);
-      if (keep || is_sure(j)) out((before[j] & 0xffff) + (i < 64 ? __popcll(kept & ((1ull << i) - 1)) : __popcll(kept)), j);
-    }
-    return;
-  }
-  uint64_t exact[kPerThread];
-  const int parts = (n_between + kSelectThreads - 1) / kSelectThreads;
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j) {
-    const int i = j * kSelectThreads + (int)threadIdx.x;
-    exact[j] = i < n_between ? between.keys[i] : 0;
-  }
-  const FoundKey<uint64_t> f = kth_largest<uint64_t>(exact, n_between, wanted);
-  // of the keys that are equal to the threshold the first ones stay
-  uint32_t place[kPerThread];
-  const uint32_t n_above = places_of(parts, [&](int j) { return exact[j] > f.threshold; }, [&](int j) { return exact[j] == f.threshold; },
-                                     sm_place, place) & 0xffff;
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j) {
-    const int i = j * kSelectThreads + (int)threadIdx.x;
-    if (i < n_between) between.blocks[i] = exact[j] > f.threshold || (exact[j] == f.threshold && (place[j] >> 16) < (uint32_t)wanted - n_above);
-  }
-  __syncthreads();
-  uint64_t keep = 0;
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j)
-    if (is_sure(j) || (is_between(j) && between.blocks[before[j] >> 16])) keep |= 1ull << j;
-  places_of(mine, [&](int j) { return (keep >> j & 1) != 0; }, [](int) { return false; }, sm_place, place);
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j)
-    if (keep >> j & 1) out(place[j] & 0xffff, j);
-}
-
-// What a token's head reads: the blocks selected, then the token's own one (all, if there are no more).
-struct Selection {
-  int32_t *ids, *selected;
-  __device__ __forceinline__ Selection(const SelectParams& p, int64_t at)
-      : ids(p.ids + at * p.n_select), selected(p.selected ? p.selected + at * p.n_select : nullptr) {}
-  __device__ __forceinline__ void put(int place, int block, int32_t id) const {
-    ids[place] = id;
-    if (selected) selected[place] = block;
-  }
-  __device__ __forceinline__ void put_all(const SelectParams& p, const int32_t* table, int nb) const {
-    for (int b = threadIdx.x; b < p.n_select; b += kSelectThreads) {
-      if (b < nb)
-        put(b, b, table[b]);
-      else if (selected)
-        selected[b] = -1;
-    }
-  }
-};
-template <int D>
-__device__ __forceinline__ void write_selection(const SelectParams& p, const _Float16* sm_q, int nb, int head, int64_t at,
-                                                const Scored& b, float most, Between between) {
-  const Selection to(p, at);
-  select_best<D>(p, sm_q, head, b, nb - 1, p.n_select - 1, most, between,
-                 [&](int place, int j) { to.put(place, j * kSelectThreads + (int)threadIdx.x, b.id[j]); });
-  if (threadIdx.x == 0) to.put(p.n_select - 1, nb - 1, b.last_id);
-}
-
-// Where the thread's blocks lie; the queries to LDS.
-__device__ __forceinline__ void request_blocks(const int32_t* table, int n, Scored& b) {
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j) {
-    const int i = j * kSelectThreads + (int)threadIdx.x;
-    b.id[j] = i < n ? table[i] : 0;
-  }
-  b.last_id = table[n];
-}
-template <int D>
-__device__ __forceinline__ void request_queries(const SelectParams& p, int row, int head, _Float16* sm_q) {
-  for (int i = threadIdx.x; i < p.group * (D / 8); i += kSelectThreads) {
-    const int h = i / (D / 8), c = i % (D / 8);
-    store_half8(sm_q + h * D + c * 8, load_half8(query_of(p, row, head * p.group + h) + c * 8));
-  }
-}
-
-// The largest of fp16 magnitudes as a number: not one, where one isn't.
-__device__ __forceinline__ float magnitude(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
-
-// Scores and selection by one workgroup, of the one new token of a request.
-template <int D, typename Reqs>
-__global__ __launch_bounds__(kSelectThreads) void select_blocks_kernel(SelectParams p, Reqs reqs) {
-  extern __shared__ __align__(16) char sm[];
-  __shared__ uint32_t sm_most[kSelectWaves];
-  const int token = blockIdx.x / p.n_heads;
-  const int head = blockIdx.x - token * p.n_heads;
-  const ChunkReq rq = reqs.req[token];
-  const int nb = (rq.seq_len + 15) >> 4;
-  const int32_t* table = p.block_tables + (size_t)rq.table_row * p.max_blocks;
-  const int64_t at = (int64_t)token * p.n_heads + head;
-  if (nb <= p.n_select) {
-    Selection(p, at).put_all(p, table, nb);
-    return;
-  }
-  if (p.n_select == 1) {
-    if (threadIdx.x == 0) Selection(p, at).put(0, nb - 1, table[nb - 1]);
-    return;
-  }
-  // queries, scores, then the operands and the wavefronts' rooms, and in their place what is between
-  _Float16* sm_q = reinterpret_cast<_Float16*>(sm);
-  float* scores = reinterpret_cast<float*>(sm_q + p.group * D);
-  char* rest = reinterpret_cast<char*>(scores) + ((p.lds_keys * sizeof(float) + 15) & ~(size_t)15);
-  const int rows = (p.group + 15) & ~15;
-  half8* sm_a = reinterpret_cast<half8*>(rest);
-  float* room = reinterpret_cast<float*>(rest + rows * 2 * D * 2) + (threadIdx.x >> 6) * rows * 16;
-  const ScoredQueries<D, kScoreRows / 2, kSelectThreads> queries(p, rq.row_off, 1, head);
-  BlockScores<D, kSelectWaves> blocks(p, table, head, 0, nb - 1);
-  Scored b;
-  request_blocks(table, nb - 1, b);
-  queries.put(sm_a, sm_q);
-  uint32_t most = blocks.run(1, sm_a, room, [&](int, int i, float s) { scores[i] = s; });
-  most = wave_max(most);
-  if ((threadIdx.x & 63) == 0) sm_most[threadIdx.x >> 6] = most;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kSelectWaves; ++w) most = max(most, sm_most[w]);
-#pragma unroll
-  for (int j = 0; j < kPerThread; ++j) {
-    const int i = j * kSelectThreads + (int)threadIdx.x;
-    b.score[j] = i < nb - 1 ? scores[i] : -INFINITY;
-  }
-  uint64_t* keys = reinterpret_cast<uint64_t*>(rest);
-  write_selection<D>(p, sm_q, nb, head, at, b, magnitude(most), Between{reinterpret_cast<int32_t*>(keys + p.lds_keys), keys});
-}
-
-// Scores alone: workgroup = (part of the blocks, some tokens of a request, head).  The requests: n_new tokens,
+// Scores: workgroup = (part of the blocks, some tokens of a request, head).  The requests: n_new tokens,
 // state_off blocks that the last one scores, in parts of p.part_blocks.
 template <int D, typename Reqs>
 __global__ __launch_bounds__(kThreads) void block_scores_kernel(SelectParams p, Reqs reqs) {
@@ -656,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void block_scores_kernel(SelectParams p, 
   }
 }
 
-// The selection alone: workgroup = (token, head).  The tokens: unit_start the first part's unit, n_new their number.
+// The selection: workgroup = (token, head).  The tokens: unit_start the first part's unit, n_new their number.
 template <int D, typename Reqs>
 __global__ __launch_bounds__(kSelectThreads) void select_scored_kernel(SelectParams p, Reqs reqs) {
   extern __shared__ __align__(16) char sm[];
@@ -666,26 +125,20 @@ __global__ __launch_bounds__(kSelectThreads) void select_scored_kernel(SelectPar
   const int nb = (rq.seq_len + 15) >> 4;
   const int32_t* table = p.block_tables + (size_t)rq.table_row * p.max_blocks;
   const int64_t at = (int64_t)token * p.n_heads + head;
-  if (nb <= p.n_select) {
-    Selection(p, at).put_all(p, table, nb);
-    return;
-  }
-  if (p.n_select == 1) {
-    if (threadIdx.x == 0) Selection(p, at).put(0, nb - 1, table[nb - 1]);
-    return;
-  }
+  const Selection to(p, p.ids + at * p.n_select, at);
+  if (to.put_all<kSelectWaves>(p, table, nb)) return;
   _Float16* sm_q = reinterpret_cast<_Float16*>(sm);
   uint64_t* keys = reinterpret_cast<uint64_t*>(sm_q + p.group * D);
   // (all of it requested before any of it is waited for)
-  Scored b;
+  Scored<kSelectWaves> b;
 #pragma unroll
-  for (int j = 0; j < kPerThread; ++j) b.score[j] = p.scores[at * p.score_stride + min(j * kSelectThreads + (int)threadIdx.x, nb - 2)];
-  request_blocks(table, nb - 1, b);
+  for (int j = 0; j < kPerThread<kSelectWaves>; ++j) b.score[j] = p.scores[at * p.score_stride + min(j * kSelectThreads + (int)threadIdx.x, nb - 2)];
+  request_blocks<kSelectWaves>(table, nb - 1, b);
   uint32_t most = 0;
   for (int i = threadIdx.x & 63; i < rq.n_new; i += 64) most = max(most, p.most[(int64_t)(rq.unit_start + i) * p.n_heads + head]);
-  request_queries<D>(p, rq.row_off, head, sm_q);
+  request_queries<D, kSelectWaves>(p, rq.row_off, head, sm_q);
   most = wave_max(most);
-  write_selection<D>(p, sm_q, nb, head, at, b, magnitude(most), Between{reinterpret_cast<int32_t*>(keys + p.lds_keys), keys});
+  write_selection<D, kSelectWaves>(p, sm_q, nb, head, to, b, magnitude(most), Between{reinterpret_cast<int32_t*>(keys + p.lds_keys), keys});
 }
 
 }  // namespace
@@ -704,27 +157,17 @@ hipError_t launch_bounds(const BoundsParams& p, const ChunkReqs& inline_reqs, hi
 
 hipError_t launch_select_blocks(const SelectParams& p, const ChunkReqs& inline_tokens, const ChunkReqs& inline_reqs, hipStream_t s) {
   if (p.n_tokens == 0) return hipSuccess;
-  if (p.group > (p.part_blocks ? kScoreRows : kScoreRows / 2) || p.tile_tokens * p.group > kScoreRows) return hipErrorInvalidValue;  // (LDS)
-  if ((p.head_dim != 64 && p.head_dim != 128) || p.n_select < 1 || p.lds_keys < 1 || p.lds_keys > kMaxKeys || p.score_stride > kMaxKeys ||
-      (p.part_blocks && p.tile_tokens < 1))
+  if ((p.head_dim != 64 && p.head_dim != 128) || p.group > kScoreRows || p.tile_tokens * p.group > kScoreRows || p.tile_tokens < 1 ||
+      p.n_select < 1 || p.part_blocks < 1 || p.lds_keys < 1 || p.lds_keys > kMaxKeys || p.score_stride > kMaxKeys)
     return hipErrorInvalidValue;
   const unsigned heads = (unsigned)p.n_tokens * p.n_heads;
   const size_t between = between_bytes(p.lds_keys), queries = (size_t)p.group * p.head_dim * sizeof(_Float16);
-  auto operands = [&](int rows, int waves) { return (size_t)((rows + 15) & ~15) * (2 * p.head_dim * 2 + waves * 16 * sizeof(float)); };
   auto launch = [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    if (p.part_blocks == 0) {
-      const size_t lds = queries + ((p.lds_keys * sizeof(float) + 15) & ~(size_t)15) + std::max(between, operands(p.group, kSelectWaves));
-      with_reqs_of(p.tokens, inline_tokens, [&](const auto& reqs) {
-        using Reqs = std::decay_t<decltype(reqs)>;
-        select_blocks_kernel<D, Reqs><<<heads, kSelectThreads, lds, s>>>(p, reqs);
-      });
-      return;
-    }
     if (p.n_units > 0)
       with_reqs_of(p.reqs, inline_reqs, [&](const auto& reqs) {
         using Reqs = std::decay_t<decltype(reqs)>;
-        block_scores_kernel<D, Reqs><<<(unsigned)p.n_units * p.n_heads, kThreads, operands(p.tile_tokens * p.group, kWaves), s>>>(p, reqs);
+        block_scores_kernel<D, Reqs><<<(unsigned)p.n_units * p.n_heads, kThreads, operand_bytes(p, p.tile_tokens * p.group, kWaves), s>>>(p, reqs);
       });
     with_reqs_of(p.tokens, inline_tokens, [&](const auto& reqs) {
       using Reqs = std::decay_t<decltype(reqs)>;

@@ -35,6 +35,14 @@ hipError_t launch_select_blocks(const SelectParams& p, const ChunkReqs&, const C
                   std::to_string(p.n_units) + ":" + std::to_string(p.lds_keys);
   return launched(s.c_str());
 }
+hipError_t launch_selected_attention(const SelectParams& sp, const AttnParams& p, const ChunkReqs& tokens, hipStream_t) {
+  std::string s = "selected" + std::to_string(p.source) + (sp.tokens ? "" : "_inline") + ":" + std::to_string(sp.n_tokens) + ":" +
+                  std::to_string(sp.lds_keys);
+  if (!sp.tokens)
+    for (int i = 0; i < sp.n_tokens && i < 3; ++i)
+      s += ":" + std::to_string(tokens.req[i].table_row) + "," + std::to_string(tokens.req[i].seq_len) + "," + std::to_string(tokens.req[i].row_off);
+  return launched(s.c_str());
+}
 }  // namespace fc
 
 // Calls just within and just beyond what one launch takes: fewer than 2^32 threads.
@@ -184,7 +192,6 @@ int main(int argc, char**) {
   };
   const int32_t one[2] = {1, 1};
   sparse("sparse", 3, &ok, &ok, 8, nullptr, table, nullptr, one);
-  for (const ChunkReq& r : g_attended) printf("reads %d %d %d %d\n", r.table_row, r.seq_len, r.n_new, r.row_off);
   sparse("sparse4", 2048, &ok, &ok, 4, nullptr, nullptr, p4);
   sparse("sparse8", 1, &ok, &ok, 4, nullptr, nullptr, p8);
   sparse("sparse_none", 0, &ok, &ok);
@@ -201,24 +208,32 @@ int main(int argc, char**) {
   report("sparse_long", fc_sparse_attention(p16, 0, table, 2048, long_lens, first, bounds, 64, &ok, 4, &ok, nullptr, 1, 0.f, nullptr));
   for (const ChunkReq& r : g_attended) printf("reads %d %d %d %d\n", r.table_row, r.seq_len, r.n_new, r.row_off);
 
-  // captured: nothing is allocated
-  const int n = 150;
-  std::vector<int32_t> l(n, 200), ones(n, 1);
+  // two tokens of one of 8001 (the first one's block ends there), one of 41
+  int32_t some_lens[2] = {8001, 41}, some_news[2] = {2, 1};
+  report("sparse_apart", fc_sparse_attention(p8, 0, table, 2048, some_lens, some_news, bounds, 64, &ok, 4, &ok, nullptr, 2, 0.f, nullptr));
+  for (const ChunkReq& r : g_attended) printf("reads %d %d %d %d\n", r.table_row, r.seq_len, r.n_new, r.row_off);
+  // 33 query heads of a head
+  const fc_rows many_q = {somewhere<void>(), 4 * 33 * 128, 128};
+  report("sparse_rows", fc_sparse_attention(p16, 0, table, 8, lens, one, bounds, 3, &many_q, 4 * 33, &many_q, nullptr, 2, 0.f, nullptr));
+
+  // captured: nothing is allocated (two tokens of 8000, so that scores need memory)
+  const int n = 80;
+  std::vector<int32_t> l(n, 8000), twos(n, 2);
   fc_pool* fresh = pool_of(FC_DTYPE_F16, 4, 128, ~(size_t)0);
   auto many = [&](const char* what, int n_req, bool captured) {
     g_capturing = captured;
-    report(what, fc_sparse_attention(fresh, 0, table, 16, l.data(), ones.data(), bounds, 3, &ok, 4, &ok, nullptr, n_req, 0.f, nullptr));
+    report(what, fc_sparse_attention(fresh, 0, table, 2048, l.data(), twos.data(), bounds, 3, &ok, 4, &ok, nullptr, n_req, 0.f, nullptr));
     g_capturing = false;
   };
-  many("captured_first", 100, true);
-  many("eager", 100, false);
+  many("captured_first", 70, true);
+  many("eager", 70, false);
   const char* used = fresh->sparse.data;
-  many("captured", 100, true);
+  many("captured", 70, true);
   printf("kept %d\n", (int)(fresh->sparse.captured && fresh->sparse.data == used));
   many("captured_many", n, true);  // (descriptors that no call left room for)
-  l.assign(4000, 200);
-  ones.assign(4000, 1);
-  report("eager_more", fc_sparse_attention(fresh, 0, table, 16, l.data(), ones.data(), bounds, 3, &ok, 4, &ok, nullptr, 4000, 0.f, nullptr));
+  l.assign(4000, 8000);
+  twos.assign(4000, 2);
+  report("eager_more", fc_sparse_attention(fresh, 0, table, 2048, l.data(), twos.data(), bounds, 3, &ok, 4, &ok, nullptr, 4000, 0.f, nullptr));
   printf("retired %d\n", (int)(fresh->retired.size() == 1 && fresh->retired[0] == used && !fresh->sparse.captured));
   for (fc_pool* p : {p4, p8, p16, other, fresh}) fc_pool_destroy(p);
   return 0;

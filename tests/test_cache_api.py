@@ -63,14 +63,16 @@ def test_what_is_launched(calls):
     # blocks: 7 + 3, of the new tokens 1 + 3
     assert lines["bounds"] == ["bounds0:10"] and lines["bounds_new"] == ["bounds2:4"] and lines["bounds8"] == ["bounds1:4"]
     assert lines["bounds_nothing"] == [] and lines["sparse_nothing"] == []
-    assert lines["sparse"] == ["select_inline:2:0x0:6", "attention1x4"]
-    assert lines["sparse4"] == ["select_inline:34:0x0:1", "attention3x4"] and lines["sparse8"][1] == "attention2x4"
+    # little to score: one launch for the tokens, which see 101 and 41 tokens, or one 101 and 33 9 to 41
+    assert lines["sparse"] == ["selected1_inline:2:6:0,101,0:1,41,1"]
+    assert lines["sparse4"] == ["selected3_inline:34:1:0,101,0:1,9,1:1,10,2"] and lines["sparse8"][0].startswith("selected2_inline:34:1:")
     # one long cache: its scores in a launch of their own, 1874 blocks in parts of 64
     assert lines["sparse_long"] == ["select_inline:1:1x30:1874", "attention1x4"]
-    assert lines["captured"] == lines["eager"] == ["select_inline:100:0x0:12", "attention1x4"]
+    assert lines["sparse_apart"] == ["select_inline:3:1x8:500", "attention2x4"] and lines["sparse_rows"][0].startswith("select_inline:2:1x1:6")
+    assert lines["captured"] == lines["eager"] == ["select_inline:140:70x140:499", "attention1x4"]
     reads = [[int(x) for x in c[1:]] for c in calls if c[0] == "reads"]
-    # three blocks of a cache of 101 (the last one holds 5 tokens), all of one of 41; 64 blocks of 30000
-    assert reads == [[1, 41, 1, 1], [0, 37, 1, 0], [0, 1024, 1, 0]]
+    # 64 blocks of 30000; of 8000 and of 8001 (the last one holds one token), all of 41
+    assert reads == [[0, 1024, 1, 0], [0, 1024, 1, 0], [1, 1009, 1, 1], [2, 41, 1, 2]]
 
 
 def test_scratch_of_captured_calls(calls):

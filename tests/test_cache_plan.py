@@ -80,12 +80,15 @@ def test_tokens_parts_and_what_they_read(plan):
         assert [tuple(t[:2]) for t in kinds["t"]] == seen and [t[2] for t in kinds["t"]] == list(range(len(seen)))
         scoring = [_blocks(n) for _, n in seen if _blocks(n) > n_select > 1]
         assert longest == max([nb - 1 for nb in scoring] + [1])
-        for row, ((r, n), a) in enumerate(zip(seen, kinds["a"])):
-            assert a == [row, n if _blocks(n) <= n_select else (n_select - 1) * 16 + (n - 1) % 16 + 1, 1, row]
+        single = all(new <= 1 for _, new in pairs)
+        assert (part == 0) == (group <= 32 and (longest <= 384 or (single and 2 * len(seen) * heads >= n_cu)))
         if part == 0:
-            assert all(new <= 1 for _, new in pairs) and group <= 32 and n_units == 0 and not kinds["q"]
+            assert n_units == 0 and not kinds["q"] and not kinds["a"]
             fused += 1
             continue
+        assert len(kinds["a"]) == len(seen)
+        for row, ((r, n), a) in enumerate(zip(seen, kinds["a"])):
+            assert a == [row, n if _blocks(n) <= n_select else (n_select - 1) * 16 + (n - 1) % 16 + 1, 1, row]
         apart += bool(scoring)
         assert part % 16 == 0 and part >= 64 and 1 <= tile and (tile * group <= 64)
         at, first = 0, {}

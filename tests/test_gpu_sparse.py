@@ -87,7 +87,8 @@ def _step(c, layer, n_select, bounds=None, want_selected=None, scale=0.0, **kw):
     ([1], [1], 1, 1, 64, 1), ([1], [1], 1, 1, 128, 9), ([300, 16, 17, 33, 0], [1, 1, 1, 3, 0], 2, 4, 128, 3),
     ([300, 97], [5, 2], 3, 1, 64, 1), ([500, 700], [1, 18], 2, 5, 64, 7), ([400], [1], 1, 40, 128, 6),
     ([260, 5, 64], [1, 1, 1], 40, 1, 64, 16),
-    ([290, 40], [4, 3], 2, 2, 64, 1), ([1200, 90, 333], [1, 1, 2], 1, 64, 64, 5)], ids=str)
+    ([290, 40], [4, 3], 2, 2, 64, 1), ([1200, 90, 333], [1, 1, 2], 1, 64, 64, 5), ([300, 90], [1, 2], 2, 20, 128, 4),
+    ([310, 50, 1], [1, 2, 1], 2, 32, 64, 4)], ids=str)
 def test_selection_and_attention(fmt, lens, news, heads, group, dim, n_select):
     c = Cache(lens, news, heads, group, dim, fmt=fmt, seed=n_select, layers=2 if fmt == "f16" else 1)
     try:
@@ -96,10 +97,13 @@ def test_selection_and_attention(fmt, lens, news, heads, group, dim, n_select):
         c.close()
 
 
-@pytest.mark.parametrize("lens,news,n_select", [([4100, 2000], [1, 2], 30), ([1041], [1], 64), ([1040], [1], 66), ([32768], [1], 2047)], ids=str)
-def test_long_caches(lens, news, n_select):
+@pytest.mark.parametrize("lens,news,n_select,fmt", [
+    ([4100, 2000], [1, 2], 30, "f16"), ([1041], [1], 64, "f16"), ([1040], [1], 66, "f16"), ([32768], [1], 2047, "f16"),
+    ([6300, 2000], [2, 2], 30, "f16"), ([6400, 300, 4600], [34, 3, 1], 7, "e2m1"), ([7000], [2], 100, "e4m3"),
+    ([7000, 4113], [1, 1], 100, "e2m1")], ids=str)
+def test_long_caches(lens, news, n_select, fmt):
     """Scores made by several workgroups, all of the keys that the selection can hold, segments of the result."""
-    c = Cache(lens, news, 1, 2, 64, fmt="f16", layers=1)
+    c = Cache(lens, news, 1, 2, 64, fmt=fmt, layers=1)
     try:
         _step(c, 0, n_select)
     finally:
@@ -107,7 +111,12 @@ def test_long_caches(lens, news, n_select):
 
 
 def test_many_heads_of_long_caches():
-    """One workgroup for scores and selection, of more than 64 blocks."""
+    """One workgroup for scores, selection and attention: many tokens of a few blocks, single ones of many."""
+    c = Cache([6400 + 16 * i for i in range(3)] * 7, [1] * 21, 7, 1, 64, fmt="f16", layers=1)
+    try:
+        _step(c, 0, 20)
+    finally:
+        c.close()
     c = Cache([1100 + 16 * i for i in range(3)] * 3, [20] * 9, 3, 1, 64, fmt="f16", layers=1)
     try:
         assert int(c.news.sum()) * c.heads >= 512
@@ -116,11 +125,10 @@ def test_many_heads_of_long_caches():
         c.close()
 
 
-@pytest.mark.parametrize("long", [False, True])
-def test_ties_go_to_the_lower_blocks(long):
+@pytest.mark.parametrize("n", [600, 4000, 7000])
+def test_ties_go_to_the_lower_blocks(n):
     """Queries of zeros, blocks that are the same, scores that differ in the last of 64 bits' places."""
     import torch
-    n = 4000 if long else 600
     c = Cache([n, n, n], [1, 1, 1], 1, 2, 64, fmt="f16", layers=1)
     try:
         c.q[0] = 0
@@ -141,10 +149,11 @@ def test_ties_go_to_the_lower_blocks(long):
         c.close()
 
 
-def test_scores_that_are_not_finite():
+@pytest.mark.parametrize("n", [400, 7000])
+def test_scores_that_are_not_finite(n):
     """Blocks with keys that are infinite or not numbers: they are read, and what they hold shows."""
     import torch
-    c = Cache([400, 400, 400], [1, 1, 1], 1, 1, 64, fmt="f16", layers=1)
+    c = Cache([n, n, n], [1, 1, 1], 1, 1, 64, fmt="f16", layers=1)
     try:
         c.q[:] = np.abs(c.q) + np.float16(0.1)
         c.kv[0, c.table[0, 5], 0, 0, 3, 2] = np.nan
