@@ -189,6 +189,7 @@ int plan_sparse(const PoolView& pool, int n_cu, int group, int n_select, const C
   // (workgroups that select have 512 threads)
   if (chunk.n_rows * pool.n_heads > kPlanMaxWorkgroups / 2) return fail(plan, PLAN_EINVAL, "batch too large for one launch");
   bool single = true;
+  int read = 0;  // most blocks of a token
   // (with one block, the token's own, nothing is scored)
   auto scores = [&](int nb) { return nb > n_select && n_select > 1; };
   for (const ChunkReq& q : chunk.reqs) {
@@ -197,10 +198,11 @@ int plan_sparse(const PoolView& pool, int n_cu, int group, int n_select, const C
       const int seen = q.seq_len - q.n_new + i + 1, nb = blocks_for(seen), row = q.row_off + i;
       plan->tokens.push_back({q.table_row, seen, 0, row, 0, 0});
       if (scores(nb)) plan->longest = std::max(plan->longest, nb - 1);
+      read = std::max(read, std::min(nb, n_select));
     }
   }
-  // One launch, a workgroup of four wavefronts for a token's head, where each has little to score, or where there are
-  // many, of single tokens; else the scores are made by as many workgroups as fill the card, and for the tokens of a
+  // One launch, a workgroup of four wavefronts for a token's head, where each has little to read and to score, or where
+  // there are many, of single tokens; else the scores are made by as many workgroups as fill the card, and for the tokens of a
   // request together.  us a step, fp16, n_select 64, one / apart, for so many single tokens times heads:
   //   tokens cached     8            32           64           128          192
   //   2000-2500         29.2 / 32.6  30.1 / 34.8  31.0 / 35.8  33.2 / 41.3  36.0 / 48.5
@@ -208,13 +210,18 @@ int plan_sparse(const PoolView& pool, int n_cu, int group, int n_select, const C
   //   8000-10000        33.3 / 32.0  37.0 / 36.6  38.0 / 38.8  40.0 / 47.4  43.5 / 56.8
   //   30000             52.0 / 32.4  53.6 / 37.9  54.8 / 41.6  59.0 / 60.9  65.8 / 85.1
   // five tokens of 32 caches of 1000-1250, 8 heads: 91 / 93, of 16 of 4000-5000 77 / 72; 256 of two of 16000: 463 / 302.
+  // By the blocks read, of 5000:
+  //   96                30.5 / 31.4  36.3 / 34.8  38.1 / 38.5  40.6 / 47.3  (256: 54 / 64)
+  //   256               56.4 / 32.5  59.6 / 38.8  62.7 / 48.9  68.9 / 69.8  (256: 104 / 114)
+  // and 384 of 1024 in caches of 100-30000 436 / 424, of whole ones 553 / 467: whole heads end unevenly.
   // (Up to half of the rows: what else is kept of the queries and blocks would not fit the LDS beside more.)
   const int cu = std::max(n_cu, 1);
-  if (group <= kScoreRows / 2 && (plan->longest <= 384 || (single && 2 * chunk.n_rows * pool.n_heads >= cu))) return PLAN_OK;
+  const bool many = 2 * chunk.n_rows * pool.n_heads >= cu;
+  if (group <= kScoreRows / 2 && read <= (many ? 256 : 64) && (plan->longest <= 384 || (single && many))) return PLAN_OK;
   for (const ChunkReq& t : plan->tokens) {
     // (whole blocks, but for the token's own, the last one)
-    const int read = (std::min(blocks_for(t.seq_len), n_select) - 1) * kPlanBlockSize + (t.seq_len - 1) % kPlanBlockSize + 1;
-    plan->attention.reqs.push_back({t.row_off, read, 1, t.row_off, 0, 0});
+    const int keys = (std::min(blocks_for(t.seq_len), n_select) - 1) * kPlanBlockSize + (t.seq_len - 1) % kPlanBlockSize + 1;
+    plan->attention.reqs.push_back({t.row_off, keys, 1, t.row_off, 0, 0});
   }
   plan->attention.n_rows = chunk.n_rows;
   plan->tile_tokens = std::max(1, kScoreRows / group);

@@ -94,7 +94,7 @@ struct fc_pool {
   fc::Scratch<int32_t> kept;
   size_t split_refused = ~(size_t)0;  // least score scratch of split heads that could not be had
   fc::Scratch<int32_t> ids;  // old ids then new ids
-  fc::Scratch<char> sparse;  // scores' order and selected blocks of fc_sparse_attention
+  fc::Scratch<char> sparse;  // scores and selected blocks of fc_sparse_attention
   std::vector<void*> retired;  // buffers that graphs use and calls do not any more
   char* dev_meta = nullptr;
   char* host_meta = nullptr;  // pinned

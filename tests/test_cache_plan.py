@@ -81,7 +81,9 @@ def test_tokens_parts_and_what_they_read(plan):
         scoring = [_blocks(n) for _, n in seen if _blocks(n) > n_select > 1]
         assert longest == max([nb - 1 for nb in scoring] + [1])
         single = all(new <= 1 for _, new in pairs)
-        assert (part == 0) == (group <= 32 and (longest <= 384 or (single and 2 * len(seen) * heads >= n_cu)))
+        many = 2 * len(seen) * heads >= n_cu
+        read = max([min(_blocks(n), n_select) for _, n in seen] + [0])
+        assert (part == 0) == (group <= 32 and read <= (256 if many else 64) and (longest <= 384 or (single and many)))
         if part == 0:
             assert n_units == 0 and not kinds["q"] and not kinds["a"]
             fused += 1
