@@ -184,6 +184,14 @@ def _rows(t, name, shape, f16):
     return Rows(t.data_ptr(), row if shape[0] > 1 else shape[1] * shape[2], head if shape[1] > 1 else shape[2])
 
 
+def _out_rows(out, name, q, shape, f16):
+    """(tensor, fc_rows) of a result: out, or a new tensor like q."""
+    if out is not None:
+        return out, _rows(out, name, shape, f16)
+    out = q.new_empty(shape)
+    return out, Rows(out.data_ptr(), shape[1] * shape[2], shape[2])
+
+
 def _stream_ptr(stream):
     if stream is not None:
         return stream.cuda_stream
@@ -631,9 +639,9 @@ def fc_rotate_store_chunk(pool, layer, block_tables, seq_lens, n_new, rotation, 
     if q is not None:
         n_q = q.shape[1]
         rows = (n_rows, n_q, d)
-        if q_out is None:
-            q_out = q.new_empty(rows)
-        q_rows, out_rows = ctypes.byref(_rows(q, "q", rows, f16)), ctypes.byref(_rows(q_out, "q_out", rows, f16))
+        q_rows = ctypes.byref(_rows(q, "q", rows, f16))
+        q_out, to = _out_rows(q_out, "q_out", q, rows, f16)
+        out_rows = ctypes.byref(to)
     elif q_out is not None:
         raise ValueError("q_out without q")
     _check(lib.fc_rotate_store_chunk(
@@ -673,15 +681,14 @@ def fc_sparse_attention(pool, layer, block_tables, seq_lens, n_new, bounds, n_se
     n_req, n_rows = _new_rows(block_tables, seq_lens, n_new)
     n_q = q.shape[1]
     rows = (n_rows, n_q, pool.head_dim)
-    if out is None:
-        out = q.new_empty(rows)
+    q_rows = _rows(q, "q", rows, torch.float16)
+    out, out_rows = _out_rows(out, "out", q, rows, torch.float16)
     if selected is not None and tuple(selected.shape) != (n_rows, pool.n_heads, n_select):
         raise ValueError("selected must be [sum n_new][n_heads][n_select]")
     _check(lib.fc_sparse_attention(
         pool.ptr, int(layer), _dev_ptr(block_tables, torch.int32), int(block_tables.shape[1]),
         _host_i32(seq_lens), _host_i32(n_new), _bounds_ptr(pool, bounds), int(n_select),
-        ctypes.byref(_rows(q, "q", rows, torch.float16)), n_q,
-        ctypes.byref(_rows(out, "out", rows, torch.float16)), _dev_ptr(selected, torch.int32), n_req,
+        ctypes.byref(q_rows), n_q, ctypes.byref(out_rows), _dev_ptr(selected, torch.int32), n_req,
         float(scale), _stream_ptr(stream)))
     return out
 
