@@ -680,9 +680,9 @@ int fc_rotate_store_chunk(fc_pool* pool, int layer, const int32_t* dev_block_tab
  *   - of the others the n_select - 1 with the best scores, ties to the lower entry of the
  *     table.  The score of a block is the largest over the query heads that
  *     share the head of  sum_c max(q_c * smallest_c, q_c * largest_c),  which no logit of the
- *     block exceeds (scale aside).  It is summed in 64 bits; a score that is not a
- *     number counts as larger than all others (of two products of which one is not a number
- *     the other one counts).
+ *     block exceeds (scale aside).  It is the sum of the exact products, rounded once to 64
+ *     bits; a score that is not a number counts as larger than all others (of two products of which
+ *     one is not a number the other one counts).
  * All of them where they are no more than n_select.  Over what it reads the
  * attention is that of fc_chunk_attention, whose arguments these are.
  *   dev_bounds    as fc_block_bounds left it (the token's own block is read whatever its entry)

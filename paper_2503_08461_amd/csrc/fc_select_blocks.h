@@ -10,8 +10,8 @@
 namespace fc {
 
 // ---------------------------------------------------------------------------
-// selection.  A score is a sum in 64 bits: a product of two fp16 numbers is exact in fp32, and which of
-// two blocks is read should follow from the inputs, not from the order in which a sum was made.  All
+// selection.  A score is a sum rounded once, to 64 bits (score_exactly): a product of two fp16 numbers is exact in
+// fp32, and which of two blocks is read should follow from the inputs, not from the order in which a sum was made.  All
 // scores are made by the matrix cores in fp32 first,
 //     S [query heads x blocks] = min(Q, 0) . LO^T + max(Q, 0) . HI^T,
 // which is the same sum, off by at most E = 2 D 2^-23 (largest sum of |q|) (largest |bound|): each of 2 D
@@ -163,6 +163,9 @@ struct BlockScores {  // W: wavefronts of the workgroup
 
 // The order of the scores in 64 bits of the n blocks listed, into keys[].  D / 8 neighbouring lanes a block;
 // sm_q: the queries [query head of the group][D].
+// A score is the sum rounded once, whatever the order: a product is a multiple of 2^-48 below 2^32, more than the 53
+// bits of a number can add up (2^30 + 2^-24 - 2^30), so its multiple of 2^-10 and what is left of it are added up apart,
+// up to 128 of each in 49 and 44 bits.
 template <int D, int W>
 __device__ __forceinline__ void score_exactly(const SelectParams& p, const _Float16* sm_q, int head, const int32_t* blocks, int n,
                                               uint64_t* keys) {
@@ -174,14 +177,24 @@ __device__ __forceinline__ void score_exactly(const SelectParams& p, const _Floa
     uint64_t best = 0;
     for (int h = 0; h < p.group; ++h) {
       const half8 q = load_half8(sm_q + h * D + piece * 8);
-      double s = 0.0;
+      double upper = 0.0, lower = 0.0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += (double)fmaxf((float)q[e] * (float)lo[e], (float)q[e] * (float)hi[e]);
-      s += from_lane_f64<0xB1>(s);
-      s += from_lane_f64<0x4E>(s);
-      s += from_lane_f64<0x141>(s);
-      if constexpr (PPR == 16) s += from_lane_f64<0x140>(s);
-      const uint64_t key = score_order(s);
+      for (int e = 0; e < 8; ++e) {
+        const double x = (double)fmaxf((float)q[e] * (float)lo[e], (float)q[e] * (float)hi[e]);
+        const double cut = (x + 0x1.8p42) - 0x1.8p42;
+        upper += cut;
+        lower += x - cut;
+      }
+      auto join = [](double& x) {
+        x += from_lane_f64<0xB1>(x);
+        x += from_lane_f64<0x4E>(x);
+        x += from_lane_f64<0x141>(x);
+        if constexpr (PPR == 16) x += from_lane_f64<0x140>(x);
+      };
+      join(upper);
+      join(lower);
+      // (of what is infinite nothing is left that is a number)
+      const uint64_t key = score_order(fabs(upper) < INFINITY ? upper + lower : upper);
       best = key > best ? key : best;
     }
     if (piece == 0) keys[i] = best;

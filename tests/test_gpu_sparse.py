@@ -149,6 +149,33 @@ def test_ties_go_to_the_lower_blocks(n):
         c.close()
 
 
+@pytest.mark.parametrize("n,lens", [(600, 1), (1600, 1), (7000, 1), (7000, 3)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_scores_whose_order_of_sums_would_decide(n, lens, dim):
+    """Sums that lose what blocks differ by where large products that cancel come first: the score is the sum
+    of all of them, rounded once."""
+    import torch
+    c = Cache([n] * lens, [1] * lens, 1, 2, dim, fmt="f16", layers=1)
+    try:
+        c.q[:] = 0
+        c.q[:, :, [0, 2]] = np.float16(2.0 ** 15)
+        c.q[:, :, 1] = 1
+        for r in range(lens):
+            ids = c.table[r, :blocks_for(n)]
+            c.kv[0, ids] = 0
+            for i, b in enumerate(ids):
+                # 2^30 + 2^-24 (7 i mod 61) - 2^30: 31 and 24 bits, 2 more than there are
+                c.kv[0, b, 0, :, :, 0] = np.float16(2.0 ** 15 if i % 2 else 0)
+                c.kv[0, b, 0, :, :, 1] = np.float16((i * 7 % 61) * 2.0 ** -24)
+                c.kv[0, b, 0, :, :, 2] = np.float16(-2.0 ** 15 if i % 2 else 0)
+        c.upload()
+        c.q_dev.copy_(torch.from_numpy(c.q))
+        for n_select in (2, 7, 25):
+            _step(c, 0, n_select, scale=2.0 ** -31)
+    finally:
+        c.close()
+
+
 @pytest.mark.parametrize("n", [400, 7000])
 def test_scores_that_are_not_finite(n):
     """Blocks with keys that are infinite or not numbers: they are read, and what they hold shows."""
