@@ -1,7 +1,8 @@
 // Rows of the 4-bit pool: e2m1 codes times one power of two for every 32 channels
-// (include/fastcache.h, "The 4-bit pool"), their layout and conversions.  The instructions'
-// rounding was compared with the definition for every fp16 number and exponent, and every value
-// with that of its code; a scale whose bits are 255 << 23 makes not-a-numbers of all codes.
+// (include/fastcache.h, "The 4-bit pool"), their layout and conversions.  The instructions round
+// as the definition has it, for every fp16 number under every exponent that its group can have, and every
+// value is its code's (tests/test_gpu_e2m1_conversions.py); a scale whose bits are 255 << 23 makes
+// not-a-numbers of all codes.
 #pragma once
 
 #include <type_traits>
