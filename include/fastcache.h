@@ -690,12 +690,15 @@ int fc_rotate_store_chunk(fc_pool* pool, int layer, const int32_t* dev_block_tab
  *   dev_selected  NULL, or dev, int32 [T][n_heads][n_select] (4-byte aligned): the table entries
  *                 that were read, ascending, -1 behind the last one
  *
- * Scores and the selection lie in scratch memory of the pool, which grows on demand: at most 4 bytes
- * for each of n_select and the longest cache's blocks, for every new token and head of K and V.
+ * Scores and the selection lie in scratch memory of the pool, which grows on demand: with B blocks
+ * of the longest cache at most T * n_heads * 4 * (n_select + B + B / 64 + 1) bytes for T new tokens,
+ * and an eighth more, in whole 4 KB (2048 tokens behind 28 000, 32 heads, n_select 64: 0.6 GB).  A chunk whose
+ * memory is too much is passed in parts, each with the length that it leaves.
  *
  * Both are asynchronous on `stream` and not part of the kernel times.  FC_EINVAL as for
  * fc_store_chunk and fc_chunk_attention; n_select outside its range, NULL or misaligned
  * dev_bounds, 2^24 or more blocks (fc_block_bounds), 2^23 or more tokens times heads of K and V.
+ * FC_EDEVICE if the scratch memory cannot be had: nothing has been queued, the pool is as it was.
  */
 int fc_block_bounds(fc_pool* pool, int layer, const int32_t* dev_block_tables,
                     int max_blocks_per_req, const int32_t* host_seq_lens,

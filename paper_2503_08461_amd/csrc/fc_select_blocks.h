@@ -165,8 +165,8 @@ struct BlockScores {  // W: wavefronts of the workgroup
 // sm_q: the queries [query head of the group][D].
 // A score is the sum rounded once, whatever the order: a product is a multiple of 2^-48 below 2^32, more than the 53
 // bits of a number can add up (2^30 + 2^-24 - 2^30), so its multiple of 2^-10 and what is left of it are added up apart,
-// up to 128 of each in 49 and 44 bits.  (One sum in 64 bits, whose order decides between such blocks: sparse_tokens of
-// the cases 55.5 us, so 55.9; 10 tokens over 28 000-30 000 32.2, 32.7)
+// up to 128 of each in 49 and 44 bits.  (One sum in 64 bits, whose order decides between such blocks: a step of
+// single tokens of 48 caches of 1280-7040, 8 heads of 4, 55.5 us, so 55.9; of 10 tokens over 28 000-30 000 32.2, 32.7)
 template <int D, int W>
 __device__ __forceinline__ void score_exactly(const SelectParams& p, const _Float16* sm_q, int head, const int32_t* blocks, int n,
                                               uint64_t* keys) {
@@ -234,39 +234,28 @@ __device__ __forceinline__ uint32_t places_of(int mine, One one, Two two, uint32
   return (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
 }
 
-// The k-th largest of n > k > 0 keys, key[j] of thread t being that of element j * 64 * W + t (0: none; Key: 32 or
-// 64 bits, no key is 0): a threshold that exactly k keys reach, or the k-th one itself where more do.  Two bits at a
-// time from the first one in which keys differ, with three counts of all keys a step.  reached: how many keys reach it.
-template <typename Key>
-struct FoundKey {
-  Key threshold;
-  int reached;
-};
-template <int W, typename Key>
-__device__ __forceinline__ FoundKey<Key> kth_largest(const Key (&key)[kPerThread<W>], int n, int k) {
+// The k-th largest of n > k > 0 keys, key[j] of thread t being that of element j * 64 * W + t (0: none, no key is 0):
+// a threshold that exactly k keys reach, or the k-th one itself where more do.  Two bits at a time from the first one
+// in which keys differ, with three counts of all keys a step.
+template <int W>
+__device__ __forceinline__ uint64_t kth_largest(const uint64_t (&key)[kPerThread<W>], int n, int k) {
   typedef int int4v __attribute__((ext_vector_type(4)));
   __shared__ int4v sm_count[2][W];
-  __shared__ Key sm_most[W], sm_least[W];
-  constexpr int kBits = 8 * sizeof(Key);
+  __shared__ uint64_t sm_most[W], sm_least[W];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int mine = (n + 64 * W - 1) / (64 * W);  // uniform
-  Key most = 0, least = ~(Key)0;
+  uint64_t most = 0, least = ~0ull;
 #pragma unroll
   for (int j = 0; j < kPerThread<W>; ++j) {
     most = key[j] > most ? key[j] : most;
     least = key[j] != 0 && key[j] < least ? key[j] : least;
   }
-  if constexpr (kBits == 32) {
-    most = wave_max(most);
-    least = wave_min(least);
-  } else {
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-      const Key a = __shfl_xor((unsigned long long)most, d), b = __shfl_xor((unsigned long long)least, d);
-      most = a > most ? a : most;
-      least = b < least ? b : least;
-    }
+  for (int d = 32; d > 0; d >>= 1) {
+    const uint64_t a = __shfl_xor((unsigned long long)most, d), b = __shfl_xor((unsigned long long)least, d);
+    most = a > most ? a : most;
+    least = b < least ? b : least;
   }
   if (lane == 0) {
     sm_most[wave] = most;
@@ -279,14 +268,14 @@ __device__ __forceinline__ FoundKey<Key> kth_largest(const Key (&key)[kPerThread
     least = sm_least[w] < least ? sm_least[w] : least;
   }
   // all keys have the bits above the pair of the first one in which the largest and the smallest differ
-  const Key differ = (most ^ least) | 1;
-  int shift = (kBits - 1 - (kBits == 64 ? __builtin_clzll((uint64_t)differ) : __builtin_clz((uint32_t)differ))) & ~1;
-  FoundKey<Key> f = {shift == kBits - 2 ? (Key)0 : most >> (shift + 2) << (shift + 2), n};
-  for (int step = 0; shift >= 0 && f.reached != k; shift -= 2, ++step) {
+  int shift = (63 - __builtin_clzll((most ^ least) | 1)) & ~1;
+  uint64_t threshold = shift == 62 ? 0 : most >> (shift + 2) << (shift + 2);
+  int reached = n;  // by so many keys
+  for (int step = 0; shift >= 0 && reached != k; shift -= 2, ++step) {
     int count[4] = {};
 #pragma unroll
     for (int d = 1; d < 4; ++d) {
-      const Key candidate = f.threshold | (Key)d << shift;
+      const uint64_t candidate = threshold | (uint64_t)d << shift;
 #pragma unroll
       for (int j = 0; j < kPerThread<W>; ++j)
         if (j < mine) count[d] += __popcll(__ballot(key[j] >= candidate));
@@ -297,10 +286,10 @@ __device__ __forceinline__ FoundKey<Key> kth_largest(const Key (&key)[kPerThread
 #pragma unroll
     for (int w = 0; w < W; ++w) sum += sm_count[step & 1][w];
     const int d = sum[3] >= k ? 3 : sum[2] >= k ? 2 : sum[1] >= k ? 1 : 0;
-    f.threshold |= (Key)d << shift;
-    if (d > 0) f.reached = d == 3 ? sum[3] : d == 2 ? sum[2] : sum[1];
+    threshold |= (uint64_t)d << shift;
+    if (d > 0) reached = d == 3 ? sum[3] : d == 2 ? sum[2] : sum[1];
   }
-  return f;
+  return threshold;
 }
 
 // What a selection needs of LDS: blocks between, their keys, whether they are kept.
@@ -454,15 +443,15 @@ __device__ __forceinline__ void select_best(const SelectParams& p, const _Float1
     const int i = j * 64 * W + (int)threadIdx.x;
     exact[j] = i < n_between ? between.keys[i] : 0;
   }
-  const FoundKey<uint64_t> f = kth_largest<W, uint64_t>(exact, n_between, wanted);
+  const uint64_t threshold = kth_largest<W>(exact, n_between, wanted);
   // of the keys that are equal to the threshold the first ones stay
   uint32_t place[kPerThread<W>];
-  const uint32_t n_above = places_of<W>(parts, [&](int j) { return exact[j] > f.threshold; }, [&](int j) { return exact[j] == f.threshold; },
+  const uint32_t n_above = places_of<W>(parts, [&](int j) { return exact[j] > threshold; }, [&](int j) { return exact[j] == threshold; },
                                      sm_place, place) & 0xffff;
 #pragma unroll
   for (int j = 0; j < kPerThread<W>; ++j) {
     const int i = j * 64 * W + (int)threadIdx.x;
-    if (i < n_between) between.blocks[i] = exact[j] > f.threshold || (exact[j] == f.threshold && (place[j] >> 16) < (uint32_t)wanted - n_above);
+    if (i < n_between) between.blocks[i] = exact[j] > threshold || (exact[j] == threshold && (place[j] >> 16) < (uint32_t)wanted - n_above);
   }
   __syncthreads();
   uint64_t keep = 0;
