@@ -52,7 +52,7 @@ typedef struct fc_pool fc_pool; /* opaque, owned by the library */
 
 enum { FC_OK = 0, FC_EINVAL = -1, FC_ENOMEM = -2, FC_EDEVICE = -3 };
 enum { FC_METHOD_NONE = 0, FC_METHOD_SNAPKV = 1, FC_METHOD_KNORM = 2, FC_METHOD_STREAMING = 3 };
-enum { FC_DTYPE_F16 = 0, FC_DTYPE_E4M3 = 1, FC_DTYPE_E2M1 = 3 };
+enum { FC_DTYPE_F16 = 0, FC_DTYPE_E4M3 = 1, FC_DTYPE_E2M1 = 3 }; /* 2 stays refused, as it was before 3 came */
 
 #define FC_BLOCK_SIZE 16      /* tokens per pool block (the only supported value) */
 #define FC_MAX_WINDOW 64      /* largest observation window */
@@ -693,7 +693,7 @@ int fc_rotate_store_chunk(fc_pool* pool, int layer, const int32_t* dev_block_tab
  * Scores and the selection lie in scratch memory of the pool, which grows on demand: with B blocks
  * of the longest cache at most T * n_heads * 4 * (n_select + B + B / 64 + 1) bytes for T new tokens,
  * and an eighth more, in whole 4 KB (2048 tokens behind 28 000, 32 heads, n_select 64: 0.6 GB).  A chunk whose
- * memory is too much is passed in parts, each with the length that it leaves.
+ * memory is too much is passed in parts, each with the cache's length at its end.
  *
  * Both are asynchronous on `stream` and not part of the kernel times.  FC_EINVAL as for
  * fc_store_chunk and fc_chunk_attention; n_select outside its range, NULL or misaligned

@@ -94,7 +94,8 @@ typedef __amdgpu_buffer_rsrc_t BufferPtr;
 __device__ __forceinline__ BufferPtr buffer_of(const void* base, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
 }
-// kOnce: the line is the first to leave the caches (no workgroup but this one reads it).
+// kOnce: the line is the first to leave the caches: no other workgroup reads it, but for the tokens of one request that
+// select their blocks each for itself (what these share comes from memory again where it has left).
 template <bool kOnce>
 __device__ __forceinline__ void load_to_lds(BufferPtr from, int lane_offset, half8* to) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, lane_offset, 0, 0,
@@ -1539,6 +1540,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, Reqs re
 // on its CU selects, and the blocks' numbers stay in LDS.  Single tokens of 48 caches of 1280-7040, 8 heads of four,
 // n_select 64, with the bounds before (us, apart / so): fp16 63.5 / 56.6, 8 bits 49 / 42.7, 4 bits 45.5 / 36.8; 256
 // blocks of 32 caches 97 / 84; in 4 bits 16 caches of 1000-4000, 32 heads, 43 / 34.
+// (4 bits, up to 16 rows, 128 channels: 128 registers would do for four workgroups a CU, its 43 KB of LDS for three;
+// 384 heads on 256 CUs are one or two, so that a head's chain shows: 36 us where the bytes take 16.)
 constexpr int kSelectedWaves = 4;
 template <int D, int SRC, bool kFew4, typename Reqs>
 __global__ __launch_bounds__(64 * kSelectedWaves, kFew4 ? 4 : 2) void attention_selected_kernel(SelectParams sp, AttnParams p, Reqs tokens, int ids_at) {

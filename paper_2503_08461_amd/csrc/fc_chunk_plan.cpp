@@ -214,6 +214,15 @@ int plan_sparse(const PoolView& pool, int n_cu, int group, int n_select, const C
   //   96                30.5 / 31.4  36.3 / 34.8  38.1 / 38.5  40.6 / 47.3  (256: 54 / 64)
   //   256               56.4 / 32.5  59.6 / 38.8  62.7 / 48.9  68.9 / 69.8  (256: 104 / 114)
   // and 384 of 1024 in caches of 100-30000 436 / 424, of whole ones 553 / 467: whole heads end unevenly.
+  // 8 bits and 4, which the rule treats alike, one / apart:
+  //   tokens cached     8            64           192              8            64           192
+  //   2000-2500         24.8 / 23.9  27.2 / 29.1  28.5 / 37.9      20.7 / 20.9  23.4 / 26.5  24.3 / 33.7
+  //   4000-5000         26.3 / 24.3  29.8 / 31.1  31.1 / 40.1      23.0 / 21.8  26.0 / 28.1  27.0 / 35.7
+  //   8000-10000        30.7 / 25.0  34.0 / 32.0  35.9 / 45.6      26.2 / 21.6  30.2 / 29.3  31.7 / 41.2
+  //   30000             51.3 / 26.9  52.6 / 38.4  60.6 / 77.6      47.3 / 24.2  48.5 / 35.5  55.9 / 72.9
+  //   256 of 5000       55.3 / 25.5  56.8 / 39.5  58.4 / 70.7      42.0 / 22.3  43.8 / 33.7  45.0 / 49.1
+  // Near a border the other side is ahead by 2 to 3 us in some, most where 128 heads read 256 blocks (8 bits 57 / 50) and for
+  // five tokens of 16 caches of 4000-5000 (fp16 75 / 72, 8 bits 59 / 55, 4 bits 40 / 42).
   // (Up to half of the rows: what else is kept of the queries and blocks would not fit the LDS beside more.)
   const int cu = std::max(n_cu, 1);
   const bool many = 2 * chunk.n_rows * pool.n_heads >= cu;

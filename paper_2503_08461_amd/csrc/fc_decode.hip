@@ -255,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void decode_attention_kernel(DecodeParams
 // channels two blocks.  Codes become fp32 numbers (exactly); a row's power of two multiplies the
 // key's logit and the value's weight, a group's, which is the lane's own, goes into the conversion.
 // 8 bits: HBM bounds it where the call has heads to offer (48 caches of 1280-7040, 2 layers: 6.4 TB/s), 4 bits too
-// (the same: 261 us, 6.5 TB/s; 8 caches of 256-1408, 32 heads: 10.9 us, one workgroup a head, the longest decides);
+// (the same: 260 us, 6.5 TB/s of what is required; 8 caches of 256-1408, 32 heads: 9.9 us, one workgroup a head, the longest decides);
 // with a block in the time of half a one the loads' latency shows earlier, so a wavefront asks
 // for the next block before it works on this one also over whole heads (4 caches of 1000-1200,
 // 32 heads: 27.2 -> 15.6 us), and its rows' states are joined by lane exchanges, not in LDS

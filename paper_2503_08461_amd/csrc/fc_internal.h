@@ -35,7 +35,8 @@ struct DecodeReqList {  // requests on the device
 static_assert(sizeof(DecodeReq) == 24, "tests count on the sizes of descriptors and argument blocks");
 static constexpr size_t kMaxArgumentBytes = 4096;  // what the arguments of a kernel may take
 
-// How a pool holds its rows (the members `e4m3` below): fp16, in 8 bits (fc_e4m3.h), in 4 (fc_e2m1.h).
+// How a pool holds its rows (the members `e4m3` below, which are older than the third form): fp16, in 8 bits
+// (fc_e4m3.h), in 4 (fc_e2m1.h).
 enum { ROWS_F16 = 0, ROWS_E4M3 = 1, ROWS_E2M1 = 2 };
 
 struct DecodeParams {
@@ -55,7 +56,7 @@ struct DecodeParams {
   float scale_log2e;
   // attention: blocks per segment of a head, segments of the longest one (1: no head is cut)
   int32_t seg_blocks, n_seg;
-  int32_t wide;            // 8- or 4-bit pool, no head cut: 16 wavefronts a head
+  int32_t wide;            // 8- or 4-bit pool, no head cut: 16 (of 4 bits 8) wavefronts a head
   float* partial;          // [n_req * layers * heads][n_seg][state_words] states of the segments
   int32_t* owner;          // ownership checks (debug mode), else NULL
   int32_t* error_flag;

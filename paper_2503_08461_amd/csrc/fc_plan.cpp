@@ -595,6 +595,15 @@ void plan_decode_segments(const PoolView& pool, int n_cu, bool over_kept, Decode
 //   1 of 30000           54.6     49.7  47.9
 //   16 of 130-16384       186      192   210
 //   1 of 8000                                            20.7  17.6  18.7
+// 4 bits, whose whole heads 8 wavefronts take, go the same way:
+//   8 caches of 256-1408       8 wavefronts  9.8   segments 12.8   four wavefronts 13.6
+//   4 of 1000-1200                           8.8             9.5                   11.4
+//   1 of 8000                               36.0            12.2                   57.1
+//   3 of 2000-2400 (8 heads of 64)          10.5             9.9                   14.2
+//   a share's          eighth  quarter  half     at least 16   32    64
+//   1 of 30000           33.7     28.2  26.6
+//   1 of 8000                                            16.8  12.2  12.1
+// (one cache of 2000, of 8 bits 15.4 whole and 10.3 in segments, of 4 11.6 and 8.8, is on the wrong side of kPlanWideE4m3.)
 void plan_decode_segments_e4m3(const PoolView& pool, int n_cu, DecodePlan* plan, int max_segments) {
   if (plan->reqs.empty()) return;
   const int64_t units = (int64_t)plan->reqs.size() * pool.n_layers * pool.n_heads;
