@@ -18,6 +18,7 @@ APART = [
     ([1100, 60, 700], [2, 1, 3], 2, 40, 64, 6),       # more rows than the one launch takes
     ([1300, 1113, 300], [1, 1, 1], 5, 4, 64, 66),     # single tokens, one of which reads all of its blocks
     ([1500], [17], 4, 5, 128, 65),                    # twelve tokens a tile, two tiles
+    ([1500], [2], 2, 40, 128, 70),                    # many rows a token, cut into segments
 ]
 # the same over 4 bits without a selection: lens, new tokens, heads, query heads of each, channels
 FEW_ROWS = [([1500, 2100], [1, 4], 3, 4, 128), ([2500, 40, 1111], [2, 1, 2], 2, 8, 64)]
